@@ -24,6 +24,7 @@
 #include <string>
 #include <vector>
 
+#include "lx_block.h"
 #include "lx_internal.h"
 #include "lx_tiles.h"
 
@@ -91,6 +92,35 @@ struct Timed {
     if (_e != hipSuccess)                                                              \
       return fail(LX_ERR_HIP, std::string(NAME) + ": " + hipGetErrorString(_e));       \
   } while (0)
+
+}  // namespace
+
+void clear_error() noexcept { g_err.clear(); }
+
+lx_status set_error(lx_status s, const char* what, const char* detail) noexcept {
+  try {
+    g_err = what;
+    if (detail) g_err.append(": ").append(detail);
+  } catch (...) {  // no memory for the message: the status still stands
+    g_err.clear();
+  }
+  return s;
+}
+
+hipError_t launch_timed(const char* name, hipStream_t s, hipError_t (*launch)(const void*, hipStream_t),
+                        const void* args) noexcept {
+  if (!g_prof) return launch(args, s);
+  try {
+    Timed t(name, s);
+    const hipError_t e = launch(args, s);
+    t.done();
+    return e;
+  } catch (...) {  // no memory for the timing record
+    return hipErrorOutOfMemory;
+  }
+}
+
+namespace {
 
 // --------------------------------------------------------------- planning
 size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
