@@ -5,6 +5,7 @@
 #include "lx_vec.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lx {
 namespace {
@@ -166,6 +167,260 @@ __global__ __launch_bounds__(256) void k_mx4_gemm(const Mx4GemmArgs a) {
   }
 }
 
+// ---------------------------------------------------------------- large tiles
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+// One direct memory -> LDS load per lane: lane i fills LDS bytes [dst + SIZE i,
+// + SIZE) from base + its own 32-bit byte offset (base and dst are uniform).
+// Inline asm, so that the only waits on it are the ones written below; M0 is
+// written here only, and the s_nop is the wait state that the load needs after
+// a write of M0.
+template <int SIZE>
+__device__ __forceinline__ void load_lds(const void* base, uint32_t off, const void* dst) {
+  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)dst);
+  if constexpr (SIZE == 16)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory");
+}
+
+// All of this wavefront's loads and LDS accesses are done, then every
+// wavefront's.
+__device__ __forceinline__ void drain_and_meet() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Row tiles over all groups (tiles of BM rows counted group by group).
+template <int BM>
+__device__ __forceinline__ int count_tiles(const Mx4GemmArgs& a) {
+  if (!a.offsets) return (a.M + BM - 1) / BM;
+  const int lane = threadIdx.x & 63;
+  int all = 0;
+  for (int g0 = 0; g0 < a.G; g0 += 64) {
+    int n = 0;
+    if (g0 + lane < a.G) {
+      const int lo = min(max(a.offsets[g0 + lane], 0), a.M);
+      n = (min(max(a.offsets[g0 + lane + 1], lo), a.M) - lo + BM - 1) / BM;
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
+    all += n;
+  }
+  return __builtin_amdgcn_readfirstlane(all);
+}
+
+// BM x BN outputs per workgroup, a 2 x 2 grid of wavefronts, 32x32x64
+// instructions. Both operands go memory -> LDS directly in steps of 256 values
+// (128 bytes a row), two steps in a ring: one streams in while the other is
+// multiplied. Inside a step's image the eight 16-byte chunks of a row are
+// XORed with (row / 2) % 8, so the 16 lanes that a read serves together hit 16
+// different bank groups; a lane fetches the chunk that belongs at its LDS
+// place. The scales of a step are 8 bytes a row. The weights are the
+// instruction's first operand: a lane ends with 4 consecutive columns of one
+// row, which go through LDS into whole rows.
+template <int BM, int BN>
+__global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_mx4_gemm_tile(const Mx4GemmArgs a) {
+  constexpr int WM = BM / 2, WN = BN / 2, MI = WM / 32, NI = WN / 32;
+  constexpr int RA = BM / 32, RB = BN / 32;      // 16-byte loads of a thread per step
+  constexpr int SA = BM / 128, SB = BN / 128;    // 4-byte scale loads of a thread per step
+  constexpr int STAGE = (BM + BN) * 136;
+  constexpr int EROW = WN + 4;                   // floats of an epilogue row
+  constexpr int LDS = 2 * STAGE > 4 * 32 * EROW * 4 ? 2 * STAGE : 4 * 32 * EROW * 4;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
+
+  // work item: XCD x (workgroups go round the 8 XCDs) takes a contiguous range;
+  // column tiles in bands of 8, so that what an XCD runs together shares rows
+  // and weights in its L2
+  const int ntn = (a.N + BN - 1) / BN;
+  const int R = count_tiles<BM>(a);
+  const int64_t items = (int64_t)R * ntn;
+  const int x = blockIdx.x & 7;
+  const int64_t per = items / 8, rest = items % 8, i = blockIdx.x >> 3;
+  if (i >= per + (x < rest)) return;
+  const int64_t L = x * per + min((int64_t)x, rest) + i;
+  const int64_t per_band = (int64_t)R * 8;
+  const int band = (int)(L / per_band), w = min(8, ntn - band * 8);
+  const int rem = (int)(L - band * per_band), ti = rem / w;
+  const int n0 = (band * 8 + rem - ti * w) * BN;
+  int g, m0, m1;
+  if (!find_tile<BM>(a, ti, g, m0, m1)) return;
+  g = __builtin_amdgcn_readfirstlane(g);
+  m0 = __builtin_amdgcn_readfirstlane(m0);
+  m1 = __builtin_amdgcn_readfirstlane(m1);
+
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int lane = tid & 63;
+  const int l32 = lane & 31, h = lane >> 5;
+  const int wm = wave >> 1, wn = wave & 1;
+  const int cp = a.Kp / 2, sp = a.Kp / 32, steps = (a.Kp + 255) / 256;
+  const bool odd = a.Kp & 128;  // the last step holds 128 values
+
+  // a row that is not there (past the tile, or a map entry out of range) reads
+  // A's first row (the host sees to it that there is one); its results are
+  // dropped
+  auto row_of = [&](int r) {
+    const int m = m0 + r;
+    if (m >= m1) return -1;
+    const int q = a.row_map ? a.row_map[m] : m;
+    return q >= 0 && q < a.a_rows ? q : -1;
+  };
+  // byte offsets from A (the host sees to it that they fit 32 bits) and from
+  // the tile's first weight row
+  uint32_t oa[RA], ob[RB], qa[SA], qb[SB];
+  const uint8_t* const B = a.b + ((int64_t)g * a.N + n0) * cp;
+  const uint8_t* const Bs = a.bs + ((int64_t)g * a.N + n0) * sp;
+#pragma unroll
+  for (int j = 0; j < RA; ++j) {
+    const int r = (j * 256 + tid) >> 3;
+    oa[j] = (uint32_t)max(row_of(r), 0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
+  }
+#pragma unroll
+  for (int j = 0; j < RB; ++j) {
+    const int r = (j * 256 + tid) >> 3;
+    ob[j] = (uint32_t)min(r, a.N - 1 - n0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
+  }
+#pragma unroll
+  for (int j = 0; j < SA; ++j) qa[j] = (uint32_t)max(row_of((j * 256 + tid) >> 1), 0) * (uint32_t)sp + (tid & 1) * 4;
+#pragma unroll
+  for (int j = 0; j < SB; ++j) qb[j] = (uint32_t)min((j * 256 + tid) >> 1, a.N - 1 - n0) * (uint32_t)sp + (tid & 1) * 4;
+  // step t of the operands into stage t % 2
+  auto issue = [&](int t) {
+    uint8_t* const st = smem + (t & 1) * STAGE;
+    if (odd && t == steps - 1) {
+      // a half step: the upper chunks and scales repeat the lower ones (they are
+      // not multiplied)
+#pragma unroll
+      for (int j = 0; j < RA; ++j) oa[j] -= (tid ^ (((j * 256 + tid) >> 3) >> 1)) & 4 ? 64 : 0;
+#pragma unroll
+      for (int j = 0; j < RB; ++j) ob[j] -= (tid ^ (((j * 256 + tid) >> 3) >> 1)) & 4 ? 64 : 0;
+#pragma unroll
+      for (int j = 0; j < SA; ++j) qa[j] -= (tid & 1) * 4;
+#pragma unroll
+      for (int j = 0; j < SB; ++j) qb[j] -= (tid & 1) * 4;
+    }
+    const int64_t at = (int64_t)t * 128;
+#pragma unroll
+    for (int j = 0; j < RA; ++j) load_lds<16>(a.a + at, oa[j], st + (j * 4 + wave) * 1024);
+#pragma unroll
+    for (int j = 0; j < RB; ++j) load_lds<16>(B + at, ob[j], st + BM * 128 + (j * 4 + wave) * 1024);
+#pragma unroll
+    for (int j = 0; j < SA; ++j) load_lds<4>(a.as + t * 8, qa[j], st + (BM + BN) * 128 + (j * 4 + wave) * 256);
+#pragma unroll
+    for (int j = 0; j < SB; ++j) load_lds<4>(Bs + t * 8, qb[j], st + (BM + BN) * 128 + BM * 8 + (j * 4 + wave) * 256);
+  };
+
+  f32x16 acc[MI][NI];
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
+
+  // step t: a row's scales; a lane's block of instruction s is 2 s + h, so after
+  // a shift by h bytes its scale is byte 0 or 2 of word s / 2
+  const uint8_t* const la = smem + (wm * WM + l32) * 128;
+  const uint8_t* const lb = smem + (BM + wn * WN + l32) * 128;
+  const uint8_t* const lsa = smem + (BM + BN) * 128 + (wm * WM + l32) * 8;
+  const uint8_t* const lsb = smem + (BM + BN) * 128 + (BM + wn * WN + l32) * 8;
+  const int swz = (l32 >> 1) & 7;
+  auto step = [&](int t, auto count) __attribute__((always_inline)) {
+    constexpr int S = decltype(count)::value;  // instructions along K
+    const int st = (t & 1) * STAGE;
+    uint2 sa[MI], sb[NI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      sa[mi] = *(const uint2*)(lsa + st + mi * 256);
+      sa[mi].x >>= 8 * h;
+      sa[mi].y >>= 8 * h;
+    }
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+      sb[ni] = *(const uint2*)(lsb + st + ni * 256);
+      sb[ni].x >>= 8 * h;
+      sb[ni].y >>= 8 * h;
+    }
+    uint4 fa[2][MI], fb[2][NI];
+    auto read = [&](int s) __attribute__((always_inline)) {
+      const int c = st + ((2 * s + h) ^ swz) * 16;
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) fb[s & 1][ni] = *(const uint4*)(lb + ni * 4096 + c);
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) fa[s & 1][mi] = *(const uint4*)(la + mi * 4096 + c);
+    };
+    read(0);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      if (s + 1 < S) read(s + 1);
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) {
+          const uint32_t wb = s < 2 ? sb[ni].x : sb[ni].y, wa = s < 2 ? sa[mi].x : sa[mi].y;
+          acc[mi][ni] = s & 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(fb[1][ni]), frag(fa[1][mi]), acc[mi][ni],
+                                                                              4, 4, 2, wb, 2, wa)
+                              : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(fb[0][ni]), frag(fa[0][mi]), acc[mi][ni],
+                                                                              4, 4, 0, wb, 0, wa);
+        }
+    }
+  };
+  issue(0);
+  drain_and_meet();
+  const int full = a.Kp / 256;
+  for (int t = 0; t < full; ++t) {
+    if (t + 1 < steps) issue(t + 1);
+    step(t, std::integral_constant<int, 4>{});
+    drain_and_meet();
+  }
+  if (odd) {
+    step(full, std::integral_constant<int, 2>{});
+    drain_and_meet();
+  }
+
+  // epilogue: 32 rows at a time through this wavefront's own LDS (the empty asm
+  // keeps its addresses from being formed before the loop, where they would not
+  // fit in registers)
+  asm volatile("" : "+v"(lane));
+  float* const e = (float*)smem + wave * 32 * EROW;
+  const int nb = n0 + wn * WN;
+  const bool vec = a.N % 8 == 0;
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) {
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(vf4*)(e + l32 * EROW + ni * 32 + q * 8 + h * 4) =
+            vf4{acc[mi][ni][4 * q], acc[mi][ni][4 * q + 1], acc[mi][ni][4 * q + 2], acc[mi][ni][4 * q + 3]};
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int LPR = WN / 8, RPI = 64 / LPR;  // lanes of a row, rows per round
+    const int c = (lane % LPR) * 8;
+#pragma unroll 4
+    for (int r0 = 0; r0 < 32; r0 += RPI) {
+      const int r = wm * WM + mi * 32 + r0 + lane / LPR, m = m0 + r;
+      const vf4 u = *(const vf4*)(e + (r0 + lane / LPR) * EROW + c), v = *(const vf4*)(e + (r0 + lane / LPR) * EROW + c + 4);
+      if (m < m1 && nb + c < a.N) {
+        F8 o{{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]}};
+        if (a.row_map && row_of(r) < 0) o = F8{};
+        const int64_t at = (int64_t)m * a.N + nb + c;
+        if (vec) {
+          store8(a.out, a.out_f32, at, o);
+        } else {
+          for (int k = 0; k < 8; ++k)
+            if (nb + c + k < a.N) {
+              if (a.out_f32)
+                ((float*)a.out)[at + k] = o.v[k];
+              else
+                ((uint16_t*)a.out)[at + k] = (uint16_t)pack_bf16(o.v[k], 0.f);
+            }
+        }
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
 }  // namespace
 
 hipError_t launch_mx4_quantize(const Mx4Args& a, hipStream_t s) {
@@ -180,7 +435,20 @@ hipError_t launch_mx4_dequantize(const Mx4Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int BM, int BN>
+static hipError_t launch_tile(const Mx4GemmArgs& a, hipStream_t s) {
+  const int64_t tiles = a.offsets ? std::min<int64_t>((int64_t)a.M / BM + a.G, a.M) : ((int64_t)a.M + BM - 1) / BM;
+  const int64_t items = tiles * (((int64_t)a.N + BN - 1) / BN);
+  k_mx4_gemm_tile<BM, BN><<<(unsigned)((items + 7) / 8 * 8), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
 hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s) {
+  const int rows = a.M / a.G;  // of a group on average
+  // the tile kernels address A and a tile's weights by 32-bit byte offsets
+  const bool near = (int64_t)a.a_rows * (a.Kp / 2) < ((int64_t)1 << 32) && a.a_rows > 0;
+  if (near && rows >= 512) return launch_tile<256, 256>(a, s);
+  if (near && rows >= 32) return launch_tile<128, 128>(a, s);
   const int tiles = a.offsets ? (int)std::min<int64_t>((int64_t)a.M / 16 + a.G, a.M) : (a.M + 15) / 16;
   k_mx4_gemm<<<dim3(tiles, (a.N + 63) / 64), 256, 0, s>>>(a);
   return hipGetLastError();
