@@ -318,65 +318,84 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_mx4_gemm_t
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
 
-  // step t: a row's scales; a lane's block of instruction s is 2 s + h, so after
-  // a shift by h bytes its scale is byte 0 or 2 of word s / 2
+  // a row's scales of a step: a lane's block of instruction s is 2 s + h, so
+  // after a shift by h bytes its scale is byte 0 or 2 of word s / 2
   const uint8_t* const la = smem + (wm * WM + l32) * 128;
   const uint8_t* const lb = smem + (BM + wn * WN + l32) * 128;
   const uint8_t* const lsa = smem + (BM + BN) * 128 + (wm * WM + l32) * 8;
   const uint8_t* const lsb = smem + (BM + BN) * 128 + (BM + wn * WN + l32) * 8;
   const int swz = (l32 >> 1) & 7;
-  auto step = [&](int t, auto count) __attribute__((always_inline)) {
-    constexpr int S = decltype(count)::value;  // instructions along K
-    const int st = (t & 1) * STAGE;
-    uint2 sa[MI], sb[NI];
+  struct Scales {
+    uint2 a[MI], b[NI];
+  } sc[2];
+  uint4 fa[2][MI], fb[2][NI];
+  auto read_scales = [&](Scales& q, int st) __attribute__((always_inline)) {
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) {
-      sa[mi] = *(const uint2*)(lsa + st + mi * 256);
-      sa[mi].x >>= 8 * h;
-      sa[mi].y >>= 8 * h;
-    }
+    for (int ni = 0; ni < NI; ++ni) q.b[ni] = *(const uint2*)(lsb + st + ni * 256);
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) {
-      sb[ni] = *(const uint2*)(lsb + st + ni * 256);
-      sb[ni].x >>= 8 * h;
-      sb[ni].y >>= 8 * h;
-    }
-    uint4 fa[2][MI], fb[2][NI];
-    auto read = [&](int s) __attribute__((always_inline)) {
-      const int c = st + ((2 * s + h) ^ swz) * 16;
-#pragma unroll
-      for (int ni = 0; ni < NI; ++ni) fb[s & 1][ni] = *(const uint4*)(lb + ni * 4096 + c);
-#pragma unroll
-      for (int mi = 0; mi < MI; ++mi) fa[s & 1][mi] = *(const uint4*)(la + mi * 4096 + c);
-    };
-    read(0);
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      if (s + 1 < S) read(s + 1);
-#pragma unroll
-      for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni) {
-          const uint32_t wb = s < 2 ? sb[ni].x : sb[ni].y, wa = s < 2 ? sa[mi].x : sa[mi].y;
-          acc[mi][ni] = s & 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(fb[1][ni]), frag(fa[1][mi]), acc[mi][ni],
-                                                                              4, 4, 2, wb, 2, wa)
-                              : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(fb[0][ni]), frag(fa[0][mi]), acc[mi][ni],
-                                                                              4, 4, 0, wb, 0, wa);
-        }
-    }
+    for (int mi = 0; mi < MI; ++mi) q.a[mi] = *(const uint2*)(lsa + st + mi * 256);
   };
+  auto shift_scales = [&](Scales& q) __attribute__((always_inline)) {
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) q.b[ni] = make_uint2(q.b[ni].x >> (8 * h), q.b[ni].y >> (8 * h));
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) q.a[mi] = make_uint2(q.a[mi].x >> (8 * h), q.a[mi].y >> (8 * h));
+  };
+  // fragments of instruction s of the stage at st, into set s % 2
+  auto read = [&](int s, int st) __attribute__((always_inline)) {
+    const int c = st + ((2 * s + h) ^ swz) * 16;
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) fb[s & 1][ni] = *(const uint4*)(lb + ni * 4096 + c);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) fa[s & 1][mi] = *(const uint4*)(la + mi * 4096 + c);
+  };
+  // the scheduling fences keep the reads of the next fragments ahead of the
+  // products of the present ones
+  auto multiply = [&](auto sv, const Scales& q) __attribute__((always_inline)) {
+    constexpr int s = decltype(sv)::value;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni)
+        acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+            frag(fb[s & 1][ni]), frag(fa[s & 1][mi]), acc[mi][ni], 4, 4, 2 * (s & 1), s < 2 ? q.b[ni].x : q.b[ni].y,
+            2 * (s & 1), s < 2 ? q.a[mi].x : q.a[mi].y);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  using std::integral_constant;
   issue(0);
   drain_and_meet();
+  if (steps > 1) issue(1);
+  read_scales(sc[0], 0);
+  read(0, 0);
+  shift_scales(sc[0]);
   const int full = a.Kp / 256;
   for (int t = 0; t < full; ++t) {
-    if (t + 1 < steps) issue(t + 1);
-    step(t, std::integral_constant<int, 4>{});
+    const int st = (t & 1) * STAGE, nx = STAGE - st;
+    read(1, st);
+    multiply(integral_constant<int, 0>{}, sc[0]);
+    read(2, st);
+    multiply(integral_constant<int, 1>{}, sc[0]);
+    read(3, st);
+    multiply(integral_constant<int, 2>{}, sc[0]);
+    // this stage has been read and the next one has landed: it is refilled, and
+    // the next one's first fragments are read, under the last products
+    // (after the last step these reads find old values, which nothing uses)
     drain_and_meet();
+    if (t + 2 < steps) issue(t + 2);
+    read_scales(sc[1], nx);
+    read(0, nx);
+    multiply(integral_constant<int, 3>{}, sc[0]);
+    sc[0] = sc[1];
+    shift_scales(sc[0]);
   }
   if (odd) {
-    step(full, std::integral_constant<int, 2>{});
-    drain_and_meet();
+    read(1, (full & 1) * STAGE);
+    multiply(integral_constant<int, 0>{}, sc[0]);
+    multiply(integral_constant<int, 1>{}, sc[0]);
   }
+  drain_and_meet();
 
   // epilogue: 32 rows at a time through this wavefront's own LDS (the empty asm
   // keeps its addresses from being formed before the loop, where they would not
