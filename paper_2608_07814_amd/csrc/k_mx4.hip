@@ -185,11 +185,10 @@ __device__ __forceinline__ void load_lds(const void* base, uint32_t off, const v
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory");
 }
 
-// All but this wavefront's newest N loads have landed and its LDS reads are
-// done, then every wavefront's.
-template <int N>
+// All of this wavefront's loads have landed and its LDS reads are done, then
+// every wavefront's.
 __device__ __forceinline__ void land_and_meet() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -214,24 +213,23 @@ __device__ __forceinline__ int count_tiles(const Mx4GemmArgs& a) {
 }
 
 // BM x BN outputs per workgroup, a 2 x 2 grid of wavefronts, 32x32x64
-// instructions. Both operands go memory -> LDS directly in steps of 128 values
-// (64 bytes a row) through a ring of four, so that three steps stream in while
-// one is multiplied: with two steps of 256 values, one of them in flight, the
-// same tiles waited for memory (8192^3: TIME2 us against TIME4). Inside a step's
-// image the four 16-byte chunks of a row are XORed with (row / 4) % 4, so the
-// 16 lanes that a read serves together hit 16 different bank groups; a lane
-// fetches the chunk that belongs at its LDS place. Scales come in groups of
-// four steps (16 bytes a row) through a ring of two. The weights are the
-// instruction's first operand: a lane ends with 4 consecutive columns of one
-// row, which go through LDS into whole rows.
+// instructions. Both operands go memory -> LDS directly in steps of 256 values
+// (128 bytes a row, a whole cache line: 64 bytes a row took twice as long per
+// byte), two steps in a ring, one streaming in while the other is multiplied.
+// Inside a step's image the eight 16-byte chunks of a row are XORed with (row /
+// 2) % 8, so the 16 lanes that a read serves together hit 16 different bank
+// groups; a lane fetches the chunk that belongs at its LDS place. Scales come
+// in groups of two steps (16 bytes a row) through a ring of two. The weights
+// are the instruction's first operand: a lane ends with 4 consecutive columns
+// of one row, which go through LDS into whole rows.
 template <int BM, int BN>
 __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_mx4_gemm_tile(const Mx4GemmArgs a) {
   constexpr int WM = BM / 2, WN = BN / 2, MI = WM / 32, NI = WN / 32;
-  constexpr int RA = BM / 64, RB = BN / 64;  // 16-byte loads of a thread per step
-  constexpr int STAGE = (BM + BN) * 64, SGRP = (BM + BN) * 16;
-  constexpr int EROW = WN + 4;               // floats of an epilogue row
-  static_assert(4 * STAGE >= 4 * 32 * EROW * 4, "the epilogue reuses the ring");
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * STAGE + 2 * SGRP];
+  constexpr int RA = BM / 32, RB = BN / 32, R = RA + RB;  // 16-byte loads of a thread per step
+  constexpr int STAGE = (BM + BN) * 128, SGRP = (BM + BN) * 16;
+  constexpr int EROW = WN + 4;                            // floats of an epilogue row
+  static_assert(2 * STAGE >= 4 * 32 * EROW * 4, "the epilogue reuses the ring");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE + 2 * SGRP];
 
   // work item: XCD x (workgroups go round the 8 XCDs) takes a contiguous range;
   // column tiles in bands of 8, so that what an XCD runs together shares rows
@@ -257,7 +255,8 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_mx4_gemm_t
   int lane = tid & 63;
   const int l32 = lane & 31, h = lane >> 5;
   const int wm = wave >> 1, wn = wave & 1;
-  const int cp = a.Kp / 2, sp = a.Kp / 32, steps = a.Kp / 128;
+  const int cp = a.Kp / 2, sp = a.Kp / 32, full = a.Kp / 256;
+  const bool odd = a.Kp & 128;  // a last step of 128 values
 
   // a row that is not there (past the tile, or a map entry out of range) reads
   // A's first row (the host sees to it that there is one); its results are
@@ -275,29 +274,29 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_mx4_gemm_t
   const uint8_t* const Bs = a.bs + ((int64_t)g * a.N + n0) * sp;
 #pragma unroll
   for (int j = 0; j < RA; ++j) {
-    const int r = (j * 256 + tid) >> 2;
-    oa[j] = (uint32_t)max(row_of(r), 0) * (uint32_t)cp + ((tid ^ (r >> 2)) & 3) * 16;
+    const int r = (j * 256 + tid) >> 3;
+    oa[j] = (uint32_t)max(row_of(r), 0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
   }
 #pragma unroll
   for (int j = 0; j < RB; ++j) {
-    const int r = (j * 256 + tid) >> 2;
-    ob[j] = (uint32_t)min(r, a.N - 1 - n0) * (uint32_t)cp + ((tid ^ (r >> 2)) & 3) * 16;
+    const int r = (j * 256 + tid) >> 3;
+    ob[j] = (uint32_t)min(r, a.N - 1 - n0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
   }
   // a thread's rows of the scale groups: one row of A (threads below BM), one
   // of B (threads below BN)
   static_assert(BM <= 256 && BN <= 256, "one row of each operand per thread");
   const uint32_t qa = (uint32_t)max(row_of(tid % BM), 0) * (uint32_t)sp;
   const uint32_t qb = (uint32_t)min(tid % BN, a.N - 1 - n0) * (uint32_t)sp;
-  // group q of the scales (words 4 q .. 4 q + 3 of every row), 16 bytes a row
+  // group q of the scales: words 4 q .. 4 q + 3 of every row, 16 bytes a row
   auto issue_scales = [&](int q) {
-    uint8_t* const st = smem + 4 * STAGE + (q & 1) * SGRP;
+    uint8_t* const st = smem + 2 * STAGE + (q & 1) * SGRP;
     if (a.wide_scales) {
       if (wave < BM / 64) load_lds<16>(a.as + q * 16, qa, st + wave * 1024);
       if (wave < BN / 64) load_lds<16>(Bs + q * 16, qb, st + BM * 16 + wave * 1024);
     } else {
       // rows that are no multiple of 16 bytes: word by word, 16 rows x 4 words
       // per load; words past the row's end repeat its last one
-      const int word = min(q * 4 + (lane & 3), steps - 1) * 4;
+      const int word = min(q * 4 + (lane & 3), sp / 4 - 1) * 4;
 #pragma unroll 1
       for (int r0 = wave * 16; r0 < BM + BN; r0 += 64) {
         const int r = r0 + (lane >> 2);
@@ -308,15 +307,22 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_mx4_gemm_t
       }
     }
   };
-  // load i of step t's operands into stage t % 4
-  constexpr int R = RA + RB;
-  auto issue_one = [&](int t, int i) __attribute__((always_inline)) {
-    uint8_t* const st = smem + (t & 3) * STAGE;
-    const int64_t at = (int64_t)t * 64;
+  // load i of step t's operands into stage t % 2; in a half step the upper
+  // chunks repeat the lower ones (they are not multiplied)
+  auto issue_one = [&](int t, int i, bool half) __attribute__((always_inline)) {
+    uint8_t* const st = smem + (t & 1) * STAGE;
+    const int64_t at = (int64_t)t * 128;
+    const int j = i < RA ? i : i - RA;
+    const uint32_t back = half ? ((tid ^ (((j * 256 + tid) >> 3) >> 1)) & 4) * 16 : 0;
     if (i < RA)
-      load_lds<16>(a.a + at, oa[i], st + (i * 4 + wave) * 1024);
+      load_lds<16>(a.a + at, oa[j] - back, st + (j * 4 + wave) * 1024);
     else
-      load_lds<16>(B + at, ob[i - RA], st + BM * 64 + ((i - RA) * 4 + wave) * 1024);
+      load_lds<16>(B + at, ob[j] - back, st + BM * 128 + (j * 4 + wave) * 1024);
+  };
+  auto issue = [&](int t, bool half) {
+    if ((t & 1) == 0) issue_scales(t >> 1);
+#pragma unroll
+    for (int i = 0; i < R; ++i) issue_one(t, i, half);
   };
 
   f32x16 acc[MI][NI];
@@ -325,101 +331,116 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_mx4_gemm_t
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
 
-  // a row's scale word of a step: a lane's block of instruction s is 2 s + h, so
-  // after a shift by h bytes its scale is byte 2 s
-  const uint8_t* const la = smem + (wm * WM + l32) * 64;
-  const uint8_t* const lb = smem + (BM + wn * WN + l32) * 64;
-  const uint8_t* const lsa = smem + 4 * STAGE + (wm * WM + l32) * 16;
-  const uint8_t* const lsb = smem + 4 * STAGE + (BM + wn * WN + l32) * 16;
-  const int swz = (l32 >> 2) & 3;
+  // a row's scales of a step are two words: a lane's block of instruction s is
+  // 2 s + h, so after a shift by h bytes its scale is byte 0 or 2 of word s / 2
+  const uint8_t* const la = smem + (wm * WM + l32) * 128;
+  const uint8_t* const lb = smem + (BM + wn * WN + l32) * 128;
+  const uint8_t* const lsa = smem + 2 * STAGE + (wm * WM + l32) * 16;
+  const uint8_t* const lsb = smem + 2 * STAGE + (BM + wn * WN + l32) * 16;
+  const int swz = (l32 >> 1) & 7;
   struct Scales {
-    uint32_t a[MI], b[NI];
+    uint2 a[MI], b[NI];
   } sc, nx;
   uint4 fa[2][MI], fb[2][NI];
   auto read_scales = [&](Scales& q, int t) __attribute__((always_inline)) {
-    const int st = ((t >> 2) & 1) * SGRP + (t & 3) * 4;
+    const int st = ((t >> 1) & 1) * SGRP + (t & 1) * 8;
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) q.b[ni] = *(const uint32_t*)(lsb + st + ni * 512);
+    for (int ni = 0; ni < NI; ++ni) q.b[ni] = *(const uint2*)(lsb + st + ni * 512);
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) q.a[mi] = *(const uint32_t*)(lsa + st + mi * 512);
+    for (int mi = 0; mi < MI; ++mi) q.a[mi] = *(const uint2*)(lsa + st + mi * 512);
   };
   auto shift_scales = [&](Scales& q) __attribute__((always_inline)) {
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) q.b[ni] >>= 8 * h;
+    for (int ni = 0; ni < NI; ++ni) q.b[ni] = make_uint2(q.b[ni].x >> (8 * h), q.b[ni].y >> (8 * h));
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) q.a[mi] >>= 8 * h;
+    for (int mi = 0; mi < MI; ++mi) q.a[mi] = make_uint2(q.a[mi].x >> (8 * h), q.a[mi].y >> (8 * h));
   };
-  // fragments of instruction s of step t, into set s
+  // fragments of instruction s of step t, into set s % 2
   auto read = [&](int s, int t) __attribute__((always_inline)) {
-    const int c = (t & 3) * STAGE + ((2 * s + h) ^ swz) * 16;
+    const int c = (t & 1) * STAGE + ((2 * s + h) ^ swz) * 16;
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) fb[s][ni] = *(const uint4*)(lb + ni * 2048 + c);
+    for (int ni = 0; ni < NI; ++ni) fb[s & 1][ni] = *(const uint4*)(lb + ni * 4096 + c);
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) fa[s][mi] = *(const uint4*)(la + mi * 2048 + c);
+    for (int mi = 0; mi < MI; ++mi) fa[s & 1][mi] = *(const uint4*)(la + mi * 4096 + c);
   };
-  // The products of instruction s; with LOADS, the loads of step t between
-  // them: issued in one go they held up the products behind them. The
+  // The products of instruction s; from FIRST on, half of the loads of step t
+  // between them: issued in one go they held up the products behind them. The
   // scheduling fences keep this order, and the reads of the next fragments
   // ahead of the products of the present ones.
-  auto multiply = [&](auto sv, auto loads, int t) __attribute__((always_inline)) {
-    constexpr int s = decltype(sv)::value;
-    constexpr int PER = MI * NI / R;
-    static_assert(MI * NI % R == 0, "as many products between any two loads");
+  constexpr int kNone = R;
+  auto multiply = [&](auto sv, auto first, int t) __attribute__((always_inline)) {
+    constexpr int s = decltype(sv)::value, FIRST = decltype(first)::value;
+    constexpr int PER = MI * NI / (R / 2);
+    static_assert(PER >= 1 && MI * NI % (R / 2) == 0, "as many products between any two loads");
 #pragma unroll
     for (int i = 0; i < MI * NI; ++i) {
       const int mi = i / NI, ni = i % NI;
       if (i % PER == 0) __builtin_amdgcn_sched_barrier(0);
-      if constexpr (decltype(loads)::value)
-        if (i % PER == 0) issue_one(t, i / PER);
-      acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(fb[s][ni]), frag(fa[s][mi]), acc[mi][ni], 4, 4,
-                                                                    2 * s, sc.b[ni], 2 * s, sc.a[mi]);
+      if constexpr (FIRST < R)
+        if (i % PER == 0) issue_one(t, FIRST + i / PER, false);
+      acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+          frag(fb[s & 1][ni]), frag(fa[s & 1][mi]), acc[mi][ni], 4, 4, 2 * (s & 1), s < 2 ? sc.b[ni].x : sc.b[ni].y,
+          2 * (s & 1), s < 2 ? sc.a[mi].x : sc.a[mi].y);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
   using std::integral_constant;
-  using std::false_type;
-  using std::true_type;
-#pragma unroll 1
-  for (int t = 0; t < min(steps, 4); ++t) {
-    if (t == 0) issue_scales(0);
-#pragma unroll
-    for (int i = 0; i < R; ++i) issue_one(t, i);
-  }
-  if (steps >= 4)
-    land_and_meet<3 * R>();
-  else
-    land_and_meet<0>();
-  read_scales(sc, 0);
-  read(0, 0);
-  shift_scales(sc);
-  // Step t. When its fragments have been read and step t + 1 has landed (the two
-  // after it may be under way; loads land in order), its place is refilled with
-  // step t + 4 and the next step's first fragments are read, under its last
-  // products (after the last step those reads find old values, which nothing
-  // uses).
-  int t = 0;
-  for (; t + 4 < steps; ++t) {
-    read(1, t);
-    multiply(integral_constant<int, 0>{}, false_type{}, 0);
-    land_and_meet<2 * R>();
-    if ((t & 3) == 0) issue_scales((t >> 2) + 1);
-    read_scales(nx, t + 1);
-    read(0, t + 1);
-    multiply(integral_constant<int, 1>{}, true_type{}, t + 4);
+  constexpr integral_constant<int, 0> i0{};
+  constexpr integral_constant<int, 1> i1{};
+  constexpr integral_constant<int, 2> i2{};
+  constexpr integral_constant<int, 3> i3{};
+  constexpr integral_constant<int, kNone> none{};
+
+  // Step t > 0, entered when it has landed and step t - 1 has been read but for
+  // its last products, which come first: under them and the next ones, step t + 1
+  // is loaded into the place of step t - 1 (LOADS).
+  auto step = [&](int t, auto loads) __attribute__((always_inline)) {
+    constexpr bool LOADS = decltype(loads)::value;
+    if (LOADS && (t & 1)) issue_scales((t + 1) >> 1);
+    read_scales(nx, t);
+    read(0, t);
+    multiply(i3, integral_constant<int, LOADS ? 0 : kNone>{}, t + 1);
     sc = nx;
     shift_scales(sc);
-  }
-  for (; t < steps; ++t) {
     read(1, t);
-    multiply(integral_constant<int, 0>{}, false_type{}, 0);
-    land_and_meet<0>();
-    read_scales(nx, t + 1);
-    read(0, t + 1);
-    multiply(integral_constant<int, 1>{}, false_type{}, 0);
-    sc = nx;
+    multiply(i0, integral_constant<int, LOADS ? R / 2 : kNone>{}, t + 1);
+    read(2, t);
+    multiply(i1, none, 0);
+    read(3, t);
+    multiply(i2, none, 0);
+    land_and_meet();
+  };
+  issue(0, full == 0);
+  land_and_meet();
+  if (full > 0) {
+    if (full > 1 || odd) issue(1, full == 1);
+    read_scales(sc, 0);
+    read(0, 0);
     shift_scales(sc);
+    read(1, 0);
+    multiply(i0, none, 0);
+    read(2, 0);
+    multiply(i1, none, 0);
+    read(3, 0);
+    multiply(i2, none, 0);
+    land_and_meet();
+    int t = 1;
+    for (; t + 1 < full; ++t) step(t, std::true_type{});
+    if (t < full) {
+      if (odd) issue(full, true);
+      step(t, std::false_type{});
+    }
+    multiply(i3, none, 0);
   }
-  land_and_meet<0>();
+  if (odd) {
+    read_scales(sc, full);
+    read(0, full);
+    shift_scales(sc);
+    read(1, full);
+    multiply(i0, none, 0);
+    multiply(i1, none, 0);
+  }
+  land_and_meet();
 
   // epilogue: 32 rows at a time through this wavefront's own LDS (the empty asm
   // keeps its addresses from being formed before the loop, where they would not
