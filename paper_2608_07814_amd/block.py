@@ -22,7 +22,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import lorex as lx
-from .lorex import LX_BF16, LX_F32, LX_ERR_UNSUPPORTED, LorexError, _check
+from .lorex import LX_BF16, LX_F32, _check
 
 MX4_NONE, MX4_SWIGLU = 0, 1
 NORM_MAX_D = 32768
@@ -82,66 +82,66 @@ def _dtype(name: str, t: torch.Tensor) -> int:
     return dt
 
 
-def _arg(name: str, t: Optional[torch.Tensor], shape: tuple, dtype, device) -> Optional[int]:
+def _gpu(name: str, t: torch.Tensor) -> int:
+    """The index of the GPU that a call's first tensor is on."""
+    i = t.get_device()
+    if i < 0:
+        raise ValueError(f"{name} must be on a GPU")
+    return i
+
+
+def _arg(name: str, t: Optional[torch.Tensor], shape: tuple, dtype, gpu: int) -> Optional[int]:
     """Address of an argument after its checks (None stays None)."""
     if t is None:
         return None
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.get_device() != gpu:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{gpu}")
     return t.data_ptr() or _EMPTY
 
 
-def _need_gpu(name: str, t: torch.Tensor):
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be on a GPU")
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr() or _EMPTY
 
 
-class _On:
-    """The stream of a call and the tensors the call allocates: those stay
-    reserved until that stream is done with them."""
+# (torch.cuda.current_stream builds an object, 1.7 us of a call of 6)
+_current_raw_stream = torch._C._cuda_getCurrentRawStream
 
-    def __init__(self, stream, device):
-        cur = torch.cuda.current_stream(device)
-        self.other = stream if stream is not None and stream != cur else None
-        self.handle = (cur if stream is None else stream).cuda_stream
-        self.device = device
 
-    def empty(self, shape, dtype):
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if self.other is not None:
-            t.record_stream(self.other)
-        return t
+def _handle(stream, gpu: int) -> int:
+    return _current_raw_stream(gpu) if stream is None else stream.cuda_stream
 
-    def workspace(self, given: Optional[torch.Tensor], need: int):
-        """(address, bytes) of a workspace; the tensor is kept by the caller's frame."""
-        if given is None and need:
-            given = self.empty(need, torch.uint8)
-        return given
+
+def _empty(shape, dtype, like: torch.Tensor, stream) -> torch.Tensor:
+    """A new tensor that stays reserved until the call's stream is done with it."""
+    t = like.new_empty(shape, dtype=dtype)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _workspace(given: Optional[torch.Tensor], need: int, like: torch.Tensor, stream):
+    """(tensor to keep during the call, address, bytes)"""
+    if given is None:
+        if not need:
+            return None, None, 0
+        given = _empty((need,), torch.uint8, like, stream)
+    return given, given.data_ptr(), given.numel()
 
 
 # ------------------------------------------------------------ block norms
-def _norm_layer(h, y, x_dtype, w_pre, w_post, scale, gate, residual_scale, eps, T, d, dev) -> LxNormLayer:
-    ws = [w for w in (w_pre, w_post, scale) if w is not None]
-    if any(w.dtype != ws[0].dtype for w in ws):
-        raise ValueError("w_pre, w_post and scale must have one dtype")
-    s = LxNormLayer()
-    s.d = d
-    s.h_dtype = _dtype("h", h)
-    s.y_dtype = s.h_dtype if y is None else _dtype("y", y)
-    s.x_dtype = x_dtype
-    s.w_dtype = _dtype("weights", ws[0]) if ws else LX_F32
-    s.residual_scale, s.eps = residual_scale, eps
-    s.w_pre = _arg("w_pre", w_pre, (d,), None, dev)
-    s.w_post = _arg("w_post", w_post, (d,), None, dev)
-    s.scale = _arg("scale", scale, (d,), None, dev)
-    s.gate = _arg("gate", gate, (T,), torch.float32, dev)
-    return s
+def _norm_layer(h, y, x_dtype, w_pre, w_post, scale, gate, residual_scale, eps, T, d, gpu) -> LxNormLayer:
+    w = w_pre if w_pre is not None else w_post if w_post is not None else scale
+    wt = None if w is None else w.dtype
+    return LxNormLayer(d, _dtype("h", h), LX_F32 if y is None else _dtype("y", y), x_dtype,
+                       LX_F32 if w is None else _dtype("weights", w), residual_scale, eps,
+                       _arg("w_pre", w_pre, (d,), wt, gpu), _arg("w_post", w_post, (d,), wt, gpu),
+                       _arg("scale", scale, (d,), wt, gpu), _arg("gate", gate, (T,), torch.float32, gpu))
 
 
 def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Optional[torch.Tensor] = None,
@@ -158,36 +158,37 @@ def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Opti
     given; h_out may be h."""
     if h.dim() != 2:
         raise ValueError("h must be [T][d]")
-    _need_gpu("h", h)
-    T, d = h.shape
-    dev = h.device
-    on = _On(stream, dev)
+    gpu = _gpu("h", h)
+    T, d = shape = h.shape
     k = y_rows = 0
+    yp = None
     if y is not None:
         y_rows = y.shape[0]
         if slot_row is None:
-            yp = _arg("y", y, (T, d), None, dev)
+            yp = _arg("y", y, shape, None, gpu)
         else:
             if slot_row.dim() != 2:
                 raise ValueError("slot_row must be [T][k]")
             k = slot_row.shape[1]
-            yp = _arg("y", y, (y_rows, d), None, dev)
+            yp = _arg("y", y, (y_rows, d), None, gpu)
         if h_out is None:
-            h_out = on.empty((T, d), h.dtype)
+            h_out = _empty(shape, h.dtype, h, stream)
     else:
-        yp = None
         if h_out is not None or slot_row is not None or slot_weights is not None or any(v is not None for v in (w_post, scale, gate)):
             raise ValueError("h_out, slots, w_post, scale and gate go with y")
     if w_pre is None:
         if x is not None:
             raise ValueError("x goes with w_pre")
     elif x is None:
-        x = on.empty((T, d), x_dtype)
-    s = _norm_layer(h, y, LX_BF16 if x is None else _dtype("x", x), w_pre, w_post, scale, gate, residual_scale, eps, T, d, dev)
-    _check(lib().lx_block_norm(ctypes.byref(s), T, _arg("h", h, (T, d), None, dev), yp, y_rows, k,
-                               _arg("slot_row", slot_row, (T, k), torch.int32, dev),
-                               _arg("slot_weights", slot_weights, (T, k), torch.float32, dev),
-                               _arg("h_out", h_out, (T, d), h.dtype, dev), _arg("x", x, (T, d), None, dev), on.handle))
+        x = _empty(shape, x_dtype, h, stream)
+    s = _norm_layer(h, y, LX_BF16 if x is None else _dtype("x", x), w_pre, w_post, scale, gate, residual_scale, eps, T, d, gpu)
+    st = lib().lx_block_norm(ctypes.byref(s), T, _arg("h", h, shape, None, gpu), yp, y_rows, k,
+                             _arg("slot_row", slot_row, (T, k), torch.int32, gpu),
+                             _arg("slot_weights", slot_weights, (T, k), torch.float32, gpu),
+                             _arg("h_out", h_out, shape, h.dtype, gpu), _arg("x", x, shape, None, gpu),
+                             _handle(stream, gpu))
+    if st:
+        _check(st)
     return (h if y is None else h_out), x
 
 
@@ -212,31 +213,29 @@ def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Opti
     are fp32."""
     if h_out.dim() != 2:
         raise ValueError("h_out must be [T][d]")
-    _need_gpu("h_out", h_out)
-    T, d = h_out.shape
-    dev = h_out.device
-    on = _On(stream, dev)
+    gpu = _gpu("h_out", h_out)
+    T, d = shape = h_out.shape
     if (dx is None) != (w_pre is None):
         raise ValueError("dx goes with w_pre")
     if y is None and (dy is not None or any(v is not None for v in (w_post, scale, gate))):
         raise ValueError("dy, w_post, scale and gate go with y")
     s = _norm_layer(h_out, y, LX_BF16 if dx is None else _dtype("dx", dx), w_pre, w_post, scale, gate, residual_scale,
-                    eps, T, d, dev)
+                    eps, T, d, gpu)
     if dh is None:
-        dh = on.empty((T, d), h_out.dtype)
+        dh = _empty(shape, h_out.dtype, h_out, stream)
     if dy is None and y is not None:
-        dy = on.empty((T, d), y.dtype)
-    grad = lambda v, n: None if v is None else on.empty((n,), torch.float32)  # noqa: E731
+        dy = _empty(shape, y.dtype, h_out, stream)
+    grad = lambda v, n: None if v is None else _empty((n,), torch.float32, h_out, stream)  # noqa: E731
     dgate, dw_pre, dw_post, dscale = grad(gate, T), grad(w_pre, d), grad(w_post, d), grad(scale, d)
     L = lib()
-    workspace = on.workspace(workspace, L.lx_block_norm_backward_workspace_bytes(T, d))
-    p = lambda v: None if v is None else v.data_ptr() or _EMPTY  # noqa: E731
-    _check(L.lx_block_norm_backward(
-        ctypes.byref(s), T, _arg("h_out", h_out, (T, d), None, dev), _arg("y", y, (T, d), None, dev),
-        _arg("dx", dx, (T, d), None, dev), _arg("dh_out", dh_out, (T, d), h_out.dtype, dev),
-        _arg("dh", dh, (T, d), h_out.dtype, dev), _arg("dy", dy, (T, d), None if y is None else y.dtype, dev),
-        p(dgate), p(dw_pre), p(dw_post), p(dscale), p(workspace), 0 if workspace is None else workspace.numel(),
-        on.handle))
+    keep, ws, n = _workspace(workspace, L.lx_block_norm_backward_workspace_bytes(T, d), h_out, stream)
+    st = L.lx_block_norm_backward(
+        ctypes.byref(s), T, _arg("h_out", h_out, shape, None, gpu), _arg("y", y, shape, None, gpu),
+        _arg("dx", dx, shape, None, gpu), _arg("dh_out", dh_out, shape, h_out.dtype, gpu),
+        _arg("dh", dh, shape, h_out.dtype, gpu), _arg("dy", dy, shape, None if y is None else y.dtype, gpu),
+        _ptr(dgate), _ptr(dw_pre), _ptr(dw_post), _ptr(dscale), ws, n, _handle(stream, gpu))
+    if st:
+        _check(st)
     return BlockNormGrads(dh, dy, dgate, dw_pre, dw_post, dscale)
 
 
@@ -248,10 +247,10 @@ class BalanceLoss(NamedTuple):
     n_tokens: torch.Tensor  # [1] int32: unmasked tokens
 
 
-def _mask_arg(mask, T, dev):
+def _mask_arg(mask, T, gpu):
     if mask is not None and mask.dtype == torch.bool:
         mask = mask.view(torch.uint8)
-    return _arg("mask", mask, (T,), torch.uint8, dev)
+    return _arg("mask", mask, (T,), torch.uint8, gpu)
 
 
 def balance_loss(logits: torch.Tensor, topk_ids: torch.Tensor, *, mask: Optional[torch.Tensor] = None,
@@ -261,20 +260,19 @@ def balance_loss(logits: torch.Tensor, topk_ids: torch.Tensor, *, mask: Optional
     or bool [T], None: all) is set."""
     if logits.dim() != 2 or topk_ids.dim() != 2:
         raise ValueError("logits must be [T][E] and topk_ids [T][k]")
-    _need_gpu("logits", logits)
+    gpu = _gpu("logits", logits)
     T, E = logits.shape
     k = topk_ids.shape[1]
-    dev = logits.device
-    on = _On(stream, dev)
-    r = BalanceLoss(on.empty((1,), torch.float32), on.empty((E,), torch.int32), on.empty((E,), torch.float32),
-                    on.empty((1,), torch.int32))
+    r = BalanceLoss(_empty((1,), torch.float32, logits, stream), _empty((E,), torch.int32, logits, stream),
+                    _empty((E,), torch.float32, logits, stream), _empty((1,), torch.int32, logits, stream))
     L = lib()
-    workspace = on.workspace(workspace, L.lx_balance_loss_workspace_bytes(T, E))
-    _check(L.lx_balance_loss(_arg("logits", logits, (T, E), None, dev), _dtype("logits", logits), T, E,
-                             _arg("topk_ids", topk_ids, (T, k), torch.int32, dev), k, _mask_arg(mask, T, dev), coef,
-                             r.loss.data_ptr(), r.counts.data_ptr(), r.prob.data_ptr(), r.n_tokens.data_ptr(),
-                             None if workspace is None else workspace.data_ptr(),
-                             0 if workspace is None else workspace.numel(), on.handle))
+    keep, ws, n = _workspace(workspace, L.lx_balance_loss_workspace_bytes(T, E), logits, stream)
+    st = L.lx_balance_loss(_arg("logits", logits, (T, E), None, gpu), _dtype("logits", logits), T, E,
+                           _arg("topk_ids", topk_ids, (T, k), torch.int32, gpu), k, _mask_arg(mask, T, gpu), coef,
+                           r.loss.data_ptr(), r.counts.data_ptr(), r.prob.data_ptr(), r.n_tokens.data_ptr(), ws, n,
+                           _handle(stream, gpu))
+    if st:
+        _check(st)
     return r
 
 
@@ -287,18 +285,19 @@ def balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_tokens: 
     or ranks; dloss: fp32 scalar tensor (None: 1)."""
     if logits.dim() != 2:
         raise ValueError("logits must be [T][E]")
-    _need_gpu("logits", logits)
-    T, E = logits.shape
-    dev = logits.device
-    on = _On(stream, dev)
+    gpu = _gpu("logits", logits)
+    T, E = shape = logits.shape
     if dlogits is None:
-        dlogits = on.empty((T, E), logits.dtype)
-    if dloss is not None:
+        dlogits = _empty(shape, logits.dtype, logits, stream)
+    if dloss is not None and dloss.dim() != 1:
         dloss = dloss.view(1)
-    _check(lib().lx_balance_loss_backward(
-        _arg("logits", logits, (T, E), None, dev), _dtype("logits", logits), T, E, k, _mask_arg(mask, T, dev),
-        _arg("counts", counts, (E,), torch.int32, dev), _arg("n_tokens", n_tokens, (1,), torch.int32, dev), coef,
-        _arg("dloss", dloss, (1,), torch.float32, dev), _arg("dlogits", dlogits, (T, E), logits.dtype, dev), on.handle))
+    st = lib().lx_balance_loss_backward(
+        _arg("logits", logits, shape, None, gpu), _dtype("logits", logits), T, E, k, _mask_arg(mask, T, gpu),
+        _arg("counts", counts, (E,), torch.int32, gpu), _arg("n_tokens", n_tokens, (1,), torch.int32, gpu), coef,
+        _arg("dloss", dloss, (1,), torch.float32, gpu), _arg("dlogits", dlogits, shape, logits.dtype, gpu),
+        _handle(stream, gpu))
+    if st:
+        _check(st)
     return dlogits
 
 
@@ -320,44 +319,42 @@ def mx4_quantize(x: torch.Tensor, *, act: int = MX4_NONE, out: Optional[Mx4] = N
     """x [..., K] fp32 or bf16 -> 4-bit values (lx_mx4_quantize). With
     ``act=MX4_SWIGLU`` x is [..., 2K], the gate and up projections of a SwiGLU
     expert, and silu(gate) * up is rounded."""
-    _need_gpu("x", x)
+    gpu = _gpu("x", x)
     if x.dim() < 1 or not x.is_contiguous():
         raise ValueError("x must be contiguous with at least one dimension")
-    lead, K = tuple(x.shape[:-1]), x.shape[-1]
+    lead, K = x.shape[:-1], x.shape[-1]
     if act == MX4_SWIGLU:
         if K % 2:
             raise ValueError("rows of gate and up projections have an even length")
         K //= 2
-    rows = 1
-    for v in lead:
-        rows *= v
+    rows = lead.numel()
     Kp = mx4_padded(K)
-    on = _On(stream, x.device)
+    cs, ss = (*lead, Kp // 2), (*lead, Kp // 32)
     if out is None:
-        out = Mx4(on.empty(lead + (Kp // 2,), torch.uint8), on.empty(lead + (Kp // 32,), torch.uint8), K)
+        out = Mx4(_empty(cs, torch.uint8, x, stream), _empty(ss, torch.uint8, x, stream), K)
     elif out.K != K:
         raise ValueError("out.K does not fit x")
-    _check(lib().lx_mx4_quantize(x.data_ptr(), _dtype("x", x), rows, K, act,
-                                 _arg("codes", out.codes, lead + (Kp // 2,), torch.uint8, x.device),
-                                 _arg("scales", out.scales, lead + (Kp // 32,), torch.uint8, x.device), on.handle))
+    st = lib().lx_mx4_quantize(x.data_ptr(), _dtype("x", x), rows, K, act, _arg("codes", out.codes, cs, torch.uint8, gpu),
+                               _arg("scales", out.scales, ss, torch.uint8, gpu), _handle(stream, gpu))
+    if st:
+        _check(st)
     return out
 
 
 def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, *, out: Optional[torch.Tensor] = None,
                    stream=None) -> torch.Tensor:
     """The values [..., K] of 4-bit codes (lx_mx4_dequantize), exact in both types."""
-    _need_gpu("codes", q.codes)
-    lead, K, dev = tuple(q.codes.shape[:-1]), q.K, q.codes.device
+    gpu = _gpu("codes", q.codes)
+    lead, K = q.codes.shape[:-1], q.K
     Kp = mx4_padded(K)
-    rows = 1
-    for v in lead:
-        rows *= v
-    on = _On(stream, dev)
+    shape = (*lead, K)
     if out is None:
-        out = on.empty(lead + (K,), dtype)
-    _check(lib().lx_mx4_dequantize(_arg("codes", q.codes, lead + (Kp // 2,), torch.uint8, dev),
-                                   _arg("scales", q.scales, lead + (Kp // 32,), torch.uint8, dev), rows, K,
-                                   _arg("out", out, lead + (K,), None, dev), _dtype("out", out), on.handle))
+        out = _empty(shape, dtype, q.codes, stream)
+    st = lib().lx_mx4_dequantize(_arg("codes", q.codes, (*lead, Kp // 2), torch.uint8, gpu),
+                                 _arg("scales", q.scales, (*lead, Kp // 32), torch.uint8, gpu), lead.numel(), K,
+                                 _arg("out", out, shape, None, gpu), _dtype("out", out), _handle(stream, gpu))
+    if st:
+        _check(st)
     return out
 
 
@@ -368,29 +365,28 @@ def mx4_gemm(a: Mx4, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map:
     [rows][K]; b [G][N][K] (or [N][K]: one group); offsets int32 [G + 1] (None: one
     group of all rows); row_map int32 [M] (None: row m of a). Rows past
     offsets[G] are left as they are."""
-    _need_gpu("a", a.codes)
-    if a.codes.dim() != 2 or b.codes.dim() not in (2, 3):
+    gpu = _gpu("a", a.codes)
+    ac, bc, K = a.codes, b.codes, a.K
+    if ac.dim() != 2 or bc.dim() not in (2, 3):
         raise ValueError("a must be [rows][K] and b [G][N][K] or [N][K]")
-    if a.K != b.K:
-        raise ValueError(f"a has {a.K} values in a row and b {b.K}")
-    dev, K = a.codes.device, a.K
+    if K != b.K:
+        raise ValueError(f"a has {K} values in a row and b {b.K}")
     Kp = mx4_padded(K)
-    rows = a.codes.shape[0]
-    lead = tuple(b.codes.shape[:-1])
+    rows = ac.shape[0]
+    *lead, _ = bc.shape
     G, N = lead if len(lead) == 2 else (1, lead[0])
     M = rows if row_map is None else row_map.shape[0]
-    on = _On(stream, dev)
     if out is None:
-        out = on.empty((M, N), out_dtype)
+        out = _empty((M, N), out_dtype, ac, stream)
     L = lib()
-    workspace = on.workspace(workspace, L.lx_mx4_gemm_workspace_bytes(M, N, K, G))
-    _check(L.lx_mx4_gemm(_arg("a codes", a.codes, (rows, Kp // 2), torch.uint8, dev),
-                         _arg("a scales", a.scales, (rows, Kp // 32), torch.uint8, dev), rows,
-                         _arg("row_map", row_map, (M,), torch.int32, dev),
-                         _arg("b codes", b.codes, lead + (Kp // 2,), torch.uint8, dev),
-                         _arg("b scales", b.scales, lead + (Kp // 32,), torch.uint8, dev),
-                         _arg("offsets", offsets, (G + 1,), torch.int32, dev), G, M, N, K,
-                         _arg("out", out, (M, N), None, dev), _dtype("out", out),
-                         None if workspace is None else workspace.data_ptr(),
-                         0 if workspace is None else workspace.numel(), on.handle))
+    keep, ws, n = _workspace(workspace, L.lx_mx4_gemm_workspace_bytes(M, N, K, G), ac, stream)
+    st = L.lx_mx4_gemm(_arg("a codes", ac, (rows, Kp // 2), torch.uint8, gpu),
+                       _arg("a scales", a.scales, (rows, Kp // 32), torch.uint8, gpu), rows,
+                       _arg("row_map", row_map, (M,), torch.int32, gpu),
+                       _arg("b codes", bc, (*lead, Kp // 2), torch.uint8, gpu),
+                       _arg("b scales", b.scales, (*lead, Kp // 32), torch.uint8, gpu),
+                       _arg("offsets", offsets, (G + 1,), torch.int32, gpu), G, M, N, K,
+                       _arg("out", out, (M, N), None, gpu), _dtype("out", out), ws, n, _handle(stream, gpu))
+    if st:
+        _check(st)
     return out

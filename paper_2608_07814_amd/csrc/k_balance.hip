@@ -3,9 +3,10 @@
 // LPT lanes own one token's row of logits and keep it in registers, lane l
 // the columns VEC (l + LPT i) .. + VEC - 1 of chunk i, so each row is read once;
 // maximum and sums go over those lanes by DPP. In the forward a lane adds up
-// its columns' probabilities over its tokens; a workgroup joins its lane
-// groups' sums in LDS in a fixed order, and a second launch joins the
-// workgroups'.
+// its columns' probabilities over its tokens; the sums of a wavefront's lane
+// groups are joined over lanes, the wavefronts' in LDS, the workgroups' by a
+// second launch, each in a fixed order. Counts are integer LDS atomics: exact
+// in any order.
 #include "lx_block.h"
 #include "lx_vec.h"
 
@@ -14,7 +15,8 @@
 namespace lx {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;  // gradient
+constexpr int kFwd = 1024;     // forward: few workgroups, whose sums are joined by one
 
 template <int VEC>
 struct Cols {
@@ -83,40 +85,40 @@ __device__ __forceinline__ void row_softmax(const void* logits, bool f32, int64_
     for (int e = 0; e < VEC; ++e) p[i].v[e] *= inv;
 }
 
-// loss, prob and n_tokens from the sums of one expert per thread in turn
-__device__ __forceinline__ void finish(const BalanceArgs& a, const float* sum_p, const int32_t* counts, int n,
-                                       float* red) {
+// The outputs from every expert's sums, by a workgroup of kFwd threads:
+// thread e has expert e's.
+__device__ __forceinline__ void finish(const BalanceArgs& a, float sum_p, int32_t count, int n) {
+  __shared__ float red[kFwd / 64];
+  const int e = threadIdx.x;
   const float inv_n = n > 0 ? 1.f / (float)n : 0.f;
   float part = 0.f;
-  for (int e = threadIdx.x; e < a.E; e += blockDim.x) {
-    const float p = sum_p[e] * inv_n;
+  if (e < a.E) {
+    const float p = sum_p * inv_n;
     a.prob[e] = p;
-    a.counts[e] = counts[e];
-    part += (float)counts[e] * p;
+    a.counts[e] = count;
+    part = (float)count * p;
   }
   part = lane_sum<64>(part);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = part;
+  if ((e & 63) == 0) red[e >> 6] = part;
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (e == 0) {
     float s = 0.f;
-    for (int w = 0; w < (int)blockDim.x / 64; ++w) s += red[w];
+#pragma unroll
+    for (int w = 0; w < kFwd / 64; ++w) s += red[w];
     *a.loss = n > 0 ? a.coef * (float)a.E * (s * inv_n / (float)a.k) : 0.f;
     *a.n_tokens = n;
   }
 }
+static_assert(kFwd >= kBalanceMaxE, "one thread per expert");
 
 template <int VEC, int LPT, int NCH>
-__global__ __launch_bounds__(kThreads) void k_balance(const BalanceArgs a) {
-  constexpr int TPB = kThreads / LPT;
-  __shared__ float sp[kBalanceMaxE];
-  __shared__ int32_t sc[kBalanceMaxE];
+__global__ __launch_bounds__(kFwd) void k_balance(const BalanceArgs a) {
+  constexpr int TPB = kFwd / LPT, NW = kFwd / 64, COLS = VEC * LPT * NCH;
+  __shared__ float sp[NW][COLS];
+  __shared__ int32_t sc[COLS];
   __shared__ int32_t sn;
-  __shared__ float red[kThreads / 64];
-  const int l = threadIdx.x % LPT, g = threadIdx.x / LPT;
-  for (int e = threadIdx.x; e < a.E; e += kThreads) {
-    sp[e] = 0.f;
-    sc[e] = 0;
-  }
+  const int l = threadIdx.x % LPT, g = threadIdx.x / LPT, wave = threadIdx.x >> 6;
+  for (int e = threadIdx.x; e < COLS; e += kFwd) sc[e] = 0;
   if (threadIdx.x == 0) sn = 0;
   __syncthreads();
   Cols<VEC> acc[NCH];
@@ -126,11 +128,11 @@ __global__ __launch_bounds__(kThreads) void k_balance(const BalanceArgs a) {
     for (int e = 0; e < VEC; ++e) acc[i].v[e] = 0.f;
   int n = 0;
   // (every lane of the workgroup runs as many rounds: the exchanges need them)
-  for (int t0 = blockIdx.x * TPB; t0 < a.T; t0 += gridDim.x * TPB) {
-    const int t = t0 + g;
+  for (int64_t t0 = (int64_t)blockIdx.x * TPB; t0 < a.T; t0 += gridDim.x * TPB) {
+    const int64_t t = t0 + g;
     const bool live = t < a.T && (!a.mask || a.mask[t]);
     Cols<VEC> p[NCH];
-    row_softmax<VEC, LPT, NCH>(a.logits, a.f32, (int64_t)t * a.E, a.E, l, live, p);
+    row_softmax<VEC, LPT, NCH>(a.logits, a.f32, t * a.E, a.E, l, live, p);
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
@@ -138,60 +140,71 @@ __global__ __launch_bounds__(kThreads) void k_balance(const BalanceArgs a) {
     if (live) {
       n += l == 0;
       for (int j = l; j < a.k; j += LPT) {
-        const int id = a.ids[(int64_t)t * a.k + j];
+        const int id = a.ids[t * a.k + j];
         if (id >= 0 && id < a.E) atomicAdd(&sc[id], 1);
       }
     }
   }
   if (n) atomicAdd(&sn, n);
-  // the lane groups add their sums one after the other
-  for (int q = 0; q < TPB; ++q) {
-    if (g == q) {
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        const int c = (i * LPT + l) * VEC;
-        if (c < a.E)
+  for (int i = 0; i < NCH; ++i)
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) sp[c + e] += acc[i].v[e];
-      }
+    for (int e = 0; e < VEC; ++e) {
+      const float s = stride_sum<LPT>(acc[i].v[e]);
+      if ((threadIdx.x & 63) < LPT) sp[wave][(i * LPT + l) * VEC + e] = s;
     }
-    __syncthreads();
+  __syncthreads();
+  const int e = threadIdx.x;
+  float s = 0.f;
+  int32_t c = 0;
+  if (e < a.E) {
+#pragma unroll
+    for (int w = 0; w < NW; ++w) s += sp[w][e];
+    c = sc[e];
   }
   if (gridDim.x == 1) {
-    finish(a, sp, sc, sn, red);
+    finish(a, s, c, sn);
     return;
   }
-  const int64_t at = (int64_t)blockIdx.x * a.E;
-  for (int e = threadIdx.x; e < a.E; e += kThreads) {
-    a.part_p[at + e] = sp[e];
-    a.part_c[at + e] = sc[e];
+  if (e < a.E) {
+    a.part_p[(int64_t)blockIdx.x * a.E + e] = s;
+    a.part_c[(int64_t)blockIdx.x * a.E + e] = c;
   }
-  if (threadIdx.x == 0) a.part_n[blockIdx.x] = sn;
+  if (e == 0) a.part_n[blockIdx.x] = sn;
 }
 
-// The workgroups' sums, by one workgroup.
-__global__ __launch_bounds__(1024) void k_balance_sum(const BalanceArgs a) {
-  __shared__ float sp[1024];
-  __shared__ int32_t sc[1024];
-  __shared__ float red[16];
+// The workgroups' sums, by one workgroup: thread (expert, slice) takes every
+// S-th workgroup's, then the slices are joined in order.
+__global__ __launch_bounds__(kFwd) void k_balance_sum(const BalanceArgs a) {
+  __shared__ float sp[kFwd];
+  __shared__ int32_t sc[kFwd];
   __shared__ int32_t sn;
-  if (threadIdx.x == 0) {
+  const int S = kFwd / a.E, e = threadIdx.x % a.E, q = threadIdx.x / a.E;
+  if (threadIdx.x < 64) {
     int n = 0;
-    for (int b = 0; b < a.blocks; ++b) n += a.part_n[b];
-    sn = n;
+    for (int b = threadIdx.x; b < a.blocks; b += 64) n += a.part_n[b];
+#pragma unroll
+    for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
+    if (threadIdx.x == 0) sn = n;
   }
-  for (int e = threadIdx.x; e < a.E; e += 1024) {
-    float p = 0.f;
-    int c = 0;
-    for (int b = 0; b < a.blocks; ++b) {
+  float p = 0.f;
+  int32_t c = 0;
+  if (q < S) {
+#pragma unroll 8
+    for (int b = q; b < a.blocks; b += S) {
       p += a.part_p[(int64_t)b * a.E + e];
       c += a.part_c[(int64_t)b * a.E + e];
     }
-    sp[e] = p;
-    sc[e] = c;
   }
+  sp[threadIdx.x] = p;
+  sc[threadIdx.x] = c;
   __syncthreads();
-  finish(a, sp, sc, sn, red);
+  if (q == 0)
+    for (int i = 1; i < S; ++i) {
+      p += sp[i * a.E + e];
+      c += sc[i * a.E + e];
+    }
+  finish(a, p, c, sn);
 }
 
 template <int VEC, int LPT, int NCH>
@@ -208,10 +221,10 @@ __global__ __launch_bounds__(kThreads) void k_balance_grad(const BalanceArgs a) 
 #pragma unroll
     for (int e = 0; e < VEC; ++e) f[i].v[e] = c < a.E ? (float)a.counts[c + e] : 0.f;
   }
-  for (int t0 = blockIdx.x * TPB; t0 < a.T; t0 += gridDim.x * TPB) {
-    const int t = t0 + g;
+  for (int64_t t0 = (int64_t)blockIdx.x * TPB; t0 < a.T; t0 += gridDim.x * TPB) {
+    const int64_t t = t0 + g;
     const bool live = t < a.T && (!a.mask || a.mask[t]);
-    const int64_t row = (int64_t)t * a.E;
+    const int64_t row = t * a.E;
     Cols<VEC> p[NCH];
     row_softmax<VEC, LPT, NCH>(a.logits, a.f32, row, a.E, l, live, p);
     float dot = 0.f;
@@ -256,36 +269,40 @@ hipError_t by_experts(int E, F&& f) {
 #undef LX_E
 }
 
-int tokens_per_block(int E) {
-  int tpb = 0;
+int lanes_per_token(int E) {
+  int n = 0;
   (void)by_experts(E, [&](auto, auto lpt, auto) {
-    tpb = kThreads / decltype(lpt)::value;
+    n = decltype(lpt)::value;
     return hipSuccess;
   });
-  return tpb;
+  return n;
 }
 
 }  // namespace
 
+// One workgroup up to 64 K logits: it takes about as long as the second launch
+// that it saves; from there on as many as give each two rounds of tokens, at
+// most 128, which is what one workgroup joins in a few microseconds.
 int balance_blocks(int T, int E) {
-  const int tpb = tokens_per_block(E);
-  return std::min(std::max((T + 4 * tpb - 1) / (4 * tpb), 1), 256);
+  if ((int64_t)T * E <= 1 << 16) return 1;
+  const int tpb = kFwd / lanes_per_token(E);
+  return (int)std::min<int64_t>(std::max<int64_t>(((int64_t)T + 2 * tpb - 1) / (2 * tpb), 1), 128);
 }
 
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {
   return by_experts(a.E, [&](auto v, auto l, auto n) {
-    k_balance<decltype(v)::value, decltype(l)::value, decltype(n)::value><<<a.blocks, kThreads, 0, s>>>(a);
+    k_balance<decltype(v)::value, decltype(l)::value, decltype(n)::value><<<a.blocks, kFwd, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 
 hipError_t launch_balance_sum(const BalanceArgs& a, hipStream_t s) {
-  k_balance_sum<<<1, 1024, 0, s>>>(a);
+  k_balance_sum<<<1, kFwd, 0, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_balance_grad(const BalanceArgs& a, hipStream_t s) {
-  const int tpb = tokens_per_block(a.E);
+  const int tpb = kThreads / lanes_per_token(a.E);
   const int grid = std::min((int)(((int64_t)a.T + tpb - 1) / tpb), 2048);
   return by_experts(a.E, [&](auto v, auto l, auto n) {
     k_balance_grad<decltype(v)::value, decltype(l)::value, decltype(n)::value><<<grid, kThreads, 0, s>>>(a);

@@ -145,8 +145,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_block_norm_grad(const
   F8 sp[NV], sq[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) sp[i] = sq[i] = F8{};
-  for (int t = grp; t < a.T; t += a.groups) {
-    const int64_t row = (int64_t)t * a.d;
+  for (int64_t t = grp; t < a.T; t += a.groups) {
+    const int64_t row = t * a.d;
     F8 m[NV], y[NV], D[NV], dx[NV];
     float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll

@@ -97,6 +97,21 @@ __device__ __forceinline__ float lane_reduce(float x) {
   }
   return x;
 }
+// Sum over the lanes of the wavefront that agree in lane % STRIDE.
+template <int STRIDE>
+__device__ __forceinline__ float stride_sum(float x) {
+  static_assert(STRIDE >= 8 && STRIDE <= 64, "");
+  if constexpr (STRIDE <= 8) x += dpp<0x128>(x);  // row_ror:8
+  if constexpr (STRIDE <= 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if constexpr (STRIDE <= 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return x;
+}
 template <int LANES>
 __device__ __forceinline__ float lane_sum(float x) {
   return lane_reduce<LANES, 0>(x);
