@@ -1,130 +1,163 @@
 // Block norms: the RMS norms before and after a block with its gate and
 // residual scale, forward and backward (formulas in lorex_block.h).
 //
-// A token's row stays in the registers of the TPR lanes that own it (NV groups
-// of 8 columns each), so every row is read once and written once; the row sums
-// go over lanes by DPP, over wavefronts through LDS.
+// Bound by memory: every row is read once and written once. A token's row stays
+// in the registers of the TPR lanes that own it, NV groups of 8 columns each;
+// row sums go over lanes by DPP, over wavefronts through LDS. Workgroups stay
+// for many rows, so the weight vectors are read once per workgroup.
 #include "lx_block.h"
 #include "lx_vec.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lx {
 namespace {
 
 // Sums of N values over the TPR lanes of a row. With more than one wavefront
-// per row each call takes LDS slots of its own (`slot`), so that one barrier
-// per call is enough.
+// per row each call takes LDS slots of its own (`lds`, N per wavefront of the
+// workgroup), so that one barrier per call is enough.
 template <int TPR, int N>
-__device__ __forceinline__ void row_sums(float (&x)[N], float* lds, int slot) {
+__device__ __forceinline__ void row_sums(float (&x)[N], float* lds) {
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = lane_sum<64>(x[i]);
   if constexpr (TPR > 64) {
     constexpr int NW = TPR / 64;
-    float* s = lds + slot * NW * N;
+    const int wave = threadIdx.x >> 6, w0 = wave / NW * NW;
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) s[(threadIdx.x >> 6) * N + i] = x[i];
+      for (int i = 0; i < N; ++i) lds[wave * N + i] = x[i];
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float t = 0.f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) t += s[w * N + i];
+      for (int w = 0; w < NW; ++w) t += lds[(w0 + w) * N + i];
       x[i] = t;
     }
   }
 }
 
+__device__ __forceinline__ float rms(float sum, int d, float eps) { return 1.f / sqrtf(sum / (float)d + eps); }
+
+// Forward workgroups: 256 threads, or one row's if it needs more.
+template <int TPR>
+constexpr int kFwdThreads = TPR < 256 ? 256 : TPR;
+
 template <int TPR, int NV>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_block_norm(const NormArgs a) {
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-  __shared__ float lds[2 * (TPR / 64)];
+__global__ __launch_bounds__(kFwdThreads<TPR>) void k_block_norm(const NormArgs a) {
+  constexpr int RPB = kFwdThreads<TPR> / TPR, NW = kFwdThreads<TPR> / 64;
+  __shared__ float lds[2 * NW];
   const int lt = threadIdx.x % TPR;
-  const int t = blockIdx.x * RPB + (int)threadIdx.x / TPR;
-  if (t >= a.T) return;  // (TPR > 64: one row per workgroup, so no barrier is missed)
-  const int64_t row = (int64_t)t * a.d;
-  F8 h[NV];
+  int col[NV];
   bool in[NV];
+  F8 sw[NV], wp[NV];  // scale w_post; w_pre
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = (i * TPR + lt) * 8;
-    in[i] = c < a.d;
-    if (in[i])
-      h[i] = load8(a.h, a.h_f32, row + c);
-    else
-      h[i] = F8{};
-  }
-  if (a.y) {
-    F8 y[NV];
+    col[i] = (i * TPR + lt) * 8;
+    in[i] = col[i] < a.d;
+    sw[i] = wp[i] = F8{{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}};
+    if (in[i]) {
+      if (a.w_pre) wp[i] = load8(a.w_pre, a.w_f32, col[i]);
+      if (a.w_post) sw[i] = load8(a.w_post, a.w_f32, col[i]);
+      if (a.scale) {
+        const F8 q = load8(a.scale, a.w_f32, col[i]);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) y[i] = F8{};
-    if (a.slot_row) {
-      for (int j = 0; j < a.k; ++j) {
-        const int r = a.slot_row[(int64_t)t * a.k + j];
-        const float w = a.slot_weights[(int64_t)t * a.k + j];
-        if (r < 0 || r >= a.y_rows) continue;
+        for (int e = 0; e < 8; ++e) sw[i].v[e] *= q.v[e];
+      }
+    }
+  }
+  // (the lanes of a row leave the loop together; with several wavefronts per
+  // row a workgroup has one row)
+  for (int64_t t = (int64_t)blockIdx.x * RPB + (int)threadIdx.x / TPR; t < a.T; t += (int64_t)gridDim.x * RPB) {
+    const int64_t row = t * a.d;
+    Raw8 rh[NV], ry[NV];
+    F8 h[NV], y[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      rh[i] = ry[i] = Raw8{};
+      if (in[i]) {
+        rh[i] = load_raw8(a.h, a.h_f32, row + col[i]);
+        if (a.y && !a.slot_row) ry[i] = load_raw8(a.y, a.y_f32, row + col[i]);
+      }
+    }
+    if (a.y) {
+      const float gate = a.gate ? a.gate[t] : 1.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) y[i] = a.slot_row ? F8{} : unpack8(ry[i], a.y_f32);
+      if (a.slot_row && a.y_rows > 0) {
+        // four slots' rows at a time; a dropped slot reads row 0 and adds nothing
+        for (int j0 = 0; j0 < a.k; j0 += 4) {
+          int r[4];
+          float w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            r[j] = j0 + j < a.k ? a.slot_row[t * a.k + j0 + j] : -1;
+            w[j] = j0 + j < a.k ? a.slot_weights[t * a.k + j0 + j] : 0.f;
+            if (r[j] >= a.y_rows) r[j] = -1;
+          }
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            Raw8 q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              q[j] = Raw8{};
+              if (in[i]) q[j] = load_raw8(a.y, a.y_f32, (int64_t)max(r[j], 0) * a.d + col[i]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (r[j] >= 0) {
+                const F8 v = unpack8(q[j], a.y_f32);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[i].v[e] += w[j] * v.v[e];
+              }
+          }
+        }
+      }
+      float g = gate;
+      if (a.w_post) {
+        float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          if (in[i]) {
-            const F8 q = load8(a.y, a.y_f32, (int64_t)r * a.d + (i * TPR + lt) * 8);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[i].v[e] += w * q.v[e];
-          }
+          for (int e = 0; e < 8; ++e) s[0] += y[i].v[e] * y[i].v[e];
+        row_sums<TPR>(s, lds);
+        g *= rms(s[0], a.d, a.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        h[i] = unpack8(rh[i], a.h_f32);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[i].v[e] = a.alpha * h[i].v[e] + g * (y[i].v[e] * sw[i].v[e]);
+        if (in[i]) store8(a.h_out, a.h_f32, row + col[i], h[i]);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (in[i]) y[i] = load8(a.y, a.y_f32, row + (i * TPR + lt) * 8);
+      for (int i = 0; i < NV; ++i) h[i] = unpack8(rh[i], a.h_f32);
     }
-    float r = a.gate ? a.gate[t] : 1.f;
-    if (a.w_post) {
+    if (a.w_pre) {
       float s[1] = {0.f};
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[0] += y[i].v[e] * y[i].v[e];
-      row_sums<TPR>(s, lds, 0);
-      r *= 1.f / sqrtf(s[0] / (float)a.d + a.eps);
+        for (int e = 0; e < 8; ++e) s[0] += in[i] ? h[i].v[e] * h[i].v[e] : 0.f;
+      row_sums<TPR>(s, lds + NW);
+      const float r = rms(s[0], a.d, a.eps);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (in[i]) {
+          F8 x;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x.v[e] = h[i].v[e] * r * wp[i].v[e];
+          store8(a.x, a.x_f32, row + col[i], x);
+        }
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (in[i]) {
-        const int c = (i * TPR + lt) * 8;
-        if (a.w_post) {
-          const F8 w = load8(a.w_post, a.w_f32, c);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[i].v[e] *= w.v[e];
-        }
-        if (a.scale) {
-          const F8 w = load8(a.scale, a.w_f32, c);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[i].v[e] *= w.v[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[i].v[e] = a.alpha * h[i].v[e] + r * y[i].v[e];
-        store8(a.h_out, a.h_f32, row + c, h[i]);
-      }
+    // without both sums a row has one barrier or none: the next row may only
+    // write the slots when all have read them
+    if constexpr (TPR > 64)
+      if (!(a.y && a.w_post && a.w_pre)) __syncthreads();
   }
-  if (!a.w_pre) return;
-  float s[1] = {0.f};
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s[0] += h[i].v[e] * h[i].v[e];
-  row_sums<TPR>(s, lds, 1);
-  const float r = 1.f / sqrtf(s[0] / (float)a.d + a.eps);
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (in[i]) {
-      const int c = (i * TPR + lt) * 8;
-      const F8 w = load8(a.w_pre, a.w_f32, c);
-      F8 x;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x.v[e] = h[i].v[e] * r * w.v[e];
-      store8(a.x, a.x_f32, row + c, x);
-    }
 }
 
 // Backward. With m = h' r_h, n = y r_y (no w_post: n = y, r_y = 1), D the
@@ -132,129 +165,154 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_block_norm(const Norm
 //   D    = dh' + r_h (dx w_pre - m mean(dx w_pre m))
 //   z    = sum_c D scale w_post n          (= dgate; gate z = sum_c dn n)
 //   dy   = r_y gate (D scale w_post - n z / d)     (no w_post: gate D scale)
-// so the row sums are {h'^2, y^2, dx w_pre h'} and then z. A row group keeps
-// its sums of dx m (dw_pre) and of gate D n (dw_post = scale q, dscale =
-// w_post q) in registers over its tokens and leaves them in part.
-template <int TPR, int NV>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_block_norm_grad(const NormGradArgs a) {
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-  __shared__ float lds[2 * 4 * (TPR / 64)];
-  const int lt = threadIdx.x % TPR;
-  const int grp = blockIdx.x * RPB + (int)threadIdx.x / TPR;
-  if (grp >= a.groups) return;
-  F8 sp[NV], sq[NV];
+// so the row sums are {h'^2, y^2, dx w_pre h'} and then z. A workgroup takes
+// one row or several at a time and stays for all of its rows, one workgroup per
+// compute unit; loading the next rows ahead of the sums cost more in registers
+// than it hid (8192 x 4096 with fp32 streams 130 against 127 us, 1777 x 2048 in
+// bf16 20.6 against 14.2). The sums over tokens of dx m (dw_pre) and of gate D n
+// (dw_post = scale q, dscale = w_post q) stay in registers, are joined over the
+// workgroup's rows in LDS and left in part, one pair of vectors per workgroup.
+// Where all rows are bf16 (BF) a lane's values take half the registers and a
+// workgroup has 1024 lanes, else 512.
+constexpr int bwd_threads(bool bf) { return bf ? 1024 : 512; }
+
+template <bool BF, int TPR, int NV>
+__global__ __launch_bounds__(bwd_threads(BF)) void k_block_norm_grad(const NormGradArgs a) {
+  constexpr int kBwd = bwd_threads(BF), RPB = kBwd / TPR, NW = kBwd / 64;
+  using Raw = std::conditional_t<BF, RawB8, Raw8>;
+  __shared__ float lds[4 * NW];
+  __shared__ float join[RPB > 1 ? 2 * RPB * TPR * NV * 8 : 1];
+  const int lt = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  int col[NV];
+  bool in[NV];
+  F8 sp[NV], sq[NV], sw[NV], wp[NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) sp[i] = sq[i] = F8{};
-  for (int64_t t = grp; t < a.T; t += a.groups) {
-    const int64_t row = t * a.d;
-    F8 m[NV], y[NV], D[NV], dx[NV];
-    float s[3] = {0.f, 0.f, 0.f};
+  for (int i = 0; i < NV; ++i) {
+    col[i] = (i * TPR + lt) * 8;
+    in[i] = col[i] < a.d;
+    sp[i] = sq[i] = F8{};
+    sw[i] = wp[i] = F8{{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}};
+    if (in[i]) {
+      if (a.w_pre) wp[i] = load8(a.w_pre, a.w_f32, col[i]);
+      if (a.w_post) sw[i] = load8(a.w_post, a.w_f32, col[i]);
+      if (a.scale) {
+        const F8 q = load8(a.scale, a.w_f32, col[i]);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + lt) * 8;
-      m[i] = y[i] = D[i] = dx[i] = F8{};
-      if (c < a.d) {
-        m[i] = load8(a.h_out, a.h_f32, row + c);
-        if (a.dh_out) D[i] = load8(a.dh_out, a.h_f32, row + c);
-        if (a.y) y[i] = load8(a.y, a.y_f32, row + c);
-        if (a.dx) {
-          dx[i] = load8(a.dx, a.x_f32, row + c);
-          const F8 w = load8(a.w_pre, a.w_f32, c);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s[2] += dx[i].v[e] * w.v[e] * m[i].v[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          s[0] += m[i].v[e] * m[i].v[e];
-          s[1] += y[i].v[e] * y[i].v[e];
-        }
-      }
-    }
-    row_sums<TPR>(s, lds, 0);
-    const float inv_d = 1.f / (float)a.d;
-    const float rh = 1.f / sqrtf(s[0] * inv_d + a.eps);
-    const float ry = a.w_post ? 1.f / sqrtf(s[1] * inv_d + a.eps) : 1.f;
-    const float mean = rh * s[2] * inv_d;
-    const float gate = a.gate ? a.gate[t] : 1.f;
-    const float alpha = a.y ? a.alpha : 1.f;
-    float z[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + lt) * 8;
-      if (c < a.d) {
-        if (a.dx) {
-          const F8 w = load8(a.w_pre, a.w_f32, c);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float mm = m[i].v[e] * rh;
-            D[i].v[e] += rh * (dx[i].v[e] * w.v[e] - mm * mean);
-            sp[i].v[e] += dx[i].v[e] * mm;
-          }
-        }
-        F8 o;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o.v[e] = alpha * D[i].v[e];
-        store8(a.dh, a.h_f32, row + c, o);
-        if (a.y) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            y[i].v[e] *= ry;
-            sq[i].v[e] += gate * D[i].v[e] * y[i].v[e];
-          }
-          if (a.scale) {
-            const F8 w = load8(a.scale, a.w_f32, c);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) D[i].v[e] *= w.v[e];
-          }
-          if (a.w_post) {
-            const F8 w = load8(a.w_post, a.w_f32, c);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) D[i].v[e] *= w.v[e];
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) z[0] += D[i].v[e] * y[i].v[e];
-        }
-      }
-    }
-    if (!a.y) {
-      if constexpr (TPR > 64) __syncthreads();  // the sums' slots are free again
-      continue;
-    }
-    // (the next row's first sums reuse the slots that every wavefront has read
-    // before this call's barrier)
-    row_sums<TPR>(z, lds, 3);
-    if (a.dgate && lt == 0) a.dgate[t] = z[0];
-    const float zn = a.w_post ? z[0] * inv_d : 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + lt) * 8;
-      if (c < a.d) {
-        F8 o;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o.v[e] = ry * gate * (D[i].v[e] - y[i].v[e] * zn);
-        store8(a.dy, a.y_f32, row + c, o);
+        for (int e = 0; e < 8; ++e) sw[i].v[e] *= q.v[e];
       }
     }
   }
-  float* const p = a.part + (int64_t)grp * 2 * a.d;
+  struct Row {
+    Raw m[NV], y[NV], D[NV], dx[NV];
+  };
+  auto load = [&](Row& r, int64_t t) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (i * TPR + lt) * 8;
-    if (c < a.d) {
-      store8(p, true, c, sp[i]);
-      store8(p + a.d, true, c, sq[i]);
+    for (int i = 0; i < NV; ++i) {
+      r.m[i] = r.y[i] = r.D[i] = r.dx[i] = Raw{};
+      if (in[i] && t < a.T) {
+        const int64_t at = t * a.d + col[i];
+        r.m[i] = load_as<Raw>(a.h_out, a.h_f32, at);
+        if (a.dx) r.dx[i] = load_as<Raw>(a.dx, a.x_f32, at);
+        if (a.dh_out) r.D[i] = load_as<Raw>(a.dh_out, a.h_f32, at);
+        if (a.y) r.y[i] = load_as<Raw>(a.y, a.y_f32, at);
+      }
+    }
+  };
+  const float inv_d = 1.f / (float)a.d, alpha = a.y ? a.alpha : 1.f;
+  const int64_t stride = (int64_t)a.groups * RPB;
+  // (all rows of the workgroup run as many rounds: the barriers need them)
+  for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < a.T; t0 += stride) {
+    const int64_t t = t0 + g, row = t * a.d;
+    const bool live = t < a.T;
+    F8 m[NV], y[NV], D[NV], dx[NV];
+    float s[3] = {0.f, 0.f, 0.f};
+    Row q;
+    load(q, t);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      m[i] = unpack8(q.m[i], a.h_f32);
+      y[i] = unpack8(q.y[i], a.y_f32);
+      D[i] = unpack8(q.D[i], a.h_f32);
+      dx[i] = unpack8(q.dx[i], a.x_f32);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s[0] += m[i].v[e] * m[i].v[e];
+        s[1] += y[i].v[e] * y[i].v[e];
+        s[2] += dx[i].v[e] * wp[i].v[e] * m[i].v[e];
+      }
+    }
+    const float gate = a.gate && live ? a.gate[t] : 1.f;
+    row_sums<TPR>(s, lds);
+    const float rh = a.dx ? rms(s[0], a.d, a.eps) : 0.f;
+    const float ry = a.w_post ? rms(s[1], a.d, a.eps) : 1.f;
+    const float mean = rh * s[2] * inv_d;
+    float z[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      F8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float mm = m[i].v[e] * rh;
+        D[i].v[e] += rh * (dx[i].v[e] * wp[i].v[e] - mm * mean);
+        sp[i].v[e] += dx[i].v[e] * mm;
+        o.v[e] = alpha * D[i].v[e];
+        y[i].v[e] *= ry;
+        sq[i].v[e] += gate * D[i].v[e] * y[i].v[e];
+        D[i].v[e] *= sw[i].v[e];
+        z[0] += D[i].v[e] * y[i].v[e];
+      }
+      if (in[i] && live) store8(a.dh, a.h_f32, row + col[i], o);
+    }
+    if (!a.y) {
+      if constexpr (TPR > 64) __syncthreads();  // (the sums' slots are free again)
+      continue;
+    }
+    row_sums<TPR>(z, lds + 3 * NW);
+    if (a.dgate && lt == 0 && live) a.dgate[t] = z[0];
+    const float zn = a.w_post ? z[0] * inv_d : 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      F8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o.v[e] = ry * gate * (D[i].v[e] - y[i].v[e] * zn);
+      if (in[i] && live) store8(a.dy, a.y_f32, row + col[i], o);
+    }
+  }
+  float* const p = a.part + (int64_t)blockIdx.x * 2 * a.d;
+  if constexpr (RPB == 1) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (in[i]) {
+        store8(p, true, col[i], sp[i]);
+        store8(p + a.d, true, col[i], sq[i]);
+      }
+  } else {
+    constexpr int W = TPR * NV * 8;  // columns of a row's lanes
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      store8(join + g * 2 * W, true, col[i], sp[i]);
+      store8(join + g * 2 * W + W, true, col[i], sq[i]);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * W; c += kBwd) {
+      float q = 0.f;
+#pragma unroll
+      for (int r = 0; r < RPB; ++r) q += join[r * 2 * W + c];
+      const int e = c < W ? c : c - W;
+      if (e < a.d) p[(c < W ? 0 : a.d) + e] = q;
     }
   }
 }
 
-// Sums of the row groups' partials: 32 columns per workgroup, its 32 rows of
-// lanes take every 32nd group, then LDS adds them in a fixed order.
+// Sums of the workgroups' partials: 32 columns per workgroup, its 32 rows of
+// lanes take every 32nd partial, then LDS adds them in a fixed order.
 __global__ __launch_bounds__(1024) void k_block_norm_grad_sum(const NormGradArgs a) {
   __shared__ float lds[32][33];
   const int x = threadIdx.x & 31, yy = threadIdx.x >> 5;
   const int col = blockIdx.x * 32 + x;  // [0, 2d)
   float s = 0.f;
   if (col < 2 * a.d)
+#pragma unroll 8
     for (int g = yy; g < a.groups; g += 32) s += a.part[(int64_t)g * 2 * a.d + col];
   lds[yy][x] = s;
   __syncthreads();
@@ -273,36 +331,53 @@ __global__ __launch_bounds__(1024) void k_block_norm_grad_sum(const NormGradArgs
   if (a.dscale) a.dscale[c] = w1(a.w_post) * s;
 }
 
-template <class F>
+// Lanes of a row and groups of 8 columns per lane: a row's lanes hold one group
+// each as long as MOST lanes do.
+template <int MOST, class F>
 hipError_t by_width(int d, F&& f) {
   using std::integral_constant;
-  if (d <= 512) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  if (d <= 1024) return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  if (d <= 2048) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-  if (d <= 4096) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  if (d <= 8192) return f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
-  if (d <= 16384) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-  return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+#define LX_W(T, N) f(integral_constant<int, T>{}, integral_constant<int, N>{})
+  if (d <= 512) return LX_W(64, 1);
+  if (d <= 1024) return LX_W(128, 1);
+  if (d <= 2048) return LX_W(256, 1);
+  if (d <= 4096) return LX_W(512, 1);
+  if (d <= 8192) return LX_W(MOST, 8192 / 8 / MOST);
+  if (d <= 16384) return LX_W(MOST, 16384 / 8 / MOST);
+  return LX_W(MOST, 32768 / 8 / MOST);
+#undef LX_W
 }
 
 }  // namespace
 
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t s) {
-  return by_width(a.d, [&](auto tpr, auto nv) {
-    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
-    constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-    k_block_norm<TPR, NV><<<(a.T + RPB - 1) / RPB, RPB * TPR, 0, s>>>(a);
+  return by_width<1024>(a.d, [&](auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, THR = kFwdThreads<TPR>;
+    constexpr int RPB = THR / TPR;
+    const int grid = (int)std::min<int64_t>(((int64_t)a.T + RPB - 1) / RPB, 256 * (2048 / THR));
+    k_block_norm<TPR, NV><<<grid, THR, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 
-int norm_grad_groups(int T, int) { return std::min(std::max(T, 1), 512); }
+// (as many for both kinds of rows: the kind's own number of rows at once only
+// moves rows between workgroups)
+int norm_grad_groups(int T, int d) {
+  int at_once = 1;
+  (void)by_width<512>(d, [&](auto tpr, auto) {
+    at_once = 512 / decltype(tpr)::value;
+    return hipSuccess;
+  });
+  return (int)std::min<int64_t>(std::max<int64_t>(((int64_t)T + at_once - 1) / at_once, 1), 256);
+}
 
 hipError_t launch_block_norm_grad(const NormGradArgs& a, hipStream_t s) {
-  return by_width(a.d, [&](auto tpr, auto nv) {
-    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
-    constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-    k_block_norm_grad<TPR, NV><<<(a.groups + RPB - 1) / RPB, RPB * TPR, 0, s>>>(a);
+  if (!a.h_f32 && (!a.y || !a.y_f32) && (!a.dx || !a.x_f32))
+    return by_width<1024>(a.d, [&](auto tpr, auto nv) {
+      k_block_norm_grad<true, decltype(tpr)::value, decltype(nv)::value><<<a.groups, 1024, 0, s>>>(a);
+      return hipGetLastError();
+    });
+  return by_width<512>(a.d, [&](auto tpr, auto nv) {
+    k_block_norm_grad<false, decltype(tpr)::value, decltype(nv)::value><<<a.groups, 512, 0, s>>>(a);
     return hipGetLastError();
   });
 }

@@ -42,7 +42,7 @@ struct NormGradArgs {
   float* part;       // [groups][2][d]: sums of dx m and of gate D n
   int32_t groups;
 };
-// Row groups whose partial weight gradients the workspace holds.
+// Workgroups of the backward, each with its partial weight gradients.
 int norm_grad_groups(int T, int d);
 hipError_t launch_block_norm_grad(const NormGradArgs& a, hipStream_t s);
 hipError_t launch_block_norm_grad_sum(const NormGradArgs& a, hipStream_t s);

@@ -54,6 +54,19 @@ __device__ __forceinline__ F8 unpack8(const Raw8& r, bool f32) {
 
 __device__ __forceinline__ F8 load8(const void* p, bool f32, int64_t i) { return unpack8(load_raw8(p, f32, i), f32); }
 
+// The same where the type is known to be bf16.
+struct RawB8 {
+  vu4 a;
+};
+template <class R>
+__device__ __forceinline__ R load_as(const void* p, bool f32, int64_t i) {
+  if constexpr (sizeof(R) == sizeof(RawB8))
+    return R{*(const vu4*)((const uint16_t*)p + i)};
+  else
+    return load_raw8(p, f32, i);
+}
+__device__ __forceinline__ F8 unpack8(const RawB8& r, bool) { return unpack8(Raw8{r.a, r.a}, false); }
+
 // two values to bf16, round to nearest even
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const vb2 q = {(__bf16)lo, (__bf16)hi};
