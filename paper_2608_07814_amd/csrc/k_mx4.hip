@@ -124,46 +124,156 @@ __device__ __forceinline__ bool find_tile(const Mx4GemmArgs& a, int tile, int& g
   return false;
 }
 
-// 16 rows x 64 columns per workgroup, 16 columns per wavefront, both operands
-// read from memory in the layout of the 16x16x128 instruction: lane l holds
-// row l % 16's block l / 16 of the 128 values of a step. The weights are the
-// instruction's first operand, so a lane ends with 4 consecutive columns of
-// one output row.
-__global__ __launch_bounds__(256) void k_mx4_gemm(const Mx4GemmArgs a) {
-  int g, m0, m1;
-  if (!find_tile<16>(a, blockIdx.x, g, m0, m1)) return;
-  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
-  const int n0 = blockIdx.y * 64 + (threadIdx.x >> 6) * 16;
-  if (n0 >= a.N) return;
-  const int m = m0 + l16;
-  int ar = -1;
-  if (m < m1) ar = a.row_map ? a.row_map[m] : m;
-  const bool live = ar >= 0 && ar < a.a_rows;
-  const int64_t arow = live ? ar : 0, brow = (int64_t)g * a.N + min(n0 + l16, a.N - 1);
-  const int cp = a.Kp / 2, sp = a.Kp / 32;
-  vf4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < a.Kp / 128; ++k) {
-    uint4 av = make_uint4(0, 0, 0, 0);
-    int as = 0;
-    if (live) {
-      av = *(const uint4*)(a.a + arow * cp + k * 64 + q * 16);
-      as = a.as[arow * sp + k * 4 + q];
+// Row tiles over all groups (tiles of BM rows counted group by group).
+template <int BM>
+__device__ __forceinline__ int count_tiles(const Mx4GemmArgs& a) {
+  if (!a.offsets) return (a.M + BM - 1) / BM;
+  const int lane = threadIdx.x & 63;
+  int all = 0;
+  for (int g0 = 0; g0 < a.G; g0 += 64) {
+    int n = 0;
+    if (g0 + lane < a.G) {
+      const int lo = min(max(a.offsets[g0 + lane], 0), a.M);
+      n = (min(max(a.offsets[g0 + lane + 1], lo), a.M) - lo + BM - 1) / BM;
     }
-    const uint4 bv = *(const uint4*)(a.b + brow * cp + k * 64 + q * 16);
-    const int bs = a.bs[brow * sp + k * 4 + q];
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag(bv), frag(av), acc, 4, 4, 0, bs, 0, as);
-  }
-  if (m >= m1) return;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int n = n0 + q * 4 + i;
-    if (n < a.N) {
-      const int64_t at = (int64_t)m * a.N + n;
-      if (a.out_f32)
-        ((float*)a.out)[at] = acc[i];
-      else
-        ((uint16_t*)a.out)[at] = (uint16_t)pack_bf16(acc[i], 0.f);
+    for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
+    all += n;
+  }
+  return __builtin_amdgcn_readfirstlane(all);
+}
+
+// ---------------------------------------------------------------- few rows
+// Four scale words of a row: 16 bytes at the words' own alignment. Read word by
+// word they took half as long again as the codes (512 rows of 128 experts of 1536
+// x 2048: 61 against 41 us).
+typedef uint32_t vu4w __attribute__((ext_vector_type(4), aligned(4)));
+
+// 16 MT rows x 16 columns per wavefront for batches of few rows per group:
+// bound by streaming the weights once. Both operands are read from memory in the
+// layout of the 16x16x128 instruction (lane l holds row l % 16's block l / 16 of
+// the 128 values of a step), 8 steps' loads in flight per wavefront; WK
+// wavefronts of a workgroup share the K of the same columns where there are few
+// columns, and add their sums in order. The weights are the instruction's first
+// operand, so a lane ends with 4 consecutive columns of one output row.
+template <int MT, int WK>
+__global__ __launch_bounds__(256) void k_mx4_gemm_rows(const Mx4GemmArgs a) {
+  constexpr int WN = 4 / WK;
+  __shared__ float part[WK > 1 ? WK - 1 : 1][MT][256];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave % WK, wn = wave / WK;
+  // work items: XCD x (workgroups go round the 8 XCDs) takes a contiguous
+  // range; without groups the row tiles of the same columns follow each other
+  const int ntn = (a.N + 16 * WN - 1) / (16 * WN);
+  const int rt = count_tiles<16 * MT>(a);
+  const int64_t items = (int64_t)rt * ntn, per = items / 8, rest = items % 8;
+  const int x = blockIdx.x & 7;
+  const int64_t mine = per + (x < rest), first = x * per + min((int64_t)x, rest);
+  const int cp = a.Kp / 2, sp = a.Kp / 32, steps = a.Kp / 128;
+  for (int64_t i = blockIdx.x >> 3; i < mine; i += gridDim.x >> 3) {
+    const int64_t L = first + i;
+    const int ti = (int)(a.offsets ? L / ntn : L % rt), n0 = (int)(a.offsets ? L % ntn : L / rt) * 16 * WN + wn * 16;
+    int g, m0, m1;
+    if (!find_tile<16 * MT>(a, ti, g, m0, m1)) return;
+    int arow[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const int m = m0 + t * 16 + l16;
+      arow[t] = -1;
+      if (m < m1) arow[t] = a.row_map ? a.row_map[m] : m;
+      if (arow[t] >= a.a_rows) arow[t] = -1;
     }
+    const int64_t brow = (int64_t)g * a.N + min(n0 + l16, a.N - 1);
+    const uint8_t* const B = a.b + brow * cp + q * 16;
+    const uint8_t* const Bs = a.bs + brow * sp;
+    vf4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = vf4{0.f, 0.f, 0.f, 0.f};
+    // U steps from k on, all of this wavefront's: their loads, then their products
+    auto batch = [&](auto count, int k) __attribute__((always_inline)) {
+      constexpr int U = decltype(count)::value, UW = U < 4 ? 1 : U / 4;
+      uint4 w[U], av[MT][U];
+      vu4 ws[UW], as[MT][UW];
+      auto words = [&](vu4(&v)[UW], const uint8_t* row) __attribute__((always_inline)) {
+        if constexpr (U < 4) {
+          v[0][0] = *(const uint32_t*)(row + k * 4);
+        } else {
+#pragma unroll
+          for (int c = 0; c < UW; ++c) v[c] = *(const vu4w*)(row + k * 4 + c * 16);
+        }
+      };
+#pragma unroll
+      for (int u = 0; u < U; ++u) w[u] = *(const uint4*)(B + (int64_t)(k + u) * 64);
+      words(ws, Bs);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) av[t][u] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int c = 0; c < UW; ++c) as[t][c] = vu4{0, 0, 0, 0};
+        if (arow[t] >= 0) {
+          const uint8_t* const A = a.a + (int64_t)arow[t] * cp + q * 16;
+#pragma unroll
+          for (int u = 0; u < U; ++u) av[t][u] = *(const uint4*)(A + (int64_t)(k + u) * 64);
+          words(as[t], a.as + (int64_t)arow[t] * sp);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+          acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag(w[u]), frag(av[t][u]), acc[t], 4, 4, 0,
+                                                                    ws[u / 4][u & 3] >> (8 * q), 0,
+                                                                    as[t][u / 4][u & 3] >> (8 * q));
+    };
+    const int k1 = (int)((int64_t)steps * (wk + 1) / WK);
+    int k = (int)((int64_t)steps * wk / WK);
+    for (; k + 8 <= k1; k += 8) batch(std::integral_constant<int, 8>{}, k);
+    if (k + 4 <= k1) {
+      batch(std::integral_constant<int, 4>{}, k);
+      k += 4;
+    }
+    for (; k < k1; ++k) batch(std::integral_constant<int, 1>{}, k);
+    if constexpr (WK > 1) {
+      if (wk > 0) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) *(vf4*)&part[wk - 1][t][lane * 4] = acc[t];
+      }
+      __syncthreads();
+      if (wk == 0) {
+#pragma unroll
+        for (int v = 0; v < WK - 1; ++v)
+#pragma unroll
+          for (int t = 0; t < MT; ++t) acc[t] += *(const vf4*)&part[v][t][lane * 4];
+      }
+    }
+    if (wk == 0) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        const int m = m0 + t * 16 + l16;
+        if (m < m1) {
+          const int64_t at = (int64_t)m * a.N + n0 + q * 4;
+          if (a.N % 4 == 0) {
+            if (n0 + q * 4 < a.N) {
+              if (a.out_f32)
+                *(vf4*)((float*)a.out + at) = acc[t];
+              else
+                *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack_bf16(acc[t][0], acc[t][1]), pack_bf16(acc[t][2], acc[t][3]));
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (n0 + q * 4 + j < a.N) {
+                if (a.out_f32)
+                  ((float*)a.out)[at + j] = acc[t][j];
+                else
+                  ((uint16_t*)a.out)[at + j] = (uint16_t)pack_bf16(acc[t][j], 0.f);
+              }
+          }
+        }
+      }
+    }
+    if constexpr (WK > 1) __syncthreads();
   }
 }
 
@@ -191,25 +301,6 @@ __device__ __forceinline__ void land_and_meet() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-}
-
-// Row tiles over all groups (tiles of BM rows counted group by group).
-template <int BM>
-__device__ __forceinline__ int count_tiles(const Mx4GemmArgs& a) {
-  if (!a.offsets) return (a.M + BM - 1) / BM;
-  const int lane = threadIdx.x & 63;
-  int all = 0;
-  for (int g0 = 0; g0 < a.G; g0 += 64) {
-    int n = 0;
-    if (g0 + lane < a.G) {
-      const int lo = min(max(a.offsets[g0 + lane], 0), a.M);
-      n = (min(max(a.offsets[g0 + lane + 1], lo), a.M) - lo + BM - 1) / BM;
-    }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
-    all += n;
-  }
-  return __builtin_amdgcn_readfirstlane(all);
 }
 
 // BM x BN outputs per workgroup, a 2 x 2 grid of wavefronts, 32x32x64
@@ -509,15 +600,25 @@ static hipError_t launch_tile(const Mx4GemmArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int MT, int WK>
+static hipError_t launch_rows(const Mx4GemmArgs& a, hipStream_t s) {
+  constexpr int BM = 16 * MT, BN = 16 * (4 / WK);
+  const int64_t tiles = a.offsets ? std::min<int64_t>((int64_t)a.M / BM + a.G, a.M) : ((int64_t)a.M + BM - 1) / BM;
+  const int64_t items = tiles * (((int64_t)a.N + BN - 1) / BN);
+  k_mx4_gemm_rows<MT, WK><<<(unsigned)std::min<int64_t>((items + 7) / 8 * 8, 1 << 16), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
 hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s) {
   const int rows = a.M / a.G;  // of a group on average
   // the tile kernels address A and a tile's weights by 32-bit byte offsets
   const bool near = (int64_t)a.a_rows * (a.Kp / 2) < ((int64_t)1 << 32) && a.a_rows > 0;
   if (near && rows >= 512) return launch_tile<256, 256>(a, s);
   if (near && rows >= 32) return launch_tile<128, 128>(a, s);
-  const int tiles = a.offsets ? (int)std::min<int64_t>((int64_t)a.M / 16 + a.G, a.M) : (a.M + 15) / 16;
-  k_mx4_gemm<<<dim3(tiles, (a.N + 63) / 64), 256, 0, s>>>(a);
-  return hipGetLastError();
+  const int64_t waves = ((int64_t)a.N + 15) / 16 * std::min(a.M, a.G);
+  if (waves < 2048) return launch_rows<1, 4>(a, s);
+  if (waves < 8192) return launch_rows<1, 2>(a, s);
+  return launch_rows<1, 1>(a, s);
 }
 
 }  // namespace lx
