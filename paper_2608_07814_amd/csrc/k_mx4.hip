@@ -314,7 +314,7 @@ __device__ __forceinline__ void land_and_meet() {
 // are the instruction's first operand: a lane ends with 4 consecutive columns
 // of one row, which go through LDS into whole rows.
 template <int BM, int BN>
-__global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_mx4_gemm_tile(const Mx4GemmArgs a) {
+__global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : BM * BN == 128 * 128 ? 2 : 3) void k_mx4_gemm_tile(const Mx4GemmArgs a) {
   constexpr int WM = BM / 2, WN = BN / 2, MI = WM / 32, NI = WN / 32;
   constexpr int RA = BM / 32, RB = BN / 32, R = RA + RB;  // 16-byte loads of a thread per step
   constexpr int STAGE = (BM + BN) * 128, SGRP = (BM + BN) * 16;
@@ -461,14 +461,16 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_mx4_gemm_t
   constexpr int kNone = R;
   auto multiply = [&](auto sv, auto first, int t) __attribute__((always_inline)) {
     constexpr int s = decltype(sv)::value, FIRST = decltype(first)::value;
-    constexpr int PER = MI * NI / (R / 2);
-    static_assert(PER >= 1 && MI * NI % (R / 2) == 0, "as many products between any two loads");
+    constexpr int P = MI * NI, H = R / 2;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < MI * NI; ++i) {
+    for (int i = 0; i < P; ++i) {
       const int mi = i / NI, ni = i % NI;
-      if (i % PER == 0) __builtin_amdgcn_sched_barrier(0);
-      if constexpr (FIRST < R)
-        if (i % PER == 0) issue_one(t, FIRST + i / PER, false);
+      if constexpr (FIRST < R) {
+        if (i * H / P < (i + 1) * H / P) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int l = i * H / P; l < (i + 1) * H / P; ++l) issue_one(t, FIRST + l, false);
+      }
       acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
           frag(fb[s & 1][ni]), frag(fa[s & 1][mi]), acc[mi][ni], 4, 4, 2 * (s & 1), s < 2 ? sc.b[ni].x : sc.b[ni].y,
           2 * (s & 1), s < 2 ? sc.a[mi].x : sc.a[mi].y);
@@ -609,16 +611,31 @@ static hipError_t launch_rows(const Mx4GemmArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Which kernel. Rows of a group are not known here, only their mean.
+//   at most 16 rows: the row kernel, K shared by four wavefronts where K is long
+//     and columns are few (4096 columns, K = 14336: 10.1 against 20.3 us alone;
+//     2048 x 2048: 8.4 against 7.1)
+//   256 x 256 tiles from a mean of 512 rows a group on, where there are enough
+//     to fill the machine (4096^3: 41 us, 128 x 128 47; 512 x 14336 x 4096, 112
+//     tiles: 34 against 24)
+//   128 x 128 tiles from a mean of 32 rows on, likewise (128 experts of 1536 x
+//     2048, 32768 rows: 144 us, 256 x 256 147, 64 x 64 186)
+//   64 x 64 tiles else (the same experts, 512 rows: 40 us, 128 x 128 45, row
+//     kernel 44 to 47; 128 x 14336 x 4096: 13.5 against 16.3)
 hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s) {
-  const int rows = a.M / a.G;  // of a group on average
   // the tile kernels address A and a tile's weights by 32-bit byte offsets
   const bool near = (int64_t)a.a_rows * (a.Kp / 2) < ((int64_t)1 << 32) && a.a_rows > 0;
-  if (near && rows >= 512) return launch_tile<256, 256>(a, s);
-  if (near && rows >= 32) return launch_tile<128, 128>(a, s);
-  const int64_t waves = ((int64_t)a.N + 15) / 16 * std::min(a.M, a.G);
-  if (waves < 2048) return launch_rows<1, 4>(a, s);
-  if (waves < 8192) return launch_rows<1, 2>(a, s);
-  return launch_rows<1, 1>(a, s);
+  if (a.M <= 16 || !near) {
+    const int64_t waves = ((int64_t)a.N + 15) / 16 * std::min(a.M, a.G);
+    if (waves <= 1024 && a.Kp >= 4096) return launch_rows<1, 4>(a, s);
+    return launch_rows<1, 1>(a, s);
+  }
+  const int64_t rows = a.M / a.G, groups = std::min(a.M, a.G);
+  // tiles of size b, a group's last one half full
+  auto tiles = [&](int64_t b) { return (a.M + groups * (b / 2)) / b * (((int64_t)a.N + b - 1) / b); };
+  if (rows >= 512 && tiles(256) >= 192) return launch_tile<256, 256>(a, s);
+  if (rows >= 32 && tiles(128) >= 192) return launch_tile<128, 128>(a, s);
+  return launch_tile<64, 64>(a, s);
 }
 
 }  // namespace lx
