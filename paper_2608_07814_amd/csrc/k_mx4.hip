@@ -13,71 +13,104 @@ namespace {
 constexpr int kBlk = 32;  // values under one scale
 
 // ---------------------------------------------------------------- rounding
-// A lane rounds 8 values, 4 lanes share a block of 32. The largest magnitude
-// goes over the 4 lanes as bits: as unsigned integers magnitudes keep their
-// order, and infinities and NaNs come out above every finite one. The
-// conversion instruction divides by a power of two, rounds to nearest even and
-// saturates at 6.
-__global__ __launch_bounds__(256) void k_mx4_quantize(const Mx4Args a) {
-  const int Kp = LX_MX4_KP(a.K);
-  const int64_t n = a.rows * (Kp / 8);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / (Kp / 8);
-    const int c = (int)(i - row * (Kp / 8)) * 8;
-    F8 x = F8{};
-    if (c < a.K) {
-      if (a.swiglu) {
-        const F8 g = load8(a.x, a.f32, row * 2 * a.K + c), u = load8(a.x, a.f32, row * 2 * a.K + a.K + c);
+// Both directions are bound by memory. A lane has 8 values of a row (4 lanes
+// share a block of 32), TPR lanes a row, and U rows under way at once; there is no
+// division by the row length.
+template <int U, class F>
+__device__ __forceinline__ void for_rows(int64_t rows, int vecs, int tpr, F&& f) {
+  const int lt = threadIdx.x & (tpr - 1), rpb = 256 / tpr;
+  for (int64_t r = (int64_t)blockIdx.x * rpb * U + (int)threadIdx.x / tpr; r < rows; r += (int64_t)gridDim.x * rpb * U)
+    for (int v = lt; v < vecs; v += tpr) f(r, rpb, v * 8);
+}
+
+// Rounding: the largest magnitude of a block goes over its 4 lanes as bits: as
+// unsigned integers magnitudes keep their order, and infinities and NaNs come
+// out above every finite one. The conversion instruction divides by a power of
+// two, rounds to nearest even and saturates at 6.
+__device__ __forceinline__ uint32_t mx4_round(F8 x, int& s) {
+  uint32_t top = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x.v[e] = g.v[e] / (1.f + expf(-g.v[e])) * u.v[e];
-      } else {
-        x = load8(a.x, a.f32, row * a.K + c);
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x.v[e]) & 0x7FFFFFFFu);
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, true));
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, true));
+  const int e = (int)(top >> 23);  // biased; 255: infinity or NaN
+  s = e == 255 ? 255 : e > 2 ? e - 2 : 0;
+  // (2^-127 is not a normal number: there the values are doubled instead)
+  const float f = __uint_as_float((uint32_t)(s > 0 ? s : 1) << 23);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x.v[j] = s > 0 ? x.v[j] : 2.f * x.v[j];
+  uint32_t code = 0;
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x.v[0], x.v[1], f, 0);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x.v[2], x.v[3], f, 1);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x.v[4], x.v[5], f, 2);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x.v[6], x.v[7], f, 3);
+  return s == 255 ? 0 : code;
+}
+
+template <int U, bool SWIGLU>
+__global__ __launch_bounds__(256) void k_mx4_quantize(const Mx4Args a, int tpr) {
+  const int Kp = LX_MX4_KP(a.K);
+  for_rows<U>(a.rows, Kp / 8, tpr, [&](int64_t r, int rpb, int c) {
+    Raw8 g[U], u[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int64_t row = r + (int64_t)j * rpb;
+      g[j] = u[j] = Raw8{};
+      if (row < a.rows && c < a.K) {
+        g[j] = load_raw8(a.x, a.f32, row * a.K * (SWIGLU ? 2 : 1) + c);
+        if (SWIGLU) u[j] = load_raw8(a.x, a.f32, row * a.K * 2 + a.K + c);
       }
     }
-    uint32_t top = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x.v[e]) & 0x7FFFFFFFu);
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, true));
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, true));
-    const int e = (int)(top >> 23);                  // biased; 255: infinity or NaN
-    const bool bad = e == 255;
-    const int s = bad ? 255 : e > 2 ? e - 2 : 0;     // scale byte
-    uint32_t code = 0;
-    if (!bad) {
-      // (2^-127 is not a normal number: there the values are doubled instead)
-      const float f = __uint_as_float((uint32_t)(s > 0 ? s : 1) << 23);
+    for (int j = 0; j < U; ++j) {
+      const int64_t row = r + (int64_t)j * rpb;
+      F8 x = unpack8(g[j], a.f32);
+      if (SWIGLU) {
+        const F8 w = unpack8(u[j], a.f32);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x.v[j] = s > 0 ? x.v[j] : 2.f * x.v[j];
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x.v[0], x.v[1], f, 0);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x.v[2], x.v[3], f, 1);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x.v[4], x.v[5], f, 2);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x.v[6], x.v[7], f, 3);
+        for (int e = 0; e < 8; ++e) x.v[e] = x.v[e] / (1.f + expf(-x.v[e])) * w.v[e];
+      }
+      int s;
+      const uint32_t code = mx4_round(x, s);
+      if (row < a.rows) {
+        *(uint32_t*)(a.codes + row * (Kp / 2) + c / 2) = code;
+        if ((c & (kBlk - 1)) == 0) a.scales[row * (Kp / kBlk) + c / kBlk] = (uint8_t)s;
+      }
     }
-    *(uint32_t*)(a.codes + row * (Kp / 2) + c / 2) = code;
-    if ((c & (kBlk - 1)) == 0) a.scales[row * (Kp / kBlk) + c / kBlk] = (uint8_t)s;
-  }
+  });
 }
 
-// 0.5 * the e2m1 value of a code, as an integer in half units: 0 1 2 3 4 6 8 12
-__device__ __forceinline__ float mx4_value(uint32_t c) {
-  const uint32_t m = c & 7;
-  const float v = (float)(m < 4 ? m : m < 6 ? 2 * m - 4 : 4 * m - 16) * 0.5f;
-  return c & 8 ? -v : v;
-}
-
-__global__ __launch_bounds__(256) void k_mx4_dequantize(const Mx4Args a) {
+template <int U>
+__global__ __launch_bounds__(256) void k_mx4_dequantize(const Mx4Args a, int tpr) {
   const int Kp = LX_MX4_KP(a.K);
-  const int64_t n = a.rows * (a.K / 8);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / (a.K / 8);
-    const int c = (int)(i - row * (a.K / 8)) * 8;
-    const uint32_t code = *(const uint32_t*)(a.codes + row * (Kp / 2) + c / 2);
-    const int s = a.scales[row * (Kp / kBlk) + c / kBlk];
-    F8 x;
+  for_rows<U>(a.rows, a.K / 8, tpr, [&](int64_t r, int rpb, int c) {
+    uint32_t code[U], s[U];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x.v[e] = s == 255 ? NAN : ldexpf(mx4_value(code >> (4 * e)), s - 127);
-    store8((void*)a.x, a.f32, row * a.K + c, x);
-  }
+    for (int j = 0; j < U; ++j) {
+      const int64_t row = r + (int64_t)j * rpb;
+      code[j] = s[j] = 0;
+      if (row < a.rows) {
+        code[j] = *(const uint32_t*)(a.codes + row * (Kp / 2) + c / 2);
+        s[j] = a.scales[row * (Kp / kBlk) + c / kBlk];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int64_t row = r + (int64_t)j * rpb;
+      const float f = __uint_as_float(s[j] == 255 ? 0x7FC00000u : s[j] ? s[j] << 23 : 0x00400000u);
+      F8 x;
+      auto two = [&](auto sel, float& lo, float& hi) {
+        const auto q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[j], 1.f, decltype(sel)::value);
+        lo = q[0] * f;
+        hi = q[1] * f;
+      };
+      two(std::integral_constant<int, 0>{}, x.v[0], x.v[1]);
+      two(std::integral_constant<int, 1>{}, x.v[2], x.v[3]);
+      two(std::integral_constant<int, 2>{}, x.v[4], x.v[5]);
+      two(std::integral_constant<int, 3>{}, x.v[6], x.v[7]);
+      if (row < a.rows) store8((void*)a.x, a.f32, row * a.K + c, x);
+    }
+  });
 }
 
 // ---------------------------------------------------------------- products
@@ -580,15 +613,35 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : BM * BN == 128 * 128
 
 }  // namespace
 
+// Lanes of a row for `vecs` groups of 8 values, workgroups for U rows at a time.
+static int row_lanes(int vecs) {
+  int n = 1;
+  while (n < vecs && n < 256) n *= 2;
+  return n;
+}
+static int row_grid(int64_t rows, int tpr, int U) {
+  const int64_t per = 256 / tpr * U;
+  return (int)std::min<int64_t>((rows + per - 1) / per, 1 << 16);
+}
+
 hipError_t launch_mx4_quantize(const Mx4Args& a, hipStream_t s) {
-  const int64_t n = a.rows * (LX_MX4_KP(a.K) / 8);
-  k_mx4_quantize<<<(int)std::min<int64_t>((n + 255) / 256, 1 << 16), 256, 0, s>>>(a);
+  const int tpr = row_lanes(LX_MX4_KP(a.K) / 8);
+  // four rows under way where that still leaves several workgroups per compute
+  // unit
+  const bool many = row_grid(a.rows, tpr, 4) >= 2048;
+  const int grid = row_grid(a.rows, tpr, many ? 4 : 1);
+  if (a.swiglu)
+    many ? k_mx4_quantize<4, true><<<grid, 256, 0, s>>>(a, tpr) : k_mx4_quantize<1, true><<<grid, 256, 0, s>>>(a, tpr);
+  else
+    many ? k_mx4_quantize<4, false><<<grid, 256, 0, s>>>(a, tpr) : k_mx4_quantize<1, false><<<grid, 256, 0, s>>>(a, tpr);
   return hipGetLastError();
 }
 
 hipError_t launch_mx4_dequantize(const Mx4Args& a, hipStream_t s) {
-  const int64_t n = a.rows * (a.K / 8);
-  k_mx4_dequantize<<<(int)std::min<int64_t>((n + 255) / 256, 1 << 16), 256, 0, s>>>(a);
+  const int tpr = row_lanes(a.K / 8);
+  const bool many = row_grid(a.rows, tpr, 4) >= 2048;
+  const int grid = row_grid(a.rows, tpr, many ? 4 : 1);
+  many ? k_mx4_dequantize<4><<<grid, 256, 0, s>>>(a, tpr) : k_mx4_dequantize<1><<<grid, 256, 0, s>>>(a, tpr);
   return hipGetLastError();
 }
 
