@@ -118,9 +118,44 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ v8i frag(const uint4& q) { return v8i{(int)q.x, (int)q.y, (int)q.z, (int)q.w, 0, 0, 0, 0}; }
 
-// The group and the first row of row tile `tile` (tiles of BM rows, counted
-// group by group), found by each wavefront: 64 groups at a time, a prefix sum
-// of their tile counts over the lanes. false: there is no such tile.
+// Inclusive prefix sum over the 64 lanes (all active): row shifts within 16
+// lanes, then the totals of the rows before.
+__device__ __forceinline__ int lane_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  const int r0 = __builtin_amdgcn_readlane(x, 15), r1 = __builtin_amdgcn_readlane(x, 31),
+            r2 = __builtin_amdgcn_readlane(x, 47), row = (threadIdx.x & 63) >> 4;
+  return x + (row >= 1 ? r0 : 0) + (row >= 2 ? r1 : 0) + (row >= 3 ? r2 : 0);
+}
+
+// A group's rows, clamped to [0, M].
+__device__ __forceinline__ void group_rows(const Mx4GemmArgs& a, int g, int& lo, int& hi) {
+  lo = hi = 0;
+  if (g < a.G) {
+    lo = min(max(a.offsets[g], 0), a.M);
+    hi = min(max(a.offsets[g + 1], lo), a.M);
+  }
+}
+
+// Row tiles over all groups (tiles of BM rows counted group by group).
+template <int BM>
+__device__ __forceinline__ int count_tiles(const Mx4GemmArgs& a) {
+  if (!a.offsets) return (a.M + BM - 1) / BM;
+  int n = 0;
+#pragma unroll 4
+  for (int g0 = 0; g0 < a.G; g0 += 64) {
+    int lo, hi;
+    group_rows(a, g0 + (threadIdx.x & 63), lo, hi);
+    n += (hi - lo + BM - 1) / BM;
+  }
+  return __builtin_amdgcn_readlane(lane_prefix(n), 63);
+}
+
+// The group and the rows of row tile `tile`, found by each wavefront: 64 groups
+// at a time, a prefix sum of their tile counts over the lanes. false: there is no
+// such tile. All results are uniform.
 template <int BM>
 __device__ __forceinline__ bool find_tile(const Mx4GemmArgs& a, int tile, int& g, int& m0, int& m1) {
   if (!a.offsets) {
@@ -129,27 +164,16 @@ __device__ __forceinline__ bool find_tile(const Mx4GemmArgs& a, int tile, int& g
     m1 = min(m0 + BM, a.M);
     return m0 < a.M;
   }
-  const int lane = threadIdx.x & 63;
+#pragma unroll 4
   for (int g0 = 0; g0 < a.G; g0 += 64) {
-    int lo = 0, hi = 0;
-    if (g0 + lane < a.G) {
-      lo = min(max(a.offsets[g0 + lane], 0), a.M);
-      hi = min(max(a.offsets[g0 + lane + 1], lo), a.M);
-    }
-    const int n = (hi - lo + BM - 1) / BM;
-    int sum = n;  // inclusive prefix sum
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int q = __shfl_up(sum, o);
-      if (lane >= o) sum += q;
-    }
-    const int all = __shfl(sum, 63);
+    int lo, hi;
+    group_rows(a, g0 + (threadIdx.x & 63), lo, hi);
+    const int n = (hi - lo + BM - 1) / BM, sum = lane_prefix(n), all = __builtin_amdgcn_readlane(sum, 63);
     if (tile < all) {
       const int src = __builtin_ctzll(__ballot(tile < sum));
       g = g0 + src;
-      const int first = __shfl(lo, src), last = __shfl(hi, src), before = __shfl(sum - n, src);
-      m0 = first + (tile - before) * BM;
-      m1 = min(m0 + BM, last);
+      m0 = __builtin_amdgcn_readlane(lo, src) + (tile - __builtin_amdgcn_readlane(sum - n, src)) * BM;
+      m1 = min(m0 + BM, __builtin_amdgcn_readlane(hi, src));
       return true;
     }
     tile -= all;
@@ -157,24 +181,18 @@ __device__ __forceinline__ bool find_tile(const Mx4GemmArgs& a, int tile, int& g
   return false;
 }
 
-// Row tiles over all groups (tiles of BM rows counted group by group).
-template <int BM>
-__device__ __forceinline__ int count_tiles(const Mx4GemmArgs& a) {
-  if (!a.offsets) return (a.M + BM - 1) / BM;
-  const int lane = threadIdx.x & 63;
-  int all = 0;
-  for (int g0 = 0; g0 < a.G; g0 += 64) {
-    int n = 0;
-    if (g0 + lane < a.G) {
-      const int lo = min(max(a.offsets[g0 + lane], 0), a.M);
-      n = (min(max(a.offsets[g0 + lane + 1], lo), a.M) - lo + BM - 1) / BM;
-    }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
-    all += n;
+// The work items of one workgroup: workgroups go round the 8 XCDs, and XCD x
+// takes a contiguous range of all items.
+struct Items {
+  int64_t at, end, step;
+  __device__ __forceinline__ Items(int64_t all) {
+    const int x = blockIdx.x & 7;
+    const int64_t per = all / 8, rest = all % 8, first = x * per + min((int64_t)x, rest);
+    at = first + (blockIdx.x >> 3);
+    end = first + per + (x < rest);
+    step = gridDim.x >> 3;
   }
-  return __builtin_amdgcn_readfirstlane(all);
-}
+};
 
 // ---------------------------------------------------------------- few rows
 // Four scale words of a row: 16 bytes at the words' own alignment. Read word by
@@ -195,16 +213,13 @@ __global__ __launch_bounds__(256) void k_mx4_gemm_rows(const Mx4GemmArgs a) {
   __shared__ float part[WK > 1 ? WK - 1 : 1][MT][256];
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave % WK, wn = wave / WK;
-  // work items: XCD x (workgroups go round the 8 XCDs) takes a contiguous
-  // range; without groups the row tiles of the same columns follow each other
   const int ntn = (a.N + 16 * WN - 1) / (16 * WN);
   const int rt = count_tiles<16 * MT>(a);
-  const int64_t items = (int64_t)rt * ntn, per = items / 8, rest = items % 8;
-  const int x = blockIdx.x & 7;
-  const int64_t mine = per + (x < rest), first = x * per + min((int64_t)x, rest);
   const int cp = a.Kp / 2, sp = a.Kp / 32, steps = a.Kp / 128;
-  for (int64_t i = blockIdx.x >> 3; i < mine; i += gridDim.x >> 3) {
-    const int64_t L = first + i;
+  Items it((int64_t)rt * ntn);
+  for (; it.at < it.end; it.at += it.step) {
+    // without groups the row tiles of the same columns follow each other
+    const int64_t L = it.at;
     const int ti = (int)(a.offsets ? L / ntn : L % rt), n0 = (int)(a.offsets ? L % ntn : L / rt) * 16 * WN + wn * 16;
     int g, m0, m1;
     if (!find_tile<16 * MT>(a, ti, g, m0, m1)) return;
@@ -346,77 +361,85 @@ __device__ __forceinline__ void land_and_meet() {
 // in groups of two steps (16 bytes a row) through a ring of two. The weights
 // are the instruction's first operand: a lane ends with 4 consecutive columns
 // of one row, which go through LDS into whole rows.
+// Workgroups stay for several items: the next item's place and rows are looked
+// up under the first loads of the present one, and its first loads are under way
+// while the present one's results are written.
+constexpr int tile_groups_per_cu(int bm, int bn) { return bm * bn > 128 * 128 ? 1 : bm * bn == 128 * 128 ? 2 : 4; }
+
 template <int BM, int BN>
-__global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : BM * BN == 128 * 128 ? 2 : 3) void k_mx4_gemm_tile(const Mx4GemmArgs a) {
+__global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_tile(const Mx4GemmArgs a) {
   constexpr int WM = BM / 2, WN = BN / 2, MI = WM / 32, NI = WN / 32;
   constexpr int RA = BM / 32, RB = BN / 32, R = RA + RB;  // 16-byte loads of a thread per step
   constexpr int STAGE = (BM + BN) * 128, SGRP = (BM + BN) * 16;
-  constexpr int EROW = WN + 4;                            // floats of an epilogue row
-  static_assert(2 * STAGE >= 4 * 32 * EROW * 4, "the epilogue reuses the ring");
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE + 2 * SGRP];
+  constexpr int LDS = 2 * STAGE + 2 * SGRP;
+  static_assert(LDS * tile_groups_per_cu(BM, BN) <= 160 * 1024, "");
+  static_assert(4 * 32 * WN * 4 <= STAGE, "32 rows of each wavefront's results fit in a stage");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
 
-  // work item: XCD x (workgroups go round the 8 XCDs) takes a contiguous range;
-  // column tiles in bands of 8, so that what an XCD runs together shares rows
-  // and weights in its L2
   const int ntn = (a.N + BN - 1) / BN;
   const int rt = count_tiles<BM>(a);
-  const int64_t items = (int64_t)rt * ntn;
-  const int x = blockIdx.x & 7;
-  const int64_t per = items / 8, rest = items % 8, i = blockIdx.x >> 3;
-  if (i >= per + (x < rest)) return;
-  const int64_t L = x * per + min((int64_t)x, rest) + i;
-  const int64_t per_band = (int64_t)rt * 8;
-  const int band = (int)(L / per_band), w = min(8, ntn - band * 8);
-  const int rem = (int)(L - band * per_band), ti = rem / w;
-  const int n0 = (band * 8 + rem - ti * w) * BN;
-  int g, m0, m1;
-  if (!find_tile<BM>(a, ti, g, m0, m1)) return;
-  g = __builtin_amdgcn_readfirstlane(g);
-  m0 = __builtin_amdgcn_readfirstlane(m0);
-  m1 = __builtin_amdgcn_readfirstlane(m1);
+  Items it((int64_t)rt * ntn);
+  if (it.at >= it.end) return;
 
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int lane = tid & 63;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int l32 = lane & 31, h = lane >> 5;
   const int wm = wave >> 1, wn = wave & 1;
   const int cp = a.Kp / 2, sp = a.Kp / 32, full = a.Kp / 256;
   const bool odd = a.Kp & 128;  // a last step of 128 values
 
-  // a row that is not there (past the tile, or a map entry out of range) reads
-  // A's first row (the host sees to it that there is one); its results are
-  // dropped
-  auto row_of = [&](int r) {
-    const int m = m0 + r;
-    if (m >= m1) return -1;
-    const int q = a.row_map ? a.row_map[m] : m;
-    return q >= 0 && q < a.a_rows ? q : -1;
+  struct Item {
+    int m0, m1, n0;
+    uint64_t there[(WM + 63) / 64];  // which of this wavefront's rows have a row of A
+    const uint8_t *B, *Bs;           // the tile's first weight row and its scales
+    uint32_t oa[RA], ob[RB];         // a thread's byte offsets from A (the host sees to it that they
+                                     // fit 32 bits) and from B
+    uint32_t qa, qb;                 // a thread's rows of the scale groups: one of A (threads below
+                                     // BM), one of B (threads below BN)
   };
-  // byte offsets from A (the host sees to it that they fit 32 bits) and from
-  // the tile's first weight row
-  uint32_t oa[RA], ob[RB];
-  const uint8_t* const B = a.b + ((int64_t)g * a.N + n0) * cp;
-  const uint8_t* const Bs = a.bs + ((int64_t)g * a.N + n0) * sp;
-#pragma unroll
-  for (int j = 0; j < RA; ++j) {
-    const int r = (j * 256 + tid) >> 3;
-    oa[j] = (uint32_t)max(row_of(r), 0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
-  }
-#pragma unroll
-  for (int j = 0; j < RB; ++j) {
-    const int r = (j * 256 + tid) >> 3;
-    ob[j] = (uint32_t)min(r, a.N - 1 - n0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
-  }
-  // a thread's rows of the scale groups: one row of A (threads below BM), one
-  // of B (threads below BN)
   static_assert(BM <= 256 && BN <= 256, "one row of each operand per thread");
-  const uint32_t qa = (uint32_t)max(row_of(tid % BM), 0) * (uint32_t)sp;
-  const uint32_t qb = (uint32_t)min(tid % BN, a.N - 1 - n0) * (uint32_t)sp;
+  // A's row for tile row r, -1 if there is none (past the tile, or a map entry out
+  // of range): its loads read A's first row (the host sees to it that there is
+  // one), its results are dropped or 0
+  auto row_of = [&](const Item& q, int r) __attribute__((always_inline)) {
+    const int m = q.m0 + r;
+    if (m >= q.m1) return -1;
+    const int src = a.row_map ? a.row_map[m] : m;
+    return src >= 0 && src < a.a_rows ? src : -1;
+  };
+  // Item L: column tiles in bands of 8, so that what an XCD runs together shares
+  // rows and weights in its L2.
+  auto look_up = [&](int64_t L, Item& q) __attribute__((always_inline)) {
+    const int64_t per_band = (int64_t)rt * 8;
+    const int band = (int)(L / per_band), w = min(8, ntn - band * 8);
+    const int rem = (int)(L - band * per_band), ti = rem / w;
+    q.n0 = (band * 8 + rem - ti * w) * BN;
+    int g = 0;
+    q.m0 = q.m1 = 0;
+    find_tile<BM>(a, ti, g, q.m0, q.m1);
+    q.B = a.b + ((int64_t)g * a.N + q.n0) * cp;
+    q.Bs = a.bs + ((int64_t)g * a.N + q.n0) * sp;
+#pragma unroll
+    for (int j = 0; j < RA; ++j) {
+      const int r = (j * 256 + tid) >> 3;
+      q.oa[j] = (uint32_t)max(row_of(q, r), 0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
+    }
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+      const int r = (j * 256 + tid) >> 3;
+      q.ob[j] = (uint32_t)min(r, a.N - 1 - q.n0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
+    }
+    q.qa = (uint32_t)max(row_of(q, tid % BM), 0) * (uint32_t)sp;
+    q.qb = (uint32_t)min(tid % BN, a.N - 1 - q.n0) * (uint32_t)sp;
+#pragma unroll
+    for (int j = 0; j < (WM + 63) / 64; ++j) q.there[j] = __ballot(row_of(q, wm * WM + j * 64 + lane) >= 0);
+  };
+  Item cur;
   // group q of the scales: words 4 q .. 4 q + 3 of every row, 16 bytes a row
-  auto issue_scales = [&](int q) {
+  auto issue_scales = [&](int q) __attribute__((always_inline)) {
     uint8_t* const st = smem + 2 * STAGE + (q & 1) * SGRP;
     if (a.wide_scales) {
-      if (wave < BM / 64) load_lds<16>(a.as + q * 16, qa, st + wave * 1024);
-      if (wave < BN / 64) load_lds<16>(Bs + q * 16, qb, st + BM * 16 + wave * 1024);
+      if (wave < BM / 64) load_lds<16>(a.as + q * 16, cur.qa, st + wave * 1024);
+      if (wave < BN / 64) load_lds<16>(cur.Bs + q * 16, cur.qb, st + BM * 16 + wave * 1024);
     } else {
       // rows that are no multiple of 16 bytes: word by word, 16 rows x 4 words
       // per load; words past the row's end repeat its last one
@@ -425,9 +448,9 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : BM * BN == 128 * 128
       for (int r0 = wave * 16; r0 < BM + BN; r0 += 64) {
         const int r = r0 + (lane >> 2);
         if (r0 < BM)
-          load_lds<4>(a.as, (uint32_t)max(row_of(r), 0) * (uint32_t)sp + word, st + r0 * 16);
+          load_lds<4>(a.as, (uint32_t)max(row_of(cur, r), 0) * (uint32_t)sp + word, st + r0 * 16);
         else
-          load_lds<4>(Bs, (uint32_t)min(r - BM, a.N - 1 - n0) * (uint32_t)sp + word, st + r0 * 16);
+          load_lds<4>(cur.Bs, (uint32_t)min(r - BM, a.N - 1 - cur.n0) * (uint32_t)sp + word, st + r0 * 16);
       }
     }
   };
@@ -439,22 +462,17 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : BM * BN == 128 * 128
     const int j = i < RA ? i : i - RA;
     const uint32_t back = half ? ((tid ^ (((j * 256 + tid) >> 3) >> 1)) & 4) * 16 : 0;
     if (i < RA)
-      load_lds<16>(a.a + at, oa[j] - back, st + (j * 4 + wave) * 1024);
+      load_lds<16>(a.a + at, cur.oa[j] - back, st + (j * 4 + wave) * 1024);
     else
-      load_lds<16>(B + at, ob[j] - back, st + BM * 128 + (j * 4 + wave) * 1024);
+      load_lds<16>(cur.B + at, cur.ob[j] - back, st + BM * 128 + (j * 4 + wave) * 1024);
   };
-  auto issue = [&](int t, bool half) {
+  auto issue = [&](int t, bool half) __attribute__((always_inline)) {
     if ((t & 1) == 0) issue_scales(t >> 1);
 #pragma unroll
     for (int i = 0; i < R; ++i) issue_one(t, i, half);
   };
 
   f32x16 acc[MI][NI];
-#pragma unroll
-  for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-    for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
-
   // a row's scales of a step are two words: a lane's block of instruction s is
   // 2 s + h, so after a shift by h bytes its scale is byte 0 or 2 of word s / 2
   const uint8_t* const la = smem + (wm * WM + l32) * 128;
@@ -536,78 +554,100 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : BM * BN == 128 * 128
     multiply(i2, none, 0);
     land_and_meet();
   };
+  look_up(it.at, cur);
   issue(0, full == 0);
-  land_and_meet();
-  if (full > 0) {
-    if (full > 1 || odd) issue(1, full == 1);
-    read_scales(sc, 0);
-    read(0, 0);
-    shift_scales(sc);
-    read(1, 0);
-    multiply(i0, none, 0);
-    read(2, 0);
-    multiply(i1, none, 0);
-    read(3, 0);
-    multiply(i2, none, 0);
+  for (;;) {
+    it.at += it.step;
+    const bool more = it.at < it.end;
+    Item next;
+    if (more) look_up(it.at, next);
     land_and_meet();
-    int t = 1;
-    for (; t + 1 < full; ++t) step(t, std::true_type{});
-    if (t < full) {
-      if (odd) issue(full, true);
-      step(t, std::false_type{});
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
+    if (full > 0) {
+      if (full > 1 || odd) issue(1, full == 1);
+      read_scales(sc, 0);
+      read(0, 0);
+      shift_scales(sc);
+      read(1, 0);
+      multiply(i0, none, 0);
+      read(2, 0);
+      multiply(i1, none, 0);
+      read(3, 0);
+      multiply(i2, none, 0);
+      land_and_meet();
+      int t = 1;
+      for (; t + 1 < full; ++t) step(t, std::true_type{});
+      if (t < full) {
+        if (odd) issue(full, true);
+        step(t, std::false_type{});
+      }
+      multiply(i3, none, 0);
     }
-    multiply(i3, none, 0);
-  }
-  if (odd) {
-    read_scales(sc, full);
-    read(0, full);
-    shift_scales(sc);
-    read(1, full);
-    multiply(i0, none, 0);
-    multiply(i1, none, 0);
-  }
-  land_and_meet();
+    if (odd) {
+      read_scales(sc, full);
+      read(0, full);
+      shift_scales(sc);
+      read(1, full);
+      multiply(i0, none, 0);
+      multiply(i1, none, 0);
+      land_and_meet();  // (the ring is free)
+    }
 
-  // epilogue: 32 rows at a time through this wavefront's own LDS (the empty asm
-  // keeps its addresses from being formed before the loop, where they would not
-  // fit in registers)
-  asm volatile("" : "+v"(lane));
-  float* const e = (float*)smem + wave * 32 * EROW;
-  const int nb = n0 + wn * WN;
-  const bool vec = a.N % 8 == 0;
+    const int m0 = cur.m0, m1 = cur.m1, nb = cur.n0 + wn * WN;
+    uint64_t there[(WM + 63) / 64];
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi) {
+    for (int j = 0; j < (WM + 63) / 64; ++j) there[j] = cur.there[j];
+    if (more) {
+      cur = next;
+      issue(0, full == 0);
+    }
+
+    // 32 rows at a time through this wavefront's part of stage 1 (the next item's
+    // first step is on its way into stage 0), 16-byte chunks XORed by the row, and
+    // out as whole rows of WN columns (the empty asm keeps the addresses from being
+    // formed before the loop, where they would not fit in registers)
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    constexpr int LPR = WN / 8;  // lanes of a row
+    uint8_t* const e = smem + STAGE + wave * 32 * WN * 4;
+    auto chunk = [](int r, int c) { return r * WN * 4 + (c ^ (WN == 32 ? (r >> 1) & 7 : r & 15)) * 16; };
+    const bool vec = a.N % 8 == 0;
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni)
+    for (int mi = 0; mi < MI; ++mi) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *(vf4*)(e + l32 * EROW + ni * 32 + q * 8 + h * 4) =
-            vf4{acc[mi][ni][4 * q], acc[mi][ni][4 * q + 1], acc[mi][ni][4 * q + 2], acc[mi][ni][4 * q + 3]};
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    constexpr int LPR = WN / 8, RPI = 64 / LPR;  // lanes of a row, rows per round
-    const int c = (lane % LPR) * 8;
+      for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *(vf4*)(e + chunk(ln & 31, ni * 8 + 2 * q + (ln >> 5))) =
+              vf4{acc[mi][ni][4 * q], acc[mi][ni][4 * q + 1], acc[mi][ni][4 * q + 2], acc[mi][ni][4 * q + 3]};
+      asm volatile("" ::: "memory");  // (a wavefront's LDS accesses run in order)
 #pragma unroll 4
-    for (int r0 = 0; r0 < 32; r0 += RPI) {
-      const int r = wm * WM + mi * 32 + r0 + lane / LPR, m = m0 + r;
-      const vf4 u = *(const vf4*)(e + (r0 + lane / LPR) * EROW + c), v = *(const vf4*)(e + (r0 + lane / LPR) * EROW + c + 4);
-      if (m < m1 && nb + c < a.N) {
-        F8 o{{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]}};
-        if (a.row_map && row_of(r) < 0) o = F8{};
-        const int64_t at = (int64_t)m * a.N + nb + c;
-        if (vec) {
-          store8(a.out, a.out_f32, at, o);
-        } else {
-          for (int k = 0; k < 8; ++k)
-            if (nb + c + k < a.N) {
-              if (a.out_f32)
-                ((float*)a.out)[at + k] = o.v[k];
-              else
-                ((uint16_t*)a.out)[at + k] = (uint16_t)pack_bf16(o.v[k], 0.f);
-            }
+      for (int r0 = 0; r0 < 32; r0 += 64 / LPR) {
+        const int r = r0 + ln / LPR, wr = mi * 32 + r, m = m0 + wm * WM + wr, c = nb + ln % LPR * 8;
+        const vf4 u = *(const vf4*)(e + chunk(r, ln % LPR * 2)), v = *(const vf4*)(e + chunk(r, ln % LPR * 2 + 1));
+        if (m < m1 && c < a.N) {
+          F8 o{{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]}};
+          if (!(there[mi / 2] >> (wr & 63) & 1)) o = F8{};
+          const int64_t at = (int64_t)m * a.N + c;
+          if (vec) {
+            store8(a.out, a.out_f32, at, o);
+          } else {
+            for (int k = 0; k < 8; ++k)
+              if (c + k < a.N) {
+                if (a.out_f32)
+                  ((float*)a.out)[at + k] = o.v[k];
+                else
+                  ((uint16_t*)a.out)[at + k] = (uint16_t)pack_bf16(o.v[k], 0.f);
+              }
+          }
         }
       }
+      asm volatile("" ::: "memory");
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (!more) break;
   }
 }
 
@@ -651,7 +691,8 @@ static hipError_t launch_tile(const Mx4GemmArgs& a, hipStream_t s) {
   const int64_t items = tiles * (((int64_t)a.N + BN - 1) / BN);
   Mx4GemmArgs t = a;
   t.wide_scales = a.Kp % 512 == 0 && ((uintptr_t)a.as & 15) == 0 && ((uintptr_t)a.bs & 15) == 0;
-  k_mx4_gemm_tile<BM, BN><<<(unsigned)((items + 7) / 8 * 8), 256, 0, s>>>(t);
+  const int64_t most = 256 * tile_groups_per_cu(BM, BN);
+  k_mx4_gemm_tile<BM, BN><<<(unsigned)std::min((items + 7) / 8 * 8, most), 256, 0, s>>>(t);
   return hipGetLastError();
 }
 
