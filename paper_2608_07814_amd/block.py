@@ -225,8 +225,10 @@ def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Opti
         dh = _empty(shape, h_out.dtype, h_out, stream)
     if dy is None and y is not None:
         dy = _empty(shape, y.dtype, h_out, stream)
-    grad = lambda v, n: None if v is None else _empty((n,), torch.float32, h_out, stream)  # noqa: E731
-    dgate, dw_pre, dw_post, dscale = grad(gate, T), grad(w_pre, d), grad(w_post, d), grad(scale, d)
+    dgate = None if gate is None else _empty((T,), torch.float32, h_out, stream)
+    given = [v is not None for v in (w_pre, w_post, scale)]
+    rows = iter(_empty((sum(given), d), torch.float32, h_out, stream).unbind(0) if any(given) else ())
+    dw_pre, dw_post, dscale = (next(rows) if g else None for g in given)
     L = lib()
     keep, ws, n = _workspace(workspace, L.lx_block_norm_backward_workspace_bytes(T, d), h_out, stream)
     st = L.lx_block_norm_backward(

@@ -249,11 +249,14 @@ __global__ __launch_bounds__(kThreads) void k_balance_grad(const BalanceArgs a) 
 }
 
 // Rows of a multiple of 8 logits are read 16 bytes (bf16) at a time by as few
-// lanes as hold the row, others one logit at a time.
+// lanes as hold the row, others and the shortest one logit at a time.
 template <class F>
 hipError_t by_experts(int E, F&& f) {
   using std::integral_constant;
 #define LX_E(V, L, N) f(integral_constant<int, V>{}, integral_constant<int, L>{}, integral_constant<int, N>{})
+  if (E <= 8) return LX_E(1, 8, 1);
+  if (E <= 16) return LX_E(1, 16, 1);
+  if (E <= 32) return LX_E(1, 32, 1);
   if (E % 8 == 0) {
     if (E <= 64) return LX_E(8, 8, 1);
     if (E <= 128) return LX_E(8, 16, 1);
@@ -280,13 +283,13 @@ int lanes_per_token(int E) {
 
 }  // namespace
 
-// One workgroup up to 64 K logits: it takes about as long as the second launch
-// that it saves; from there on as many as give each two rounds of tokens, at
-// most 128, which is what one workgroup joins in a few microseconds.
+// A round is the tokens that a workgroup takes at once. One workgroup up to
+// three rounds, which take about as long as the second launch that it saves;
+// from there on as many as have two rounds each, at most 128, which is what one
+// workgroup joins in a few microseconds.
 int balance_blocks(int T, int E) {
-  if ((int64_t)T * E <= 1 << 16) return 1;
-  const int tpb = kFwd / lanes_per_token(E);
-  return (int)std::min<int64_t>(std::max<int64_t>(((int64_t)T + 2 * tpb - 1) / (2 * tpb), 1), 128);
+  const int64_t tpb = kFwd / lanes_per_token(E), rounds = (T + tpb - 1) / tpb;
+  return rounds <= 3 ? 1 : (int)std::min<int64_t>((rounds + 1) / 2, 128);
 }
 
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {

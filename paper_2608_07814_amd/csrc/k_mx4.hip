@@ -199,6 +199,7 @@ struct Items {
 // word they took half as long again as the codes (512 rows of 128 experts of 1536
 // x 2048: 61 against 41 us).
 typedef uint32_t vu4w __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t vu2h __attribute__((ext_vector_type(2), aligned(2)));
 
 // 16 MT rows x 16 columns per wavefront for batches of few rows per group:
 // bound by streaming the weights once. Both operands are read from memory in the
@@ -301,13 +302,11 @@ __global__ __launch_bounds__(256) void k_mx4_gemm_rows(const Mx4GemmArgs a) {
         const int m = m0 + t * 16 + l16;
         if (m < m1) {
           const int64_t at = (int64_t)m * a.N + n0 + q * 4;
-          if (a.N % 4 == 0) {
-            if (n0 + q * 4 < a.N) {
-              if (a.out_f32)
-                *(vf4*)((float*)a.out + at) = acc[t];
-              else
-                *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack_bf16(acc[t][0], acc[t][1]), pack_bf16(acc[t][2], acc[t][3]));
-            }
+          if (n0 + q * 4 + 4 <= a.N) {
+            if (a.out_f32)
+              *(vf4w*)((float*)a.out + at) = acc[t];
+            else
+              *(vu2h*)((uint16_t*)a.out + at) = vu2h{pack_bf16(acc[t][0], acc[t][1]), pack_bf16(acc[t][2], acc[t][3])};
           } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -371,7 +370,7 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
   constexpr int WM = BM / 2, WN = BN / 2, MI = WM / 32, NI = WN / 32;
   constexpr int RA = BM / 32, RB = BN / 32, R = RA + RB;  // 16-byte loads of a thread per step
   constexpr int STAGE = (BM + BN) * 128, SGRP = (BM + BN) * 16;
-  constexpr int LDS = 2 * STAGE + 2 * SGRP;
+  constexpr int LDS = 2 * STAGE + 2 * SGRP + 16;  // (a half step reads a word past its scales)
   static_assert(LDS * tile_groups_per_cu(BM, BN) <= 160 * 1024, "");
   static_assert(4 * 32 * WN * 4 <= STAGE, "32 rows of each wavefront's results fit in a stage");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
@@ -434,16 +433,21 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     for (int j = 0; j < (WM + 63) / 64; ++j) q.there[j] = __ballot(row_of(q, wm * WM + j * 64 + lane) >= 0);
   };
   Item cur;
-  // group q of the scales: words 4 q .. 4 q + 3 of every row, 16 bytes a row
+  // Group q of the scales: words 4 q .. 4 q + 3 of every row, 16 bytes a row (a
+  // memory address need only be aligned to words). A row's last group holds its
+  // last four words, so a step finds its words `late` words further on.
+  const int words = sp / 4;
+  auto late = [&](int q) __attribute__((always_inline)) { return words < 4 ? 0 : max(q * 4 - (words - 4), 0); };
   auto issue_scales = [&](int q) __attribute__((always_inline)) {
     uint8_t* const st = smem + 2 * STAGE + (q & 1) * SGRP;
-    if (a.wide_scales) {
-      if (wave < BM / 64) load_lds<16>(a.as + q * 16, cur.qa, st + wave * 1024);
-      if (wave < BN / 64) load_lds<16>(cur.Bs + q * 16, cur.qb, st + BM * 16 + wave * 1024);
+    if (words >= 4) {
+      const int at = (q * 4 - late(q)) * 4;
+      if (wave < BM / 64) load_lds<16>(a.as + at, cur.qa, st + wave * 1024);
+      if (wave < BN / 64) load_lds<16>(cur.Bs + at, cur.qb, st + BM * 16 + wave * 1024);
     } else {
-      // rows that are no multiple of 16 bytes: word by word, 16 rows x 4 words
-      // per load; words past the row's end repeat its last one
-      const int word = min(q * 4 + (lane & 3), sp / 4 - 1) * 4;
+      // rows of fewer words: word by word, 16 rows x 4 words per load, the last
+      // one repeated
+      const int word = min(lane & 3, words - 1) * 4;
 #pragma unroll 1
       for (int r0 = wave * 16; r0 < BM + BN; r0 += 64) {
         const int r = r0 + (lane >> 2);
@@ -485,11 +489,14 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
   } sc, nx;
   uint4 fa[2][MI], fb[2][NI];
   auto read_scales = [&](Scales& q, int t) __attribute__((always_inline)) {
-    const int st = ((t >> 1) & 1) * SGRP + (t & 1) * 8;
+    const int st = ((t >> 1) & 1) * SGRP + (t & 1) * 8 + late(t >> 1) * 4;
+    auto two = [&](const uint8_t* p) __attribute__((always_inline)) {
+      return make_uint2(*(const uint32_t*)p, *(const uint32_t*)(p + 4));
+    };
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) q.b[ni] = *(const uint2*)(lsb + st + ni * 512);
+    for (int ni = 0; ni < NI; ++ni) q.b[ni] = two(lsb + st + ni * 512);
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) q.a[mi] = *(const uint2*)(lsa + st + mi * 512);
+    for (int mi = 0; mi < MI; ++mi) q.a[mi] = two(lsa + st + mi * 512);
   };
   auto shift_scales = [&](Scales& q) __attribute__((always_inline)) {
 #pragma unroll
@@ -577,7 +584,7 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
       multiply(i1, none, 0);
       read(3, 0);
       multiply(i2, none, 0);
-      land_and_meet();
+        land_and_meet();
       int t = 1;
       for (; t + 1 < full; ++t) step(t, std::true_type{});
       if (t < full) {
@@ -614,7 +621,6 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     constexpr int LPR = WN / 8;  // lanes of a row
     uint8_t* const e = smem + STAGE + wave * 32 * WN * 4;
     auto chunk = [](int r, int c) { return r * WN * 4 + (c ^ (WN == 32 ? (r >> 1) & 7 : r & 15)) * 16; };
-    const bool vec = a.N % 8 == 0;
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
 #pragma unroll
@@ -632,10 +638,11 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
           F8 o{{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]}};
           if (!(there[mi / 2] >> (wr & 63) & 1)) o = F8{};
           const int64_t at = (int64_t)m * a.N + c;
-          if (vec) {
-            store8(a.out, a.out_f32, at, o);
+          if (c + 8 <= a.N) {
+            store8_any(a.out, a.out_f32, at, o);
           } else {
-            for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int k = 0; k < 7; ++k)
               if (c + k < a.N) {
                 if (a.out_f32)
                   ((float*)a.out)[at + k] = o.v[k];
@@ -689,10 +696,8 @@ template <int BM, int BN>
 static hipError_t launch_tile(const Mx4GemmArgs& a, hipStream_t s) {
   const int64_t tiles = a.offsets ? std::min<int64_t>((int64_t)a.M / BM + a.G, a.M) : ((int64_t)a.M + BM - 1) / BM;
   const int64_t items = tiles * (((int64_t)a.N + BN - 1) / BN);
-  Mx4GemmArgs t = a;
-  t.wide_scales = a.Kp % 512 == 0 && ((uintptr_t)a.as & 15) == 0 && ((uintptr_t)a.bs & 15) == 0;
   const int64_t most = 256 * tile_groups_per_cu(BM, BN);
-  k_mx4_gemm_tile<BM, BN><<<(unsigned)std::min((items + 7) / 8 * 8, most), 256, 0, s>>>(t);
+  k_mx4_gemm_tile<BM, BN><<<(unsigned)std::min((items + 7) / 8 * 8, most), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -95,7 +95,6 @@ struct Mx4GemmArgs {
   const int32_t* offsets;
   int32_t G, M, N, Kp;
   uint8_t out_f32;
-  uint8_t wide_scales;  // tile kernels: scale rows may be read 16 bytes at a time
   void* out;
 };
 hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s);

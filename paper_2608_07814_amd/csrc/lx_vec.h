@@ -84,6 +84,20 @@ __device__ __forceinline__ void store8(void* p, bool f32, int64_t i, const F8& x
   }
 }
 
+// 8 values to a place that is only aligned to its type.
+typedef uint32_t vu4h __attribute__((ext_vector_type(4), aligned(2)));
+typedef float vf4w __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void store8_any(void* p, bool f32, int64_t i, const F8& x) {
+  if (f32) {
+    vf4w* q = (vf4w*)((float*)p + i);
+    q[0] = vf4w{x.v[0], x.v[1], x.v[2], x.v[3]};
+    q[1] = vf4w{x.v[4], x.v[5], x.v[6], x.v[7]};
+  } else {
+    *(vu4h*)((uint16_t*)p + i) = vu4h{pack_bf16(x.v[0], x.v[1]), pack_bf16(x.v[2], x.v[3]), pack_bf16(x.v[4], x.v[5]),
+                                      pack_bf16(x.v[6], x.v[7])};
+  }
+}
+
 // The value of the lane that DPP control C selects (all lanes active).
 template <int C>
 __device__ __forceinline__ float dpp(float x) {
