@@ -714,13 +714,13 @@ static hipError_t launch_rows(const Mx4GemmArgs& a, hipStream_t s) {
 //   at most 16 rows: the row kernel, K shared by four wavefronts where K is long
 //     and columns are few (4096 columns, K = 14336: 10.1 against 20.3 us alone;
 //     2048 x 2048: 8.4 against 7.1)
-//   256 x 256 tiles from a mean of 512 rows a group on, where there are enough
-//     to fill the machine (4096^3: 41 us, 128 x 128 47; 512 x 14336 x 4096, 112
-//     tiles: 34 against 24)
-//   128 x 128 tiles from a mean of 32 rows on, likewise (128 experts of 1536 x
-//     2048, 32768 rows: 144 us, 256 x 256 147, 64 x 64 186)
-//   64 x 64 tiles else (the same experts, 512 rows: 40 us, 128 x 128 45, row
-//     kernel 44 to 47; 128 x 14336 x 4096: 13.5 against 16.3)
+//   else the tile that leaves the fullest compute unit the least work: a 256 x 256
+//     tile counts 1, one of 128 x 128 0.3 and one of 64 x 64 0.1, what they take
+//     next to each other on a full machine (4096^3, 1024 tiles of 128 x 128: 47
+//     against 41 us; 128 experts of 1536 x 2048, 32768 rows, 64 x 64 186 against
+//     144); a group's last tile is taken to be half full. So 512 x 14336 x 4096 runs
+//     on 448 tiles of 128 x 128 (24 us) and not on 112 of 256 x 256 (34), and 512 rows
+//     of the 128 experts on 64 x 64 ones (40, 128 x 128 45, row kernel 44 to 47)
 hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s) {
   // the tile kernels address A and a tile's weights by 32-bit byte offsets
   const bool near = (int64_t)a.a_rows * (a.Kp / 2) < ((int64_t)1 << 32) && a.a_rows > 0;
@@ -729,11 +729,14 @@ hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s) {
     if (waves <= 1024 && a.Kp >= 4096) return launch_rows<1, 4>(a, s);
     return launch_rows<1, 1>(a, s);
   }
-  const int64_t rows = a.M / a.G, groups = std::min(a.M, a.G);
-  // tiles of size b, a group's last one half full
-  auto tiles = [&](int64_t b) { return (a.M + groups * (b / 2)) / b * (((int64_t)a.N + b - 1) / b); };
-  if (rows >= 512 && tiles(256) >= 192) return launch_tile<256, 256>(a, s);
-  if (rows >= 32 && tiles(128) >= 192) return launch_tile<128, 128>(a, s);
+  const int64_t groups = std::min(a.M, a.G);
+  auto load = [&](int64_t b, double weight) {
+    const int64_t rows = a.G > 1 ? (a.M + groups * (b / 2)) / b : (a.M + b - 1) / b;
+    return (double)((rows * (((int64_t)a.N + b - 1) / b) + 255) / 256) * weight;
+  };
+  const double w256 = load(256, 1.0), w128 = load(128, 0.3), w64 = load(64, 0.1);
+  if (w256 < w128 && w256 < w64) return launch_tile<256, 256>(a, s);
+  if (w128 <= w64) return launch_tile<128, 128>(a, s);
   return launch_tile<64, 64>(a, s);
 }
 
