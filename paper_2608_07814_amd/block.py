@@ -392,3 +392,70 @@ def mx4_gemm(a: Mx4, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map:
     if st:
         _check(st)
     return out
+
+
+# ------------------------------------------------------------ a MoE block in 4 bits
+class Mx4Experts(NamedTuple):
+    """The E experts of a layer in 4 bits: the gate and up projections as one
+    weight [E][2f][d] (gate rows first), the down projection [E][d][f]."""
+    gate_up: Mx4
+    down: Mx4
+
+
+def mx4_experts(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, stream=None) -> Mx4Experts:
+    """Experts w_gate, w_up [E][f][d], w_down [E][d][f] rounded to 4 bits, once
+    when a model is loaded."""
+    return Mx4Experts(mx4_quantize(torch.cat([w_gate, w_up], dim=1), stream=stream),
+                      mx4_quantize(w_down.contiguous(), stream=stream))
+
+
+class Mx4BlockOut(NamedTuple):
+    h_out: torch.Tensor              # [T][d] the stream after the block
+    x_next: Optional[torch.Tensor]   # [T][d] the next block's input (w_next given)
+    x: torch.Tensor                  # [T][d] this block's input
+    topk_ids: torch.Tensor
+    topk_weights: torch.Tensor
+    logits: Optional[torch.Tensor]   # [T][E] (balance_coef given)
+    balance: Optional[BalanceLoss]
+
+
+def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, experts: Mx4Experts, k: int, *,
+                  w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0, eps: float = 1e-6,
+                  w_next: Optional[torch.Tensor] = None, balance_coef: Optional[float] = None,
+                  mask: Optional[torch.Tensor] = None) -> Mx4BlockOut:
+    """One MoE block with its experts in 4 bits, on the current stream: norm,
+    router (lx_route_topk), bucketing (lx_bucket), the experts' products per
+    group of rows with SwiGLU and rounding between them, then the experts' sum,
+    norm, gate, residual and the next block's norm in one kernel. h [T][d], w_r
+    [E][d] bf16 (d a multiple of 64, E of 4); the other arguments as in
+    :func:`block_norm`. With ``balance_coef`` the router's logits and balance
+    loss too (tokens whose ``mask`` is 0 left out)."""
+    T, d = h.shape
+    E = experts.gate_up.codes.shape[0]
+    f = experts.down.K
+    _, x = block_norm(h, w_pre=w_pre, eps=eps)
+    ids, weights = lx.route_topk(x, w_r, k)
+    logits = balance = None
+    if balance_coef is not None:
+        logits = x @ w_r.t()
+        balance = balance_loss(logits, ids, mask=mask, coef=balance_coef)
+    # rows of the experts: a tree without levels, whose weights bucketing does not read
+    tree = lx.LxTreeLayer()
+    tree.E, tree.d, tree.f, tree.dtype, tree.n_anchors = E, d, f, LX_BF16, E
+    tree.anchor_gate = tree.anchor_up = tree.anchor_down = experts.gate_up.codes.data_ptr()
+    L = lib()
+    n = L.lx_moe_tree_workspace_bytes(ctypes.byref(tree), T, k)
+    if not n:
+        raise lx.LorexError(lx.LX_ERR_UNSUPPORTED, L.lx_last_error().decode())
+    ws = h.new_empty(n, dtype=torch.uint8)
+    row_token = h.new_empty(T * min(k, E), dtype=torch.int32)
+    offsets = h.new_empty(E + 1, dtype=torch.int32)
+    slot_row = h.new_empty((T, k), dtype=torch.int32)
+    _check(L.lx_bucket(ctypes.byref(tree), T, k, ids.data_ptr(), 0, row_token.data_ptr(), offsets.data_ptr(),
+                       slot_row.data_ptr(), ws.data_ptr(), n, _handle(None, h.get_device())))
+    gate_up = mx4_gemm(mx4_quantize(x), experts.gate_up, offsets=offsets, row_map=row_token, out_dtype=torch.bfloat16)
+    y = mx4_gemm(mx4_quantize(gate_up, act=MX4_SWIGLU), experts.down, offsets=offsets, out_dtype=torch.float32)
+    h_out, x_next = block_norm(h, y, w_pre=w_next, w_post=w_post, scale=scale, gate=gate, slot_row=slot_row,
+                               slot_weights=weights, residual_scale=residual_scale, eps=eps)
+    return Mx4BlockOut(h_out, x_next, x, ids, weights, logits, balance)
