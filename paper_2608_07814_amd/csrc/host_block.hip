@@ -91,6 +91,10 @@ lx_status check_mx4_gemm(int32_t M, int32_t N, int32_t K, int32_t G) {
   return LX_OK;
 }
 
+size_t mx4_gemm_bytes(const Mx4GemmPlan& p, int M, int N) {
+  return p.splits > 1 ? up256((size_t)p.splits * M * N * sizeof(float)) : 0;
+}
+
 }  // namespace
 }  // namespace lx
 
@@ -292,7 +296,7 @@ lx_status lx_mx4_dequantize(const void* codes, const void* scales, int64_t rows,
 size_t lx_mx4_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t G) {
   clear_error();
   if (check_mx4_gemm(M, N, K, G) != LX_OK) return 0;
-  return 0;
+  return mx4_gemm_bytes(mx4_gemm_plan(M, N, LX_MX4_KP(K), G), M, N);
 }
 
 lx_status lx_mx4_gemm(const void* a, const void* a_scales, int32_t a_rows, const int32_t* row_map, const void* b,
@@ -308,9 +312,16 @@ lx_status lx_mx4_gemm(const void* a, const void* a_scales, int32_t a_rows, const
   if (!a || !a_scales || !b || !b_scales || !out || !al(a, 16) || !al(b, 16) || !al(out, 16) || !al(a_scales, 4) ||
       !al(b_scales, 4) || !al(row_map, 4) || !al(offsets, 4))
     return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
-  (void)workspace;
-  (void)workspace_bytes;
   Mx4GemmArgs g{};
+  g.plan = mx4_gemm_plan(M, N, LX_MX4_KP(K), G);
+  const size_t need = mx4_gemm_bytes(g.plan, M, N);
+  if (need) {
+    if (!workspace || !al(workspace, 256)) return set_error(LX_ERR_INVALID_ARGUMENT, "workspace null or not 256-byte aligned");
+    if (workspace_bytes < need) return set_error(LX_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than required");
+  }
+  // the tile kernels address A and a tile's weights by 32-bit byte offsets
+  if (a_rows == 0 || (int64_t)a_rows * (LX_MX4_KP(K) / 2) >= ((int64_t)1 << 32)) g.plan = {Mx4GemmPlan::kRows, 1, 0};
+  g.part = (float*)workspace;
   g.a = (const uint8_t*)a;
   g.as = (const uint8_t*)a_scales;
   g.b = (const uint8_t*)b;
@@ -324,7 +335,9 @@ lx_status lx_mx4_gemm(const void* a, const void* a_scales, int32_t a_rows, const
   g.Kp = LX_MX4_KP(K);
   g.out_f32 = out_dtype == LX_F32;
   g.out = out;
-  return run("mx4_gemm", launch_mx4_gemm, g, stream);
+  const lx_status s1 = run("mx4_gemm", launch_mx4_gemm, g, stream);
+  if (s1 != LX_OK || g.plan.splits == 1) return s1;
+  return run("mx4_gemm_sum", launch_mx4_gemm_sum, g, stream);
 }
 
 }  // extern "C"

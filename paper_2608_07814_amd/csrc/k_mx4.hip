@@ -360,12 +360,15 @@ __device__ __forceinline__ void land_and_meet() {
 // in groups of two steps (16 bytes a row) through a ring of two. The weights
 // are the instruction's first operand: a lane ends with 4 consecutive columns
 // of one row, which go through LDS into whole rows.
+// SPLIT: an item is one of a.plan.splits parts of a tile's K (whole steps, an even
+// number in all but the last), and its results are an fp32 [M][N] of its own, which
+// a second launch adds up in order.
 // Workgroups stay for several items: the next item's place and rows are looked
 // up under the first loads of the present one, and its first loads are under way
 // while the present one's results are written.
 constexpr int tile_groups_per_cu(int bm, int bn) { return bm * bn > 128 * 128 ? 1 : bm * bn == 128 * 128 ? 2 : 4; }
 
-template <int BM, int BN>
+template <int BM, int BN, bool SPLIT>
 __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_tile(const Mx4GemmArgs a) {
   constexpr int WM = BM / 2, WN = BN / 2, MI = WM / 32, NI = WN / 32;
   constexpr int RA = BM / 32, RB = BN / 32, R = RA + RB;  // 16-byte loads of a thread per step
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
 
   const int ntn = (a.N + BN - 1) / BN;
   const int rt = count_tiles<BM>(a);
-  Items it((int64_t)rt * ntn);
+  Items it((int64_t)rt * ntn * (SPLIT ? a.plan.splits : 1));
   if (it.at >= it.end) return;
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -388,6 +391,8 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
 
   struct Item {
     int m0, m1, n0;
+    int split, t0, t1;               // steps t0 .. t1 - 1 of 256 values (t0 is even)
+    bool tail;                       // and then the half step
     uint64_t there[(WM + 63) / 64];  // which of this wavefront's rows have a row of A
     const uint8_t *B, *Bs;           // the tile's first weight row and its scales
     uint32_t oa[RA], ob[RB];         // a thread's byte offsets from A (the host sees to it that they
@@ -408,6 +413,18 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
   // Item L: column tiles in bands of 8, so that what an XCD runs together shares
   // rows and weights in its L2.
   auto look_up = [&](int64_t L, Item& q) __attribute__((always_inline)) {
+    q.split = 0;
+    q.t0 = 0;
+    q.t1 = full;
+    q.tail = odd;
+    if constexpr (SPLIT) {
+      const int64_t all = (int64_t)rt * ntn;
+      q.split = (int)(L / all);
+      L -= q.split * all;
+      q.t0 = q.split * a.plan.split_steps;
+      q.t1 = min(q.t0 + a.plan.split_steps, full);
+      q.tail = odd && q.split == a.plan.splits - 1;
+    }
     const int64_t per_band = (int64_t)rt * 8;
     const int band = (int)(L / per_band), w = min(8, ntn - band * 8);
     const int rem = (int)(L - band * per_band), ti = rem / w;
@@ -562,7 +579,7 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     land_and_meet();
   };
   look_up(it.at, cur);
-  issue(0, full == 0);
+  issue(cur.t0, cur.t0 == full);
   for (;;) {
     it.at += it.step;
     const bool more = it.at < it.end;
@@ -573,27 +590,28 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
-    if (full > 0) {
-      if (full > 1 || odd) issue(1, full == 1);
-      read_scales(sc, 0);
-      read(0, 0);
+    int t = cur.t0;
+    const int t1 = cur.t1;
+    if (t < t1) {
+      if (t + 1 < t1 || cur.tail) issue(t + 1, t + 1 == full);
+      read_scales(sc, t);
+      read(0, t);
       shift_scales(sc);
-      read(1, 0);
+      read(1, t);
       multiply(i0, none, 0);
-      read(2, 0);
+      read(2, t);
       multiply(i1, none, 0);
-      read(3, 0);
+      read(3, t);
       multiply(i2, none, 0);
-        land_and_meet();
-      int t = 1;
-      for (; t + 1 < full; ++t) step(t, std::true_type{});
-      if (t < full) {
-        if (odd) issue(full, true);
+      land_and_meet();
+      for (++t; t + 1 < t1; ++t) step(t, std::true_type{});
+      if (t < t1) {
+        if (cur.tail) issue(full, true);
         step(t, std::false_type{});
       }
       multiply(i3, none, 0);
     }
-    if (odd) {
+    if (cur.tail) {
       read_scales(sc, full);
       read(0, full);
       shift_scales(sc);
@@ -607,9 +625,11 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     uint64_t there[(WM + 63) / 64];
 #pragma unroll
     for (int j = 0; j < (WM + 63) / 64; ++j) there[j] = cur.there[j];
+    void* const out = SPLIT ? (void*)(a.part + (int64_t)cur.split * a.M * a.N) : a.out;
+    const bool out_f32 = SPLIT || a.out_f32;
     if (more) {
       cur = next;
-      issue(0, full == 0);
+      issue(cur.t0, cur.t0 == full);
     }
 
     // 32 rows at a time through this wavefront's part of stage 1 (the next item's
@@ -639,15 +659,15 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
           if (!(there[mi / 2] >> (wr & 63) & 1)) o = F8{};
           const int64_t at = (int64_t)m * a.N + c;
           if (c + 8 <= a.N) {
-            store8_any(a.out, a.out_f32, at, o);
+            store8_any(out, out_f32, at, o);
           } else {
 #pragma unroll
             for (int k = 0; k < 7; ++k)
               if (c + k < a.N) {
-                if (a.out_f32)
-                  ((float*)a.out)[at + k] = o.v[k];
+                if (out_f32)
+                  ((float*)out)[at + k] = o.v[k];
                 else
-                  ((uint16_t*)a.out)[at + k] = (uint16_t)pack_bf16(o.v[k], 0.f);
+                  ((uint16_t*)out)[at + k] = (uint16_t)pack_bf16(o.v[k], 0.f);
               }
           }
         }
@@ -655,6 +675,33 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
       asm volatile("" ::: "memory");
     }
     if (!more) break;
+  }
+}
+
+// The parts' sums, in order, for the rows that belong to a group.
+__global__ __launch_bounds__(256) void k_mx4_gemm_sum(const Mx4GemmArgs a) {
+  const int lo = a.offsets ? min(max(a.offsets[0], 0), a.M) : 0, hi = a.offsets ? min(max(a.offsets[a.G], lo), a.M) : a.M;
+  const int64_t first = (int64_t)lo * a.N, end = (int64_t)hi * a.N, all = (int64_t)a.M * a.N;
+  for (int64_t i = first + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < end; i += (int64_t)gridDim.x * 1024) {
+    const int n = (int)min(end - i, (int64_t)4);
+    vf4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.plan.splits; ++s) {
+      const float* const p = a.part + s * all + i;
+      if (n == 4)
+        v += *(const vf4w*)p;
+      else
+        for (int j = 0; j < n; ++j) v[j] += p[j];
+    }
+    if (a.out_f32) {
+      if (n == 4)
+        *(vf4w*)((float*)a.out + i) = v;
+      else
+        for (int j = 0; j < n; ++j) ((float*)a.out)[i + j] = v[j];
+    } else if (n == 4) {
+      *(vu2h*)((uint16_t*)a.out + i) = vu2h{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    } else {
+      for (int j = 0; j < n; ++j) ((uint16_t*)a.out)[i + j] = (uint16_t)pack_bf16(v[j], 0.f);
+    }
   }
 }
 
@@ -692,12 +739,12 @@ hipError_t launch_mx4_dequantize(const Mx4Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int BM, int BN>
+template <int BM, int BN, bool SPLIT = false>
 static hipError_t launch_tile(const Mx4GemmArgs& a, hipStream_t s) {
   const int64_t tiles = a.offsets ? std::min<int64_t>((int64_t)a.M / BM + a.G, a.M) : ((int64_t)a.M + BM - 1) / BM;
-  const int64_t items = tiles * (((int64_t)a.N + BN - 1) / BN);
+  const int64_t items = tiles * (((int64_t)a.N + BN - 1) / BN) * (SPLIT ? a.plan.splits : 1);
   const int64_t most = 256 * tile_groups_per_cu(BM, BN);
-  k_mx4_gemm_tile<BM, BN><<<(unsigned)std::min((items + 7) / 8 * 8, most), 256, 0, s>>>(a);
+  k_mx4_gemm_tile<BM, BN, SPLIT><<<(unsigned)std::min((items + 7) / 8 * 8, most), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -721,23 +768,51 @@ static hipError_t launch_rows(const Mx4GemmArgs& a, hipStream_t s) {
 //     144); a group's last tile is taken to be half full. So 512 x 14336 x 4096 runs
 //     on 448 tiles of 128 x 128 (24 us) and not on 112 of 256 x 256 (34), and 512 rows
 //     of the 128 experts on 64 x 64 ones (40, 128 x 128 45, row kernel 44 to 47)
-hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s) {
-  // the tile kernels address A and a tile's weights by 32-bit byte offsets
-  const bool near = (int64_t)a.a_rows * (a.Kp / 2) < ((int64_t)1 << 32) && a.a_rows > 0;
-  if (a.M <= 16 || !near) {
-    const int64_t waves = ((int64_t)a.N + 15) / 16 * std::min(a.M, a.G);
-    if (waves <= 1024 && a.Kp >= 4096) return launch_rows<1, 4>(a, s);
-    return launch_rows<1, 1>(a, s);
+//   64 x 64 tiles that would leave half the machine idle over a long K share it (64
+//     x 4096 x 14336, 64 tiles: 35 us, in four parts 16; not yet at K = 4096, where
+//     the second launch takes more than the parts save: 9 against 12)
+Mx4GemmPlan mx4_gemm_plan(int M, int N, int Kp, int G) {
+  Mx4GemmPlan p{};
+  p.splits = 1;
+  if (M <= 16) {
+    const int64_t waves = ((int64_t)N + 15) / 16 * std::min(M, G);
+    p.kernel = waves <= 1024 && Kp >= 4096 ? Mx4GemmPlan::kRows4 : Mx4GemmPlan::kRows;
+    return p;
   }
-  const int64_t groups = std::min(a.M, a.G);
-  auto load = [&](int64_t b, double weight) {
-    const int64_t rows = a.G > 1 ? (a.M + groups * (b / 2)) / b : (a.M + b - 1) / b;
-    return (double)((rows * (((int64_t)a.N + b - 1) / b) + 255) / 256) * weight;
-  };
+  const int64_t groups = std::min(M, G);
+  auto tiles = [&](int64_t b) { return (G > 1 ? (M + groups * (b / 2)) / b : (M + b - 1) / b) * (((int64_t)N + b - 1) / b); };
+  auto load = [&](int64_t b, double weight) { return (double)((tiles(b) + 255) / 256) * weight; };
   const double w256 = load(256, 1.0), w128 = load(128, 0.3), w64 = load(64, 0.1);
-  if (w256 < w128 && w256 < w64) return launch_tile<256, 256>(a, s);
-  if (w128 <= w64) return launch_tile<128, 128>(a, s);
-  return launch_tile<64, 64>(a, s);
+  if (w256 < w128 && w256 < w64) {
+    p.kernel = Mx4GemmPlan::kTile256;
+  } else if (w128 <= w64) {
+    p.kernel = Mx4GemmPlan::kTile128;
+  } else {
+    p.kernel = Mx4GemmPlan::kTile64;
+    const int full = Kp / 256;
+    const int64_t s = std::min<int64_t>(256 / std::max<int64_t>(tiles(64), 1), full / 8);
+    if (s > 1 && full >= 24) {
+      p.split_steps = (int)((full + s - 1) / s + 1) & ~1;
+      p.splits = (full + p.split_steps - 1) / p.split_steps;
+    }
+  }
+  return p;
+}
+
+hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s) {
+  switch (a.plan.kernel) {
+    case Mx4GemmPlan::kRows4: return launch_rows<1, 4>(a, s);
+    case Mx4GemmPlan::kRows: return launch_rows<1, 1>(a, s);
+    case Mx4GemmPlan::kTile256: return launch_tile<256, 256>(a, s);
+    case Mx4GemmPlan::kTile128: return launch_tile<128, 128>(a, s);
+    default: return a.plan.splits > 1 ? launch_tile<64, 64, true>(a, s) : launch_tile<64, 64>(a, s);
+  }
+}
+
+hipError_t launch_mx4_gemm_sum(const Mx4GemmArgs& a, hipStream_t s) {
+  const int64_t n = ((int64_t)a.M * a.N + 1023) / 1024;
+  k_mx4_gemm_sum<<<(unsigned)std::min<int64_t>(n, 1 << 16), 256, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace lx

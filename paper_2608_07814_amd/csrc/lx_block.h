@@ -88,6 +88,13 @@ hipError_t launch_mx4_quantize(const Mx4Args& a, hipStream_t s);
 // x is the output of the reading back
 hipError_t launch_mx4_dequantize(const Mx4Args& a, hipStream_t s);
 
+// Which kernel a product runs on, and into how many parts its K is split (each
+// but the last of split_steps steps of 256 values).
+struct Mx4GemmPlan {
+  enum Kernel : int32_t { kRows, kRows4, kTile64, kTile128, kTile256 } kernel;
+  int32_t splits, split_steps;
+};
+Mx4GemmPlan mx4_gemm_plan(int M, int N, int Kp, int G);
 struct Mx4GemmArgs {
   const uint8_t *a, *as, *b, *bs;
   int32_t a_rows;
@@ -96,7 +103,10 @@ struct Mx4GemmArgs {
   int32_t G, M, N, Kp;
   uint8_t out_f32;
   void* out;
+  float* part;       // splits > 1: [splits][M][N]
+  Mx4GemmPlan plan;
 };
 hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s);
+hipError_t launch_mx4_gemm_sum(const Mx4GemmArgs& a, hipStream_t s);
 
 }  // namespace lx

@@ -205,6 +205,29 @@ def test_grouped_product(M, N, K, G, out):
     exact(o, ref)
 
 
+@pytest.mark.parametrize("M,N,K,G", [(20, 64, 8192, 1), (64, 130, 6280, 1), (33, 257, 8056, 1), (60, 100, 6408, 3), (90, 67, 12288, 2), (17, 1, 6144, 1)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_product_with_its_sum_in_parts(M, N, K, G, out):
+    """Few tiles and a long K: the parts of a sum go through the workspace. Rows of
+    no group stay as they are."""
+    require_gpu()
+    say(f"mx4_gemm in parts M={M} N={N} K={K} G={G} {out}")
+    assert lb.lib().lx_mx4_gemm_workspace_bytes(M, N, K, G) >= 2 * M * N * 4
+    off = None if G == 1 else ragged(M - 7, G, M) + 3
+    o, _, _, ref = run(M, N, K, G, offsets=off, out=out)
+    exact(o, ref)
+
+
+def test_workspace_refusals():
+    require_gpu()
+    a, b = dev(*operand((20,), 8192, 1), 8192), dev(*operand((1, 64), 8192, 2), 8192)
+    for ws, code in ((torch.empty(256, dtype=torch.uint8, device="cuda"), lx.LX_ERR_WORKSPACE_TOO_SMALL),
+                     (torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[128:], lx.LX_ERR_INVALID_ARGUMENT)):
+        with pytest.raises(lx.LorexError) as e:
+            lb.mx4_gemm(a, b, workspace=ws)
+        assert e.value.status == code
+
+
 def test_offsets_outside_the_rows_are_clamped():
     require_gpu()
     off = np.array([-3, 10, 25, 10 ** 6])
@@ -247,7 +270,7 @@ def test_nan_scale_spreads_along_its_row_and_column_only(M):
     assert torch.equal(o.isnan(), nan) and torch.equal(o[~nan], clean[~nan])
 
 
-@pytest.mark.parametrize("M,N,K,G", [(1, 2000, 2048, 1), (64, 256, 1024, 16), (600, 512, 512, 1), (2000, 512, 512, 6)])
+@pytest.mark.parametrize("M,N,K,G", [(1, 2000, 2048, 1), (64, 256, 1024, 16), (600, 512, 512, 1), (2000, 512, 512, 6), (50, 200, 8192, 1)])
 def test_same_bits_on_every_run_and_in_a_graph(M, N, K, G):
     require_gpu()
     off = None if G == 1 else torch.from_numpy(ragged(M, G, 2).astype(np.int32)).cuda()
