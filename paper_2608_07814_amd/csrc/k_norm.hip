@@ -245,8 +245,10 @@ __global__ __launch_bounds__(bwd_threads(BF)) void k_block_norm_grad(const NormG
     }
     const float gate = a.gate && live ? a.gate[t] : 1.f;
     row_sums<TPR>(s, lds);
-    const float rh = a.dx ? rms(s[0], a.d, a.eps) : 0.f;
-    const float ry = a.w_post ? rms(s[1], a.d, a.eps) : 1.f;
+    // (a row past T has zeros only, and with eps = 0 an infinite factor: 0 times
+    // it must not reach the sums over tokens)
+    const float rh = a.dx && live ? rms(s[0], a.d, a.eps) : 0.f;
+    const float ry = a.w_post && live ? rms(s[1], a.d, a.eps) : 1.f;
     const float mean = rh * s[2] * inv_d;
     float z[1] = {0.f};
 #pragma unroll

@@ -213,6 +213,14 @@ def test_backward_of_no_tokens_clears_weight_gradients():
     assert lb.block_norm(e("h"), e("y"), w_pre=p["w_pre"])[1].shape == (0, 64)
 
 
+@pytest.mark.parametrize("T,d,h", [(3, 64, "f32"), (5, 512, "bf16"), (3, 1000, "bf16"), (257, 2048, "f32")])
+def test_backward_with_eps_0(T, d, h):
+    """The rows that a workgroup has to spare add nothing to the weights' gradients,
+    also where their norm factor would be infinite."""
+    require_gpu()
+    check_backward(make(T, d, h, "bf16", "bf16"), eps=0.0)
+
+
 def test_backward_agrees_with_differences():
     """The gradients against differences of the library's own forward, fp32,
     loss = sum(a h_out) + sum(b x): central differences with step s of a smooth
