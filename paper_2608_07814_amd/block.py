@@ -435,11 +435,18 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
     E = experts.gate_up.codes.shape[0]
     f = experts.down.K
     _, x = block_norm(h, w_pre=w_pre, eps=eps)
-    ids, weights = lx.route_topk(x, w_r, k)
+    if T:
+        ids, weights = lx.route_topk(x, w_r, k)
+    else:  # nothing to route
+        ids, weights = h.new_empty((0, k), dtype=torch.int32), h.new_empty((0, k), dtype=torch.float32)
     logits = balance = None
     if balance_coef is not None:
         logits = x @ w_r.t()
         balance = balance_loss(logits, ids, mask=mask, coef=balance_coef)
+    if not T:
+        h_out, x_next = block_norm(h, h.new_empty((0, d), dtype=torch.float32), w_pre=w_next, w_post=w_post, scale=scale,
+                                   gate=gate, residual_scale=residual_scale, eps=eps)
+        return Mx4BlockOut(h_out, x_next, x, ids, weights, logits, balance)
     # rows of the experts: a tree without levels, whose weights bucketing does not read
     tree = lx.LxTreeLayer()
     tree.E, tree.d, tree.f, tree.dtype, tree.n_anchors = E, d, f, LX_BF16, E

@@ -71,6 +71,20 @@ def test_block_matches_oracle(T, E, d, f, k):
     assert abs(out.balance.loss.item() - loss) <= 1e-4 * loss
 
 
+def test_block_of_no_tokens():
+    require_gpu()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    r = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()  # noqa: E731
+    E, d, f, k = 8, 128, 64, 2
+    ex = lb.mx4_experts(r(E, f, d), r(E, f, d), r(E, d, f))
+    out = lb.mx4_moe_block(r(0, d), r(d), r(E, d), ex, k, w_next=r(d), balance_coef=1.0)
+    torch.cuda.synchronize()
+    assert out.h_out.shape == out.x_next.shape == out.x.shape == (0, d) and out.h_out.dtype == torch.bfloat16
+    assert out.topk_ids.shape == out.topk_weights.shape == (0, k) and out.logits.shape == (0, E)
+    assert out.balance.loss.item() == 0 and not out.balance.counts.any()
+
+
 def test_example_runs():
     require_gpu()
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
