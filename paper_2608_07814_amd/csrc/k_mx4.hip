@@ -328,7 +328,10 @@ __device__ __forceinline__ void land_and_meet() {
   asm volatile("" ::: "memory");
 }
 
-// BM x BN outputs per workgroup, a 2 x 2 grid of wavefronts, 32x32x64
+// BM x BN outputs per workgroup, a 2 x 2 grid of wavefronts (256 x 256: 2 x 4, two
+// wavefronts per SIMD: one multiplies while the other waits for LDS or the barrier,
+// and twice as many write results out; against 2 x 2 with twice the accumulators
+// 8192 x 8192 x 2048 takes 87 for 97 us, 8192^3 283 for 288), 32x32x64
 // instructions. Both operands go memory -> LDS directly in steps of 256 values
 // (128 bytes a row, a whole cache line: 64 bytes a row took twice as long per
 // byte), two steps in a ring, one streaming in while the other is multiplied.
@@ -337,26 +340,31 @@ __device__ __forceinline__ void land_and_meet() {
 // groups; a lane fetches the chunk that belongs at its LDS place. Scales come
 // in groups of two steps (16 bytes a row) through a ring of two. The weights
 // are the instruction's first operand: a lane ends with 4 consecutive columns
-// of one row, which go through LDS into whole rows. 8192^3: 297 us, 3.7 PFLOP/s,
-// where the instructions alone reach 6.5 from registers; without loads, LDS reads
-// and barriers these loops run at 5.5, and each adds its part: there is one
-// wavefront per SIMD to cover them, a second has no room for its accumulators.
+// of one row, which go through LDS into whole rows. 8192^3: 283 us, 3.9 PFLOP/s,
+// the matrix units busy for 48% of the cycles at a clock that has fallen to 1.9 GHz
+// (the instructions alone reach 6.5 from registers). Tried and slower: the two
+// wavefronts of a SIMD half a phase apart (8192^3 297), scales read 16 bytes at a
+// time without bank conflicts (301), the lines of the step after the next one
+// touched ahead (5 to 20% more).
 // SPLIT: an item is one of a.plan.splits parts of a tile's K (whole steps, an even
 // number in all but the last), and its results are an fp32 [M][N] of its own, which
 // a second launch adds up in order.
 // Workgroups stay for several items: the next item's place and rows are looked
 // up under the first loads of the present one, and its first loads are under way
 // while the present one's results are written.
+constexpr int tile_threads(int bm, int bn) { return bm * bn > 128 * 128 ? 512 : 256; }
 constexpr int tile_groups_per_cu(int bm, int bn) { return bm * bn > 128 * 128 ? 1 : bm * bn == 128 * 128 ? 2 : 4; }
 
 template <int BM, int BN, bool SPLIT>
-__global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_tile(const Mx4GemmArgs a) {
-  constexpr int WM = BM / 2, WN = BN / 2, MI = WM / 32, NI = WN / 32;
-  constexpr int RA = BM / 32, RB = BN / 32, R = RA + RB;  // 16-byte loads of a thread per step
+__global__ __launch_bounds__(tile_threads(BM, BN), tile_groups_per_cu(BM, BN) * tile_threads(BM, BN) / 256)
+void k_mx4_gemm_tile(const Mx4GemmArgs a) {
+  constexpr int THR = tile_threads(BM, BN), NW = THR / 64, WC = NW / 2;
+  constexpr int WM = BM / 2, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+  constexpr int RA = BM * 8 / THR, RB = BN * 8 / THR, R = RA + RB;  // 16-byte loads of a thread per step
   constexpr int STAGE = (BM + BN) * 128, SGRP = (BM + BN) * 16;
   constexpr int LDS = 2 * STAGE + 2 * SGRP + 16;  // (a half step reads a word past its scales)
   static_assert(LDS * tile_groups_per_cu(BM, BN) <= 160 * 1024, "");
-  static_assert(4 * 32 * WN * 4 <= STAGE, "32 rows of each wavefront's results fit in a stage");
+  static_assert(NW * 32 * WN * 4 <= STAGE, "32 rows of each wavefront's results fit in a stage");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
 
   const int ntn = (a.N + BN - 1) / BN;
@@ -366,7 +374,7 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int l32 = lane & 31, h = lane >> 5;
-  const int wm = wave >> 1, wn = wave & 1;
+  const int wm = wave / WC, wn = wave % WC;
   const int cp = a.Kp / 2, sp = a.Kp / 32, full = a.Kp / 256;
   const bool odd = a.Kp & 128;  // a last step of 128 values
 
@@ -376,12 +384,12 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     bool tail;                       // and then the half step
     uint64_t there[(WM + 63) / 64];  // which of this wavefront's rows have a row of A
     const uint8_t *B, *Bs;           // the tile's first weight row and its scales
-    uint32_t oa[RA], ob[RB];         // a thread's byte offsets from A (the host sees to it that they
-                                     // fit 32 bits) and from B
-    uint32_t qa, qb;                 // a thread's rows of the scale groups: one of A (threads below
-                                     // BM), one of B (threads below BN)
+    uint32_t oa[RA];                 // a thread's byte offsets from A (the host sees to it that they fit
+                                     // 32 bits)
+    uint32_t qs;                     // its row of the scale groups: of A (threads below BM) or of B (the
+                                     // last BN threads)
   };
-  static_assert(BM <= 256 && BN <= 256, "one row of each operand per thread");
+  static_assert(BM + BN <= THR, "one row of scales per thread");
   // A's row for tile row r, -1 if there is none (past the tile, or a map entry out
   // of range): its loads read A's first row (the host sees to it that there is
   // one), its results are dropped or 0
@@ -417,20 +425,26 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     q.Bs = a.bs + ((int64_t)g * a.N + q.n0) * sp;
 #pragma unroll
     for (int j = 0; j < RA; ++j) {
-      const int r = (j * 256 + tid) >> 3;
+      const int r = (j * THR + tid) >> 3;
       q.oa[j] = (uint32_t)max(row_of(q, r), 0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
     }
-#pragma unroll
-    for (int j = 0; j < RB; ++j) {
-      const int r = (j * 256 + tid) >> 3;
-      q.ob[j] = (uint32_t)min(r, a.N - 1 - q.n0) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
-    }
-    q.qa = (uint32_t)max(row_of(q, tid % BM), 0) * (uint32_t)sp;
-    q.qb = (uint32_t)min(tid % BN, a.N - 1 - q.n0) * (uint32_t)sp;
+    q.qs = (uint32_t)max(row_of(q, tid % BM), 0) * (uint32_t)sp;
 #pragma unroll
     for (int j = 0; j < (WM + 63) / 64; ++j) q.there[j] = __ballot(row_of(q, wm * WM + j * 64 + lane) >= 0);
   };
   Item cur;
+  // the offsets from B, formed when an item begins: they need no loads, and next
+  // to the present item's they would not fit in registers
+  uint32_t ob[RB];
+  auto from_b = [&]() __attribute__((always_inline)) {
+    const int last = a.N - 1 - cur.n0;
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+      const int r = (j * THR + tid) >> 3;
+      ob[j] = (uint32_t)min(r, last) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
+    }
+    if (wave >= NW - BN / 64) cur.qs = (uint32_t)min(tid % BN, last) * (uint32_t)sp;
+  };
   // Group q of the scales: words 4 q .. 4 q + 3 of every row, 16 bytes a row (a
   // memory address need only be aligned to words). A row's last group holds its
   // last four words, so a step finds its words `late` words further on.
@@ -440,14 +454,14 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     uint8_t* const st = smem + 2 * STAGE + (q & 1) * SGRP;
     if (words >= 4) {
       const int at = (q * 4 - late(q)) * 4;
-      if (wave < BM / 64) load_lds<16>(a.as + at, cur.qa, st + wave * 1024);
-      if (wave < BN / 64) load_lds<16>(cur.Bs + at, cur.qb, st + BM * 16 + wave * 1024);
+      if (wave < BM / 64) load_lds<16>(a.as + at, cur.qs, st + wave * 1024);
+      if (wave >= NW - BN / 64) load_lds<16>(cur.Bs + at, cur.qs, st + BM * 16 + (wave - (NW - BN / 64)) * 1024);
     } else {
       // rows of fewer words: word by word, 16 rows x 4 words per load, the last
       // one repeated
       const int word = min(lane & 3, words - 1) * 4;
 #pragma unroll 1
-      for (int r0 = wave * 16; r0 < BM + BN; r0 += 64) {
+      for (int r0 = wave * 16; r0 < BM + BN; r0 += NW * 16) {
         const int r = r0 + (lane >> 2);
         if (r0 < BM)
           load_lds<4>(a.as, (uint32_t)max(row_of(cur, r), 0) * (uint32_t)sp + word, st + r0 * 16);
@@ -462,11 +476,11 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     uint8_t* const st = smem + (t & 1) * STAGE;
     const int64_t at = (int64_t)t * 128;
     const int j = i < RA ? i : i - RA;
-    const uint32_t back = half ? ((tid ^ (((j * 256 + tid) >> 3) >> 1)) & 4) * 16 : 0;
+    const uint32_t back = half ? ((tid ^ (((j * THR + tid) >> 3) >> 1)) & 4) * 16 : 0;
     if (i < RA)
-      load_lds<16>(a.a + at, cur.oa[j] - back, st + (j * 4 + wave) * 1024);
+      load_lds<16>(a.a + at, cur.oa[j] - back, st + (j * NW + wave) * 1024);
     else
-      load_lds<16>(cur.B + at, cur.ob[j] - back, st + BM * 128 + (j * 4 + wave) * 1024);
+      load_lds<16>(cur.B + at, ob[j] - back, st + BM * 128 + (j * NW + wave) * 1024);
   };
   auto issue = [&](int t, bool half) __attribute__((always_inline)) {
     if ((t & 1) == 0) issue_scales(t >> 1);
@@ -505,10 +519,13 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
   // fragments of instruction s of step t, into set s % 2
   auto read = [&](int s, int t) __attribute__((always_inline)) {
     const int c = (t & 1) * STAGE + ((2 * s + h) ^ swz) * 16;
+    // (B's address from A's where a register less is what keeps the loop free of
+    // scratch; elsewhere its own is 1% faster)
+    const uint8_t *const pa = la + c, *const pb = THR == 512 ? pa + (BM + wn * WN - wm * WM) * 128 : lb + c;
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) fb[s & 1][ni] = *(const uint4*)(lb + ni * 4096 + c);
+    for (int ni = 0; ni < NI; ++ni) fb[s & 1][ni] = *(const uint4*)(pb + ni * 4096);
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) fa[s & 1][mi] = *(const uint4*)(la + mi * 4096 + c);
+    for (int mi = 0; mi < MI; ++mi) fa[s & 1][mi] = *(const uint4*)(pa + mi * 4096);
   };
   // The products of instruction s; from FIRST on, half of the loads of step t
   // between them: issued in one go they held up the products behind them. The
@@ -560,6 +577,7 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     land_and_meet();
   };
   look_up(it.at, cur);
+  from_b();
   issue(cur.t0, cur.t0 == full);
   for (;;) {
     it.at += it.step;
@@ -610,6 +628,7 @@ __global__ __launch_bounds__(256, tile_groups_per_cu(BM, BN)) void k_mx4_gemm_ti
     const bool out_f32 = SPLIT || a.out_f32;
     if (more) {
       cur = next;
+      from_b();
       issue(cur.t0, cur.t0 == full);
     }
 
@@ -725,7 +744,7 @@ static hipError_t launch_tile(const Mx4GemmArgs& a, hipStream_t s) {
   const int64_t tiles = a.offsets ? std::min<int64_t>((int64_t)a.M / BM + a.G, a.M) : ((int64_t)a.M + BM - 1) / BM;
   const int64_t items = tiles * (((int64_t)a.N + BN - 1) / BN) * (SPLIT ? a.plan.splits : 1);
   const int64_t most = 256 * tile_groups_per_cu(BM, BN);
-  k_mx4_gemm_tile<BM, BN, SPLIT><<<(unsigned)std::min((items + 7) / 8 * 8, most), 256, 0, s>>>(a);
+  k_mx4_gemm_tile<BM, BN, SPLIT><<<(unsigned)std::min((items + 7) / 8 * 8, most), tile_threads(BM, BN), 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -743,11 +762,14 @@ static hipError_t launch_rows(const Mx4GemmArgs& a, hipStream_t s) {
 //     and columns are few (4096 columns, K = 14336: 10.1 against 20.3 us alone;
 //     2048 x 2048: 8.4 against 7.1)
 //   else the tile that leaves the fullest compute unit the least work: a 256 x 256
-//     tile counts 1, one of 128 x 128 0.3 and one of 64 x 64 0.1, what they take
-//     next to each other on a full machine (4096^3, 1024 tiles of 128 x 128: 47
-//     against 41 us; 128 experts of 1536 x 2048, 32768 rows, 64 x 64 186 against
-//     144); a group's last tile is taken to be half full. So 512 x 14336 x 4096 runs
-//     on 448 tiles of 128 x 128 (24 us) and not on 112 of 256 x 256 (34), and 512 rows
+//     tile counts 0.88, one of 128 x 128 0.3 and one of 64 x 64 0.1, what they take
+//     next to each other on a full machine (4096^3, 1024 tiles of 128 x 128: 55
+//     against 46 us; 8192 rows of 16 experts of 4096 x 4096 126 against 117; 6144 x
+//     6144 x 4096 119 against 113; 128 experts of 1536 x 2048, 32768 rows, 64 x 64 186
+//     against 128 x 128 144); a group's last tile is taken to be half full, which
+//     errs where groups have a little less than a tile (24576 rows of the 128
+//     experts, 192 each: 256 x 256 111, 128 x 128 100). So 512 x 14336 x 4096 runs
+//     on 448 tiles of 128 x 128 (26 us) and not on 112 of 256 x 256 (35), and 512 rows
 //     of the 128 experts on 64 x 64 ones (40, 128 x 128 45, row kernel 44 to 47)
 //   64 x 64 tiles that would leave half the machine idle over a long K share it (64
 //     x 4096 x 14336, 64 tiles: 35 us, in four parts 16; not yet at K = 4096, where
@@ -763,7 +785,7 @@ Mx4GemmPlan mx4_gemm_plan(int M, int N, int Kp, int G) {
   const int64_t groups = std::min(M, G);
   auto tiles = [&](int64_t b) { return (G > 1 ? (M + groups * (b / 2)) / b : (M + b - 1) / b) * (((int64_t)N + b - 1) / b); };
   auto load = [&](int64_t b, double weight) { return (double)((tiles(b) + 255) / 256) * weight; };
-  const double w256 = load(256, 1.0), w128 = load(128, 0.3), w64 = load(64, 0.1);
+  const double w256 = load(256, 0.88), w128 = load(128, 0.3), w64 = load(64, 0.1);
   if (w256 < w128 && w256 < w64) {
     p.kernel = Mx4GemmPlan::kTile256;
   } else if (w128 <= w64) {

@@ -23,13 +23,13 @@ def _sizes(asm, what, name):
 def test_products_keep_everything_in_registers():
     """A tile's accumulators and fragments stay in registers, and as many
     workgroups as the tile's size plans for fit on a compute unit: 64 x 64 four
-    (at most 128 registers a lane of 512), 128 x 128 two (256)."""
+    (at most 128 registers a lane of 512), 128 x 128 two (256); one of 256 x 256
+    has two wavefronts per SIMD (256)."""
     asm = _asm("k_mx4.hip")
     scratch, vgpr, agpr = (_sizes(asm, w, "k_mx4_gemm") for w in ("private_seg_size", "num_vgpr", "num_agpr"))
     assert len(scratch) >= 6 and max(scratch.values()) == 0, scratch
     for n in vgpr:
-        # (the accumulators of 256 x 256 fill the second half of the register file)
-        most = 128 if "ILi64ELi64E" in n else 256 if "ILi128ELi128E" in n else 512
+        most = 128 if "ILi64ELi64E" in n else 256 if "gemm_tile" in n else 512
         assert vgpr[n] + agpr[n] <= most, (n, vgpr[n], agpr[n])
 
 
