@@ -6,7 +6,7 @@
 // row sums go over lanes by DPP, over wavefronts through LDS. Workgroups stay
 // for many rows, so the weight vectors are read once per workgroup. Measured:
 // forward 8192 x 4096 (fp32 output of the block, bf16 streams) 68 us, 4.9 TB/s;
-// backward 8192 x 4096 (fp32 stream) 130 us, 4.7 TB/s; a large copy reaches 5.45.
+// backward 8192 x 4096 (fp32 stream) 126 us, 4.8 TB/s; a large copy reaches 5.45.
 #include "lx_block.h"
 #include "lx_vec.h"
 
@@ -31,13 +31,11 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float* lds) {
       for (int i = 0; i < N; ++i) lds[wave * N + i] = x[i];
     }
     __syncthreads();
+    // each lane takes one wavefront's sum
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float t = 0.f;
+    for (int i = 0; i < N; ++i) x[i] = lds[(w0 + threadIdx.x % NW) * N + i];
 #pragma unroll
-      for (int w = 0; w < NW; ++w) t += lds[(w0 + w) * N + i];
-      x[i] = t;
-    }
+    for (int i = 0; i < N; ++i) x[i] = lane_sum<NW>(x[i]);
   }
 }
 
@@ -163,139 +161,165 @@ __global__ __launch_bounds__(kFwdThreads<TPR>) void k_block_norm(const NormArgs 
 }
 
 // Backward. With m = h' r_h, n = y r_y (no w_post: n = y, r_y = 1), D the
-// gradient of h':
+// gradient of h' and s = scale w_post:
 //   D    = dh' + r_h (dx w_pre - m mean(dx w_pre m))
-//   z    = sum_c D scale w_post n          (= dgate; gate z = sum_c dn n)
-//   dy   = r_y gate (D scale w_post - n z / d)     (no w_post: gate D scale)
-// so the row sums are {h'^2, y^2, dx w_pre h'} and then z. A workgroup takes
-// one row or several at a time and stays for all of its rows, one workgroup per
-// compute unit; loading the next rows ahead of the sums cost more in registers
-// than it hid (8192 x 4096 with fp32 streams 130 against 127 us, 1777 x 2048 in
-// bf16 20.6 against 14.2). The sums over tokens of dx m (dw_pre) and of gate D n
-// (dw_post = scale q, dscale = w_post q) stay in registers, are joined over the
-// workgroup's rows in LDS and left in part, one pair of vectors per workgroup.
-// Where all rows are bf16 (BF) a lane's values take half the registers and a
-// workgroup has 1024 lanes, else 512.
-constexpr int bwd_threads(bool bf) { return bf ? 1024 : 512; }
+//   z    = sum_c D s n                             (= dgate; gate z = sum_c dn n)
+//   dy   = r_y gate (D s - n z / d)                (no w_post: gate D s)
+// z is linear in D, so all sums are over what is stored, {h'^2, y^2, dx w_pre h',
+// dh' s y, dx w_pre s y, h' s y}, and are joined at once: one pass for the sums,
+// one for the results, one barrier per row (with z summed from D after the others
+// 8192 x 4096 with fp32 streams took 130 us for 126, 2048 x 8192 in bf16 55 for
+// 50). A workgroup takes one row or several at a time and stays for all of its
+// rows, one workgroup per compute unit; loading the next row ahead of the sums
+// gave 49 for 50 us at 2048 x 8192 and cost 22.6 for 20.3 at 5000 x 1024. The
+// sums over tokens of dx m (dw_pre) and of gate D n (dw_post = scale q, dscale =
+// w_post q) stay in registers, are joined over the workgroup's rows in LDS and
+// left in part, one pair of vectors per workgroup. KEEP: the row stays in
+// registers, as it is stored, between the passes (and the weights for all rows);
+// else (rows of more than 8192, which do not fit) both are read again, from L2
+// (1024 x 16384 in bf16 67 us, with the row kept and the weights read again 96).
+constexpr int kBwd = 1024;
+__device__ __forceinline__ void again(RawB8& r) { asm volatile("" : "+v"(r.a)); }
+__device__ __forceinline__ void again(Raw8& r) { asm volatile("" : "+v"(r.a), "+v"(r.b)); }
 
-template <bool BF, int TPR, int NV>
-__global__ __launch_bounds__(bwd_threads(BF)) void k_block_norm_grad(const NormGradArgs a) {
-  constexpr int kBwd = bwd_threads(BF), RPB = kBwd / TPR, NW = kBwd / 64;
+template <bool BF, int TPR, int NV, bool KEEP>
+__global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) {
+  constexpr int RPB = kBwd / TPR, NW = kBwd / 64;
   using Raw = std::conditional_t<BF, RawB8, Raw8>;
-  __shared__ float lds[4 * NW];
+  __shared__ float lds[2 * 6 * NW];
   __shared__ float join[RPB > 1 ? 2 * RPB * TPR * NV * 8 : 1];
-  const int lt = threadIdx.x % TPR, g = threadIdx.x / TPR;
-  int col[NV];
-  bool in[NV];
-  F8 sp[NV], sq[NV], sw[NV], wp[NV];
+  const int lt = threadIdx.x % TPR, g = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+  auto col = [&](int i) __attribute__((always_inline)) { return (i * TPR + lt) * 8; };
+  struct Weights {
+    F8 pre, s;
+  };
+  auto weights = [&](int i) __attribute__((always_inline)) {
+    Weights w;
+    w.pre = w.s = F8{{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}};
+    if (col(i) < a.d) {
+      if (a.w_pre) w.pre = load8(a.w_pre, a.w_f32, col(i));
+      if (a.w_post) w.s = load8(a.w_post, a.w_f32, col(i));
+      if (a.scale) {
+        const F8 q = load8(a.scale, a.w_f32, col(i));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w.s.v[e] *= q.v[e];
+      }
+    }
+    return w;
+  };
+  struct Row {
+    Raw m, y, D, dx;
+  };
+  auto load = [&](int i, int64_t t) __attribute__((always_inline)) {
+    Row r;
+    r.m = r.y = r.D = r.dx = Raw{};
+    if (col(i) < a.d && t < a.T) {
+      const int64_t at = t * a.d + col(i);
+      r.m = load_as<Raw>(a.h_out, a.h_f32, at);
+      if (a.dx) r.dx = load_as<Raw>(a.dx, a.x_f32, at);
+      if (a.dh_out) r.D = load_as<Raw>(a.dh_out, a.h_f32, at);
+      if (a.y) r.y = load_as<Raw>(a.y, a.y_f32, at);
+    }
+    return r;
+  };
+  F8 sp[NV], sq[NV];
+  Weights w[KEEP ? NV : 1];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    col[i] = (i * TPR + lt) * 8;
-    in[i] = col[i] < a.d;
     sp[i] = sq[i] = F8{};
-    sw[i] = wp[i] = F8{{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}};
-    if (in[i]) {
-      if (a.w_pre) wp[i] = load8(a.w_pre, a.w_f32, col[i]);
-      if (a.w_post) sw[i] = load8(a.w_post, a.w_f32, col[i]);
-      if (a.scale) {
-        const F8 q = load8(a.scale, a.w_f32, col[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sw[i].v[e] *= q.v[e];
-      }
-    }
+    if constexpr (KEEP) w[i] = weights(i);
   }
-  struct Row {
-    Raw m[NV], y[NV], D[NV], dx[NV];
-  };
-  auto load = [&](Row& r, int64_t t) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      r.m[i] = r.y[i] = r.D[i] = r.dx[i] = Raw{};
-      if (in[i] && t < a.T) {
-        const int64_t at = t * a.d + col[i];
-        r.m[i] = load_as<Raw>(a.h_out, a.h_f32, at);
-        if (a.dx) r.dx[i] = load_as<Raw>(a.dx, a.x_f32, at);
-        if (a.dh_out) r.D[i] = load_as<Raw>(a.dh_out, a.h_f32, at);
-        if (a.y) r.y[i] = load_as<Raw>(a.y, a.y_f32, at);
-      }
-    }
-  };
   const float inv_d = 1.f / (float)a.d, alpha = a.y ? a.alpha : 1.f;
   const int64_t stride = (int64_t)a.groups * RPB;
+  int slots = 0;  // the sums' LDS slots of this row: the previous row's may still be read
   // (all rows of the workgroup run as many rounds: the barriers need them)
-  for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < a.T; t0 += stride) {
+  for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < a.T; t0 += stride, slots ^= 6 * NW) {
     const int64_t t = t0 + g, row = t * a.d;
     const bool live = t < a.T;
-    F8 m[NV], y[NV], D[NV], dx[NV];
-    float s[3] = {0.f, 0.f, 0.f};
-    Row q;
-    load(q, t);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      m[i] = unpack8(q.m[i], a.h_f32);
-      y[i] = unpack8(q.y[i], a.y_f32);
-      D[i] = unpack8(q.D[i], a.h_f32);
-      dx[i] = unpack8(q.dx[i], a.x_f32);
+    float s[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    auto add = [&](const Row& q, const Weights& w) __attribute__((always_inline)) {
+      const F8 m = unpack8(q.m, a.h_f32), y = unpack8(q.y, a.y_f32), D = unpack8(q.D, a.h_f32), dx = unpack8(q.dx, a.x_f32);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        s[0] += m[i].v[e] * m[i].v[e];
-        s[1] += y[i].v[e] * y[i].v[e];
-        s[2] += dx[i].v[e] * wp[i].v[e] * m[i].v[e];
+        const float dm = dx.v[e] * w.pre.v[e], sy = w.s.v[e] * y.v[e];
+        s[0] += m.v[e] * m.v[e];
+        s[1] += y.v[e] * y.v[e];
+        s[2] += dm * m.v[e];
+        s[3] += D.v[e] * sy;
+        s[4] += dm * sy;
+        s[5] += m.v[e] * sy;
       }
+    };
+    Row q[KEEP ? NV : 1];
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) q[i] = load(i, t);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) add(q[i], w[i]);
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < NV; ++i) add(load(i, t), weights(i));
     }
     const float gate = a.gate && live ? a.gate[t] : 1.f;
-    row_sums<TPR>(s, lds);
+    row_sums<TPR>(s, lds + slots);
     // (a row past T has zeros only, and with eps = 0 an infinite factor: 0 times
     // it must not reach the sums over tokens)
     const float rh = a.dx && live ? rms(s[0], a.d, a.eps) : 0.f;
     const float ry = a.w_post && live ? rms(s[1], a.d, a.eps) : 1.f;
     const float mean = rh * s[2] * inv_d;
-    float z[1] = {0.f};
+    const float z = ry * (a.dx ? s[3] + rh * (s[4] - rh * mean * s[5]) : s[3]);
+    const float zn = a.w_post ? z * inv_d : 0.f;
+    if (a.dgate && lt == 0 && live) a.dgate[t] = z;
+    // (the row is unpacked anew: next to its stored form it would not fit)
+    if constexpr (KEEP) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      F8 o;
+      for (int i = 0; i < NV; ++i) {
+        again(q[i].m);
+        again(q[i].y);
+        again(q[i].D);
+        again(q[i].dx);
+      }
+    }
+    auto give = [&](int i, const Row& q, const Weights& w) __attribute__((always_inline)) {
+      const F8 m = unpack8(q.m, a.h_f32), y = unpack8(q.y, a.y_f32), D = unpack8(q.D, a.h_f32), dx = unpack8(q.dx, a.x_f32);
+      F8 dh, dy;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float mm = m[i].v[e] * rh;
-        D[i].v[e] += rh * (dx[i].v[e] * wp[i].v[e] - mm * mean);
-        sp[i].v[e] += dx[i].v[e] * mm;
-        o.v[e] = alpha * D[i].v[e];
-        y[i].v[e] *= ry;
-        sq[i].v[e] += gate * D[i].v[e] * y[i].v[e];
-        D[i].v[e] *= sw[i].v[e];
-        z[0] += D[i].v[e] * y[i].v[e];
+        const float mm = m.v[e] * rh, n = y.v[e] * ry, d = D.v[e] + rh * (dx.v[e] * w.pre.v[e] - mm * mean);
+        sp[i].v[e] += dx.v[e] * mm;
+        sq[i].v[e] += gate * d * n;
+        dh.v[e] = alpha * d;
+        dy.v[e] = ry * gate * (d * w.s.v[e] - n * zn);
       }
-      if (in[i] && live) store8(a.dh, a.h_f32, row + col[i], o);
-    }
-    if (!a.y) {
-      if constexpr (TPR > 64) __syncthreads();  // (the sums' slots are free again)
-      continue;
-    }
-    row_sums<TPR>(z, lds + 3 * NW);
-    if (a.dgate && lt == 0 && live) a.dgate[t] = z[0];
-    const float zn = a.w_post ? z[0] * inv_d : 0.f;
+      if (col(i) < a.d && live) {
+        store8(a.dh, a.h_f32, row + col(i), dh);
+        if (a.y) store8(a.dy, a.y_f32, row + col(i), dy);
+      }
+    };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      F8 o;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o.v[e] = ry * gate * (D[i].v[e] - y[i].v[e] * zn);
-      if (in[i] && live) store8(a.dy, a.y_f32, row + col[i], o);
+      if constexpr (KEEP) {
+        give(i, q[i], w[i]);
+      } else {
+        asm volatile("" ::: "memory");  // (one group's loads at a time)
+        give(i, load(i, t), weights(i));
+      }
     }
   }
   float* const p = a.part + (int64_t)blockIdx.x * 2 * a.d;
   if constexpr (RPB == 1) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      if (in[i]) {
-        store8(p, true, col[i], sp[i]);
-        store8(p + a.d, true, col[i], sq[i]);
+      if (col(i) < a.d) {
+        store8(p, true, col(i), sp[i]);
+        store8(p + a.d, true, col(i), sq[i]);
       }
   } else {
     constexpr int W = TPR * NV * 8;  // columns of a row's lanes
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      store8(join + g * 2 * W, true, col[i], sp[i]);
-      store8(join + g * 2 * W + W, true, col[i], sq[i]);
+      store8(join + g * 2 * W, true, col(i), sp[i]);
+      store8(join + g * 2 * W + W, true, col(i), sq[i]);
     }
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * W; c += kBwd) {
@@ -336,8 +360,8 @@ __global__ __launch_bounds__(1024) void k_block_norm_grad_sum(const NormGradArgs
 }
 
 // Lanes of a row and groups of 8 columns per lane: a row's lanes hold one group
-// each as long as MOST lanes do.
-template <int MOST, class F>
+// each as long as 1024 lanes do.
+template <class F>
 hipError_t by_width(int d, F&& f) {
   using std::integral_constant;
 #define LX_W(T, N) f(integral_constant<int, T>{}, integral_constant<int, N>{})
@@ -345,16 +369,16 @@ hipError_t by_width(int d, F&& f) {
   if (d <= 1024) return LX_W(128, 1);
   if (d <= 2048) return LX_W(256, 1);
   if (d <= 4096) return LX_W(512, 1);
-  if (d <= 8192) return LX_W(MOST, 8192 / 8 / MOST);
-  if (d <= 16384) return LX_W(MOST, 16384 / 8 / MOST);
-  return LX_W(MOST, 32768 / 8 / MOST);
+  if (d <= 8192) return LX_W(1024, 1);
+  if (d <= 16384) return LX_W(1024, 2);
+  return LX_W(1024, 4);
 #undef LX_W
 }
 
 }  // namespace
 
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t s) {
-  return by_width<1024>(a.d, [&](auto tpr, auto nv) {
+  return by_width(a.d, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, THR = kFwdThreads<TPR>;
     constexpr int RPB = THR / TPR;
     const int grid = (int)std::min<int64_t>(((int64_t)a.T + RPB - 1) / RPB, 256 * (2048 / THR));
@@ -363,25 +387,23 @@ hipError_t launch_block_norm(const NormArgs& a, hipStream_t s) {
   });
 }
 
-// (as many for both kinds of rows: the kind's own number of rows at once only
-// moves rows between workgroups)
 int norm_grad_groups(int T, int d) {
   int at_once = 1;
-  (void)by_width<512>(d, [&](auto tpr, auto) {
-    at_once = 512 / decltype(tpr)::value;
+  (void)by_width(d, [&](auto tpr, auto) {
+    at_once = kBwd / decltype(tpr)::value;
     return hipSuccess;
   });
   return (int)std::min<int64_t>(std::max<int64_t>(((int64_t)T + at_once - 1) / at_once, 1), 256);
 }
 
 hipError_t launch_block_norm_grad(const NormGradArgs& a, hipStream_t s) {
-  if (!a.h_f32 && (!a.y || !a.y_f32) && (!a.dx || !a.x_f32))
-    return by_width<1024>(a.d, [&](auto tpr, auto nv) {
-      k_block_norm_grad<true, decltype(tpr)::value, decltype(nv)::value><<<a.groups, 1024, 0, s>>>(a);
-      return hipGetLastError();
-    });
-  return by_width<512>(a.d, [&](auto tpr, auto nv) {
-    k_block_norm_grad<false, decltype(tpr)::value, decltype(nv)::value><<<a.groups, 512, 0, s>>>(a);
+  const bool bf = !a.h_f32 && (!a.y || !a.y_f32) && (!a.dx || !a.x_f32);
+  return by_width(a.d, [&](auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
+    if (bf)
+      k_block_norm_grad<true, TPR, NV, NV == 1><<<a.groups, kBwd, 0, s>>>(a);
+    else
+      k_block_norm_grad<false, TPR, NV, NV == 1><<<a.groups, kBwd, 0, s>>>(a);
     return hipGetLastError();
   });
 }
