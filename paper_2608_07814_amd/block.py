@@ -131,6 +131,8 @@ def _workspace(given: Optional[torch.Tensor], need: int, like: torch.Tensor, str
         if not need:
             return None, None, 0
         given = _empty((need,), torch.uint8, like, stream)
+    elif given.dtype != torch.uint8 or not given.is_contiguous() or given.get_device() != like.get_device():
+        raise ValueError(f"workspace must be contiguous uint8 on {like.device}")
     return given, given.data_ptr(), given.numel()
 
 
@@ -434,6 +436,10 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
     T, d = h.shape
     E = experts.gate_up.codes.shape[0]
     f = experts.down.K
+    if w_r.shape != (E, d) or experts.down.codes.shape[:2] != (E, d) or experts.gate_up.codes.shape[1] != 2 * f:
+        raise ValueError("w_r must be [E][d], the experts [E][2f][d] and [E][d][f] for h [T][d]")
+    if w_r.get_device() != _gpu("h", h):
+        raise ValueError(f"w_r is on {w_r.device}, h on {h.device}")
     _, x = block_norm(h, w_pre=w_pre, eps=eps)
     if T:
         ids, weights = lx.route_topk(x, w_r, k)

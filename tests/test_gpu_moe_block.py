@@ -85,6 +85,42 @@ def test_block_of_no_tokens():
     assert out.balance.loss.item() == 0 and not out.balance.counts.any()
 
 
+def test_block_refuses_what_does_not_fit():
+    require_gpu()
+    r = lambda *s: torch.randn(*s, device="cuda").bfloat16()  # noqa: E731
+    E, d, f = 8, 128, 64
+    ex = lb.mx4_experts(r(E, f, d), r(E, f, d), r(E, d, f))
+    other = lb.mx4_experts(r(E, f, d), r(E, f, d), r(4, d, f))
+    for h, w_r, e in ((r(3, d), r(E + 4, d), ex), (r(3, d), r(E, 2 * d), ex), (r(3, 2 * d), r(E, 2 * d), ex),
+                      (r(3, d), r(E, d).cpu(), ex), (r(3, d), r(E, d), lb.Mx4Experts(ex.gate_up, other.down)),
+                      (r(3, d), r(E, d), lb.Mx4Experts(ex.down, ex.down))):
+        with pytest.raises(ValueError):
+            lb.mx4_moe_block(h, r(d), w_r, e, 2)
+
+
+def test_given_workspaces():
+    """A workspace that is not plain bytes on the call's GPU is refused; one that is
+    large enough is used."""
+    require_gpu()
+    T, E, k, d = 3000, 64, 2, 256
+    lg = torch.randn(T, E, device="cuda")
+    ids = torch.topk(lg, k, dim=1).indices.int()
+    need = lb.lib().lx_balance_loss_workspace_bytes(T, E)
+    assert need > 0
+    ref = lb.balance_loss(lg, ids)
+    got = lb.balance_loss(lg, ids, workspace=torch.empty(need, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(got.loss, ref.loss) and torch.equal(got.counts, ref.counts)
+    h = torch.randn(T, d, device="cuda")
+    big = lb.lib().lx_block_norm_backward_workspace_bytes(T, d)
+    for n, call in ((need, lambda w: lb.balance_loss(lg, ids, workspace=w)),
+                    (big, lambda w: lb.block_norm_backward(h, None, h, w_pre=h[0], workspace=w))):
+        for w in (torch.empty(n, dtype=torch.uint8), torch.empty(n, dtype=torch.float32, device="cuda"),
+                  torch.empty(1, dtype=torch.uint8, device="cuda").expand(n),
+                  torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2]):
+            with pytest.raises(ValueError):
+                call(w)
+
+
 def test_example_runs():
     require_gpu()
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
