@@ -341,7 +341,7 @@ __device__ __forceinline__ void land_and_meet() {
 // in groups of two steps (16 bytes a row) through a ring of two. The weights
 // are the instruction's first operand: a lane ends with 4 consecutive columns
 // of one row, which go through LDS into whole rows. 8192^3: 283 us, 3.9 PFLOP/s,
-// the matrix units busy for 48% of the cycles at a clock that has fallen to 1.9 GHz
+// the matrix units busy for 48% of the cycles at a clock that has fallen below 2 GHz
 // (the instructions alone reach 6.5 from registers). Tried and slower: the two
 // wavefronts of a SIMD half a phase apart (8192^3 297), scales read 16 bytes at a
 // time without bank conflicts (301), the lines of the step after the next one
