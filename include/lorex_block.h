@@ -13,7 +13,8 @@
  * The conventions of lorex.h hold: device pointers to dense row-major
  * caller-owned memory, asynchronous on `stream`, nothing allocated, no
  * pointer kept, argument errors returned before anything is enqueued
- * (lx_last_error), workspaces that need no initialisation. Every call may be
+ * (lx_last_error), workspaces that need no initialisation. Memory and `stream`
+ * belong to the GPU that is current at the call. Every call may be
  * captured into a HIP graph. Results do not change from run to run: no sum
  * depends on the order in which workgroups run.
  */

@@ -10,13 +10,16 @@
 * :class:`Mx4Experts`, :func:`mx4_moe_block`: a MoE block whose experts are held
   in 4 bits, built from these and the library's router and bucketing.
 
-Tensors are contiguous and on one GPU. Calls are asynchronous on ``stream`` (a
-``torch.cuda.Stream``; default: the current one). Outputs can be given; those
-that are not are allocated, as are workspaces.
+Tensors are contiguous and on one GPU, which need not be the current one. Calls
+are asynchronous on ``stream`` (a ``torch.cuda.Stream`` of that GPU; default: its
+current one). Outputs can be given; those that are not are allocated, as are
+workspaces.
 """
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 from typing import NamedTuple, Optional
 
 import torch
@@ -117,6 +120,39 @@ def _handle(stream, gpu: int) -> int:
     return _current_raw_stream(gpu) if stream is None else stream.cuda_stream
 
 
+_current_device = torch._C._cuda_getDevice
+
+
+def _on_its_gpu(fn):
+    """Runs ``fn`` with the GPU of its first argument (a tensor or Mx4) as the
+    current one: the library launches there, and the default stream's handle is
+    the same on every GPU."""
+    name = next(iter(inspect.signature(fn).parameters))
+
+    @functools.wraps(fn)
+    def call(*args, **kw):
+        first = args[0] if args else kw[name]
+        gpu = (first.codes if isinstance(first, Mx4) else first).get_device()
+        if gpu >= 0:  # (else refused by fn)
+            stream = kw.get("stream")
+            if stream is not None and stream.device_index != gpu:
+                raise ValueError(f"stream is on cuda:{stream.device_index}, {name} on cuda:{gpu}")
+            if gpu != _current_device():
+                with torch.cuda.device(gpu):
+                    return fn(*args, **kw)
+        return fn(*args, **kw)
+
+    return call
+
+
+class Mx4(NamedTuple):
+    """4-bit values: codes uint8 [..., Kp / 2], scales uint8 [..., Kp / 32], and
+    the K values of a row."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    K: int
+
+
 def _empty(shape, dtype, like: torch.Tensor, stream) -> torch.Tensor:
     """A new tensor that stays reserved until the call's stream is done with it."""
     t = like.new_empty(shape, dtype=dtype)
@@ -146,6 +182,7 @@ def _norm_layer(h, y, x_dtype, w_pre, w_post, scale, gate, residual_scale, eps, 
                        _arg("scale", scale, (d,), wt, gpu), _arg("gate", gate, (T,), torch.float32, gpu))
 
 
+@_on_its_gpu
 def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Optional[torch.Tensor] = None,
                w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                gate: Optional[torch.Tensor] = None, slot_row: Optional[torch.Tensor] = None,
@@ -203,6 +240,7 @@ class BlockNormGrads(NamedTuple):
     dscale: Optional[torch.Tensor]
 
 
+@_on_its_gpu
 def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Optional[torch.Tensor],
                         dh_out: Optional[torch.Tensor] = None, *, w_pre: Optional[torch.Tensor] = None,
                         w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
@@ -257,6 +295,7 @@ def _mask_arg(mask, T, gpu):
     return _arg("mask", mask, (T,), torch.uint8, gpu)
 
 
+@_on_its_gpu
 def balance_loss(logits: torch.Tensor, topk_ids: torch.Tensor, *, mask: Optional[torch.Tensor] = None,
                  coef: float = 1.0, workspace: Optional[torch.Tensor] = None, stream=None) -> BalanceLoss:
     """The balance loss of router logits [T][E] (fp32 or bf16) and the chosen
@@ -280,6 +319,7 @@ def balance_loss(logits: torch.Tensor, topk_ids: torch.Tensor, *, mask: Optional
     return r
 
 
+@_on_its_gpu
 def balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_tokens: torch.Tensor, k: int, *,
                           mask: Optional[torch.Tensor] = None, coef: float = 1.0,
                           dloss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
@@ -311,14 +351,7 @@ def mx4_padded(K: int) -> int:
     return -(-K // 128) * 128
 
 
-class Mx4(NamedTuple):
-    """4-bit values: codes uint8 [..., Kp / 2], scales uint8 [..., Kp / 32], and
-    the K values of a row."""
-    codes: torch.Tensor
-    scales: torch.Tensor
-    K: int
-
-
+@_on_its_gpu
 def mx4_quantize(x: torch.Tensor, *, act: int = MX4_NONE, out: Optional[Mx4] = None, stream=None) -> Mx4:
     """x [..., K] fp32 or bf16 -> 4-bit values (lx_mx4_quantize). With
     ``act=MX4_SWIGLU`` x is [..., 2K], the gate and up projections of a SwiGLU
@@ -345,6 +378,7 @@ def mx4_quantize(x: torch.Tensor, *, act: int = MX4_NONE, out: Optional[Mx4] = N
     return out
 
 
+@_on_its_gpu
 def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, *, out: Optional[torch.Tensor] = None,
                    stream=None) -> torch.Tensor:
     """The values [..., K] of 4-bit codes (lx_mx4_dequantize), exact in both types."""
@@ -362,6 +396,7 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, *, out: Optional
     return out
 
 
+@_on_its_gpu
 def mx4_gemm(a: Mx4, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map: Optional[torch.Tensor] = None,
              out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
              workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -421,6 +456,7 @@ class Mx4BlockOut(NamedTuple):
     balance: Optional[BalanceLoss]
 
 
+@_on_its_gpu
 def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, experts: Mx4Experts, k: int, *,
                   w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                   gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0, eps: float = 1e-6,

@@ -1,0 +1,165 @@
+"""On which GPU, in which streams and from which memory the bindings around the
+expert layer issue their work, on the CPU: tensors, streams and the library are
+stand-ins that record what happens."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2608_07814_amd import block as lb
+from paper_2608_07814_amd import lorex as lx
+
+
+class Stream:
+    def __init__(self, gpu, handle):
+        self.device_index, self.cuda_stream = gpu, handle
+
+
+class Tensor:
+    """`pool` is the stream whose memory it is in, `ready` the one whose work
+    fills it, `recorded` the streams whose work its release waits for."""
+
+    def __init__(self, world, shape, dtype, gpu, pool=None):
+        self.world, self.shape, self.dtype, self.gpu = world, torch.Size(shape), dtype, gpu
+        self.pool, self.ready, self.recorded = pool, pool, []
+
+    device = property(lambda self: f"cuda:{self.gpu}")
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def get_device(self):
+        return self.gpu
+
+    def is_contiguous(self):
+        return True
+
+    def contiguous(self):
+        return self
+
+    def data_ptr(self):
+        self.world.tensors[id(self)] = self
+        return id(self) * 256
+
+    def record_stream(self, stream):
+        self.recorded.append(stream)
+
+    def new_empty(self, shape, dtype=None):
+        shape = (shape,) if isinstance(shape, int) else shape
+        t = Tensor(self.world, shape, dtype or self.dtype, self.gpu, self.world.stream(self.gpu))
+        self.world.made.append(t)
+        return t
+
+    def unbind(self, dim):
+        rows = [Tensor(self.world, self.shape[1:], self.dtype, self.gpu, self.pool) for _ in range(self.shape[0])]
+        for r in rows:
+            r.recorded = self.recorded  # one allocation
+        return rows
+
+
+class World:
+    """Two GPUs, each with its default stream (handle 0) and others."""
+
+    def __init__(self):
+        self.device, self.current = 0, [Stream(0, 0), Stream(1, 0)]
+        self.tensors, self.made, self.calls = {}, [], []
+
+    def stream(self, gpu=None):
+        return self.current[self.device if gpu is None else gpu]
+
+    @contextlib.contextmanager
+    def on_device(self, gpu):
+        before, self.device = self.device, gpu
+        yield
+        self.device = before
+
+    @contextlib.contextmanager
+    def on_stream(self, stream):
+        with self.on_device(stream.device_index):
+            before, self.current[stream.device_index] = self.current[stream.device_index], stream
+            yield
+            self.current[stream.device_index] = before
+
+    def __getattr__(self, name):  # the library
+        if not name.startswith("lx_"):
+            raise AttributeError(name)
+        if name.endswith("_bytes"):
+            return lambda *a: 4096
+
+        def call(*a):
+            handle = a[-1] or 0
+            # a handle of 0 is the default stream of the current GPU
+            self.calls.append((name, self.device, handle, [self.tensors[p // 256] for p in a if isinstance(p, int) and p // 256 in self.tensors]))
+            return 0
+        return call
+
+
+@pytest.fixture
+def world(monkeypatch):
+    w = World()
+    monkeypatch.setattr(lb, "lib", lambda: w)
+    monkeypatch.setattr(lx, "lib", lambda: w)
+    monkeypatch.setattr(torch.cuda, "device", w.on_device)
+    monkeypatch.setattr(torch.cuda, "stream", w.on_stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", w.stream)
+    monkeypatch.setattr(lb, "_current_raw_stream", lambda gpu: w.stream(gpu).cuda_stream)
+    monkeypatch.setattr(lb, "_current_device", lambda: w.device, raising=False)
+    return w
+
+
+F32, BF16, I32, U8 = torch.float32, torch.bfloat16, torch.int32, torch.uint8
+
+
+def calls(world, gpu):
+    """Every entry that takes a stream, on tensors of one GPU."""
+    t = lambda dtype, *shape: Tensor(world, shape, dtype, gpu)  # noqa: E731
+    h, y, w = t(BF16, 4, 64), t(F32, 4, 64), t(BF16, 64)
+    a, b = lb.Mx4(t(U8, 4, 64), t(U8, 4, 4), 128), lb.Mx4(t(U8, 8, 64), t(U8, 8, 4), 128)
+    return {
+        "block_norm": lambda **kw: lb.block_norm(h, y, w_pre=w, w_post=w, **kw),
+        "block_norm by names": lambda **kw: lb.block_norm(h=h, w_pre=w, **kw),
+        "block_norm_backward": lambda **kw: lb.block_norm_backward(h, y, h, h, w_pre=w, w_post=w, gate=t(F32, 4), **kw),
+        "balance_loss": lambda **kw: lb.balance_loss(h, t(I32, 4, 2), **kw),
+        "balance_loss_backward": lambda **kw: lb.balance_loss_backward(h, t(I32, 64), t(I32, 1), 2, **kw),
+        "mx4_quantize": lambda **kw: lb.mx4_quantize(h, **kw),
+        "mx4_dequantize": lambda **kw: lb.mx4_dequantize(a, **kw),
+        "mx4_gemm": lambda **kw: lb.mx4_gemm(a, b, **kw),
+    }
+
+
+ENTRIES = sorted(calls(None, 0))
+
+
+@pytest.mark.parametrize("entry", ENTRIES)
+def test_the_tensors_gpu_is_current_during_the_launch(world, entry):
+    """A launch on stream 0, and any without a stream, goes to the current GPU."""
+    calls(world, 1)[entry]()
+    ((_, device, handle, _),) = world.calls
+    assert (device, handle) == (1, 0) and world.device == 0
+    side = Stream(1, 77)
+    calls(world, 1)[entry](stream=side)
+    assert world.calls[1][1:3] == (1, 77) and world.device == 0 and world.current[1].cuda_stream == 0
+    with world.on_device(1):
+        calls(world, 0)[entry]()
+    assert world.calls[2][1:3] == (0, 0)
+
+
+@pytest.mark.parametrize("entry", ENTRIES)
+def test_a_stream_of_another_gpu_is_refused(world, entry):
+    with pytest.raises(ValueError):
+        calls(world, 0)[entry](stream=Stream(1, 77))
+    assert not world.calls
+
+
+def test_moe_block_runs_on_its_gpu(world):
+    t = lambda dtype, *shape: Tensor(world, shape, dtype, 1)  # noqa: E731
+    E, d, f, k = 8, 128, 128, 2
+    ex = lb.Mx4Experts(lb.Mx4(t(U8, E, 2 * f, 64), t(U8, E, 2 * f, 4), d), lb.Mx4(t(U8, E, d, 64), t(U8, E, d, 4), f))
+    with pytest.MonkeyPatch.context() as m:
+        m.setattr(lx, "route_topk", lambda x, w_r, k, **kw: (x.new_empty((4, k), dtype=I32), x.new_empty((4, k), dtype=F32)))
+        out = lb.mx4_moe_block(t(BF16, 4, d), t(BF16, d), t(BF16, E, d), ex, k)
+    assert len(world.calls) == 7 and {c[1] for c in world.calls} == {1} and world.device == 0
+    assert out.h_out.gpu == 1
