@@ -13,7 +13,9 @@
 Tensors are contiguous and on one GPU, which need not be the current one. Calls
 are asynchronous on ``stream`` (a ``torch.cuda.Stream`` of that GPU; default: its
 current one). Outputs can be given; those that are not are allocated, as are
-workspaces.
+workspaces, in the order of the call's stream: with ``stream`` the caller has
+that stream wait for inputs that another one makes, and its own stream wait for
+that one before it uses the outputs.
 """
 from __future__ import annotations
 
@@ -125,8 +127,10 @@ _current_device = torch._C._cuda_getDevice
 
 def _on_its_gpu(fn):
     """Runs ``fn`` with the GPU of its first argument (a tensor or Mx4) as the
-    current one: the library launches there, and the default stream's handle is
-    the same on every GPU."""
+    current one, where the library launches (the default stream's handle is the
+    same on every GPU), and with the call's stream as the current one, so that what
+    the call allocates is memory of that stream's order: memory of another
+    stream's pool may still be in use by that stream's pending work."""
     name = next(iter(inspect.signature(fn).parameters))
 
     @functools.wraps(fn)
@@ -135,14 +139,30 @@ def _on_its_gpu(fn):
         gpu = (first.codes if isinstance(first, Mx4) else first).get_device()
         if gpu >= 0:  # (else refused by fn)
             stream = kw.get("stream")
-            if stream is not None and stream.device_index != gpu:
-                raise ValueError(f"stream is on cuda:{stream.device_index}, {name} on cuda:{gpu}")
+            if stream is not None:
+                if stream.device_index != gpu:
+                    raise ValueError(f"stream is on cuda:{stream.device_index}, {name} on cuda:{gpu}")
+                caller = torch.cuda.current_stream(gpu)
+                with torch.cuda.stream(stream):
+                    out = fn(*args, **kw)
+                _record(out, caller)
+                return out
             if gpu != _current_device():
                 with torch.cuda.device(gpu):
                     return fn(*args, **kw)
         return fn(*args, **kw)
 
     return call
+
+
+def _record(out, stream):
+    """The memory of ``out``'s tensors, once they are freed, is not reused before
+    ``stream`` has done the work that it has by then."""
+    if isinstance(out, tuple):
+        for v in out:
+            _record(v, stream)
+    elif hasattr(out, "record_stream"):
+        out.record_stream(stream)
 
 
 class Mx4(NamedTuple):
@@ -153,20 +173,12 @@ class Mx4(NamedTuple):
     K: int
 
 
-def _empty(shape, dtype, like: torch.Tensor, stream) -> torch.Tensor:
-    """A new tensor that stays reserved until the call's stream is done with it."""
-    t = like.new_empty(shape, dtype=dtype)
-    if stream is not None:
-        t.record_stream(stream)
-    return t
-
-
-def _workspace(given: Optional[torch.Tensor], need: int, like: torch.Tensor, stream):
+def _workspace(given: Optional[torch.Tensor], need: int, like: torch.Tensor):
     """(tensor to keep during the call, address, bytes)"""
     if given is None:
         if not need:
             return None, None, 0
-        given = _empty((need,), torch.uint8, like, stream)
+        given = like.new_empty((need,), dtype=torch.uint8)
     elif given.dtype != torch.uint8 or not given.is_contiguous() or given.get_device() != like.get_device():
         raise ValueError(f"workspace must be contiguous uint8 on {like.device}")
     return given, given.data_ptr(), given.numel()
@@ -211,7 +223,7 @@ def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Opti
             k = slot_row.shape[1]
             yp = _arg("y", y, (y_rows, d), None, gpu)
         if h_out is None:
-            h_out = _empty(shape, h.dtype, h, stream)
+            h_out = h.new_empty(shape, dtype=h.dtype)
     else:
         if h_out is not None or slot_row is not None or slot_weights is not None or any(v is not None for v in (w_post, scale, gate)):
             raise ValueError("h_out, slots, w_post, scale and gate go with y")
@@ -219,7 +231,7 @@ def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Opti
         if x is not None:
             raise ValueError("x goes with w_pre")
     elif x is None:
-        x = _empty(shape, x_dtype, h, stream)
+        x = h.new_empty(shape, dtype=x_dtype)
     s = _norm_layer(h, y, LX_BF16 if x is None else _dtype("x", x), w_pre, w_post, scale, gate, residual_scale, eps, T, d, gpu)
     st = lib().lx_block_norm(ctypes.byref(s), T, _arg("h", h, shape, None, gpu), yp, y_rows, k,
                              _arg("slot_row", slot_row, (T, k), torch.int32, gpu),
@@ -262,15 +274,15 @@ def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Opti
     s = _norm_layer(h_out, y, LX_BF16 if dx is None else _dtype("dx", dx), w_pre, w_post, scale, gate, residual_scale,
                     eps, T, d, gpu)
     if dh is None:
-        dh = _empty(shape, h_out.dtype, h_out, stream)
+        dh = h_out.new_empty(shape, dtype=h_out.dtype)
     if dy is None and y is not None:
-        dy = _empty(shape, y.dtype, h_out, stream)
-    dgate = None if gate is None else _empty((T,), torch.float32, h_out, stream)
+        dy = h_out.new_empty(shape, dtype=y.dtype)
+    dgate = None if gate is None else h_out.new_empty((T,), dtype=torch.float32)
     given = [v is not None for v in (w_pre, w_post, scale)]
-    rows = iter(_empty((sum(given), d), torch.float32, h_out, stream).unbind(0) if any(given) else ())
+    rows = iter(h_out.new_empty((sum(given), d), dtype=torch.float32).unbind(0) if any(given) else ())
     dw_pre, dw_post, dscale = (next(rows) if g else None for g in given)
     L = lib()
-    keep, ws, n = _workspace(workspace, L.lx_block_norm_backward_workspace_bytes(T, d), h_out, stream)
+    keep, ws, n = _workspace(workspace, L.lx_block_norm_backward_workspace_bytes(T, d), h_out)
     st = L.lx_block_norm_backward(
         ctypes.byref(s), T, _arg("h_out", h_out, shape, None, gpu), _arg("y", y, shape, None, gpu),
         _arg("dx", dx, shape, None, gpu), _arg("dh_out", dh_out, shape, h_out.dtype, gpu),
@@ -306,10 +318,10 @@ def balance_loss(logits: torch.Tensor, topk_ids: torch.Tensor, *, mask: Optional
     gpu = _gpu("logits", logits)
     T, E = logits.shape
     k = topk_ids.shape[1]
-    r = BalanceLoss(_empty((1,), torch.float32, logits, stream), _empty((E,), torch.int32, logits, stream),
-                    _empty((E,), torch.float32, logits, stream), _empty((1,), torch.int32, logits, stream))
+    r = BalanceLoss(logits.new_empty((1,), dtype=torch.float32), logits.new_empty((E,), dtype=torch.int32),
+                    logits.new_empty((E,), dtype=torch.float32), logits.new_empty((1,), dtype=torch.int32))
     L = lib()
-    keep, ws, n = _workspace(workspace, L.lx_balance_loss_workspace_bytes(T, E), logits, stream)
+    keep, ws, n = _workspace(workspace, L.lx_balance_loss_workspace_bytes(T, E), logits)
     st = L.lx_balance_loss(_arg("logits", logits, (T, E), None, gpu), _dtype("logits", logits), T, E,
                            _arg("topk_ids", topk_ids, (T, k), torch.int32, gpu), k, _mask_arg(mask, T, gpu), coef,
                            r.loss.data_ptr(), r.counts.data_ptr(), r.prob.data_ptr(), r.n_tokens.data_ptr(), ws, n,
@@ -332,7 +344,7 @@ def balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_tokens: 
     gpu = _gpu("logits", logits)
     T, E = shape = logits.shape
     if dlogits is None:
-        dlogits = _empty(shape, logits.dtype, logits, stream)
+        dlogits = logits.new_empty(shape, dtype=logits.dtype)
     if dloss is not None and dloss.dim() != 1:
         dloss = dloss.view(1)
     st = lib().lx_balance_loss_backward(
@@ -368,7 +380,7 @@ def mx4_quantize(x: torch.Tensor, *, act: int = MX4_NONE, out: Optional[Mx4] = N
     Kp = mx4_padded(K)
     cs, ss = (*lead, Kp // 2), (*lead, Kp // 32)
     if out is None:
-        out = Mx4(_empty(cs, torch.uint8, x, stream), _empty(ss, torch.uint8, x, stream), K)
+        out = Mx4(x.new_empty(cs, dtype=torch.uint8), x.new_empty(ss, dtype=torch.uint8), K)
     elif out.K != K:
         raise ValueError("out.K does not fit x")
     st = lib().lx_mx4_quantize(x.data_ptr(), _dtype("x", x), rows, K, act, _arg("codes", out.codes, cs, torch.uint8, gpu),
@@ -387,7 +399,7 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, *, out: Optional
     Kp = mx4_padded(K)
     shape = (*lead, K)
     if out is None:
-        out = _empty(shape, dtype, q.codes, stream)
+        out = q.codes.new_empty(shape, dtype=dtype)
     st = lib().lx_mx4_dequantize(_arg("codes", q.codes, (*lead, Kp // 2), torch.uint8, gpu),
                                  _arg("scales", q.scales, (*lead, Kp // 32), torch.uint8, gpu), lead.numel(), K,
                                  _arg("out", out, shape, None, gpu), _dtype("out", out), _handle(stream, gpu))
@@ -416,9 +428,9 @@ def mx4_gemm(a: Mx4, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map:
     G, N = lead if len(lead) == 2 else (1, lead[0])
     M = rows if row_map is None else row_map.shape[0]
     if out is None:
-        out = _empty((M, N), out_dtype, ac, stream)
+        out = ac.new_empty((M, N), dtype=out_dtype)
     L = lib()
-    keep, ws, n = _workspace(workspace, L.lx_mx4_gemm_workspace_bytes(M, N, K, G), ac, stream)
+    keep, ws, n = _workspace(workspace, L.lx_mx4_gemm_workspace_bytes(M, N, K, G), ac)
     st = L.lx_mx4_gemm(_arg("a codes", ac, (rows, Kp // 2), torch.uint8, gpu),
                        _arg("a scales", a.scales, (rows, Kp // 32), torch.uint8, gpu), rows,
                        _arg("row_map", row_map, (M,), torch.int32, gpu),

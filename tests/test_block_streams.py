@@ -163,3 +163,27 @@ def test_moe_block_runs_on_its_gpu(world):
         out = lb.mx4_moe_block(t(BF16, 4, d), t(BF16, d), t(BF16, E, d), ex, k)
     assert len(world.calls) == 7 and {c[1] for c in world.calls} == {1} and world.device == 0
     assert out.h_out.gpu == 1
+
+
+def tensors(r):
+    return [t for v in r for t in tensors(v)] if isinstance(r, tuple) else [r] if isinstance(r, Tensor) else []
+
+
+@pytest.mark.parametrize("entry", ENTRIES)
+def test_memory_of_a_call_is_in_its_streams_order(world, entry):
+    """What a call allocates, workspaces among it, is memory of the call's stream:
+    memory of another stream's pool may still be in use by that stream's pending
+    work. What is handed to the caller is not reused before the caller's stream,
+    as it stood at the call, is done with it."""
+    side, caller = Stream(0, 77), world.current[0]
+    out = tensors(calls(world, 0)[entry](stream=side))
+    ((_, _, handle, used),) = world.calls
+    assert handle == 77 and world.made
+    for t in world.made:
+        assert t.pool is side
+    new = [t for t in out if t.pool is not None]
+    assert new and all(caller in t.recorded for t in new)
+    assert {id(t) for t in used if t.pool is not None} >= {id(t) for t in new}
+    world.made.clear()
+    calls(world, 0)[entry]()
+    assert world.made and all(t.pool is caller for t in world.made)
