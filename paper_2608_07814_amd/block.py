@@ -131,14 +131,15 @@ def _on_its_gpu(fn):
     same on every GPU), and with the call's stream as the current one, so that what
     the call allocates is memory of that stream's order: memory of another
     stream's pool may still be in use by that stream's pending work."""
-    name = next(iter(inspect.signature(fn).parameters))
+    names = list(inspect.signature(fn).parameters)
+    name, at = names[0], names.index("stream") if "stream" in names else len(names)
 
     @functools.wraps(fn)
     def call(*args, **kw):
         first = args[0] if args else kw[name]
         gpu = (first.codes if isinstance(first, Mx4) else first).get_device()
         if gpu >= 0:  # (else refused by fn)
-            stream = kw.get("stream")
+            stream = args[at] if len(args) > at else kw.get("stream")
             if stream is not None:
                 if stream.device_index != gpu:
                     raise ValueError(f"stream is on cuda:{stream.device_index}, {name} on cuda:{gpu}")
@@ -451,9 +452,11 @@ class Mx4Experts(NamedTuple):
     down: Mx4
 
 
+@_on_its_gpu
 def mx4_experts(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, stream=None) -> Mx4Experts:
     """Experts w_gate, w_up [E][f][d], w_down [E][d][f] rounded to 4 bits, once
-    when a model is loaded."""
+    when a model is loaded; all of it in ``stream``, the joining of the projections
+    too."""
     return Mx4Experts(mx4_quantize(torch.cat([w_gate, w_up], dim=1), stream=stream),
                       mx4_quantize(w_down.contiguous(), stream=stream))
 

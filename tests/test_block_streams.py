@@ -187,3 +187,37 @@ def test_memory_of_a_call_is_in_its_streams_order(world, entry):
     world.made.clear()
     calls(world, 0)[entry]()
     assert world.made and all(t.pool is caller for t in world.made)
+
+
+def test_experts_are_rounded_in_one_stream(world, monkeypatch):
+    """Joining the projections, making them contiguous, rounding: all of it in the
+    given stream (else the rounding may read what is not yet written), the
+    temporaries in its memory."""
+    side, caller, where = Stream(0, 77), world.current[0], []
+
+    def cat(parts, dim):
+        where.append(world.stream())
+        return parts[0].new_empty((8, 256, 128))
+
+    def contiguous(self):
+        where.append(world.stream())
+        return self.new_empty(self.shape)
+
+    monkeypatch.setattr(torch, "cat", cat)
+    monkeypatch.setattr(Tensor, "contiguous", contiguous)
+    w = Tensor(world, (8, 128, 128), BF16, 0)
+    for give in (lambda: lb.mx4_experts(w, w, w, side), lambda: lb.mx4_experts(w, w, w, stream=side)):
+        ex = give()
+        assert len(where) >= 2 and all(s is side for s in where)
+        assert [c[2] for c in world.calls] == [77, 77] and all(t.pool is side for t in world.made)
+        assert all(caller in t.recorded for t in tensors(ex)) and len(tensors(ex)) == 4
+        for v in (where, world.calls, world.made):
+            v.clear()
+    lb.mx4_experts(w, w, w)
+    assert all(s is caller for s in where) and [c[2] for c in world.calls] == [0, 0]
+    where.clear()
+    w.gpu = 1
+    lb.mx4_experts(w, w, w)
+    assert {c[1] for c in world.calls[2:]} == {1} and all(s is world.current[1] for s in where)
+    with pytest.raises(ValueError):
+        lb.mx4_experts(w, w, w, side)
