@@ -50,6 +50,7 @@ def main():
 
     hd = r(a.decode, d).bfloat16()
     side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())  # (the current stream makes hd)
     with torch.cuda.stream(side):
         for _ in range(2):
             eager = block(hd)
@@ -57,6 +58,7 @@ def main():
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=side):
             replayed = block(hd)
+    torch.cuda.current_stream().wait_stream(side)
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(replayed.h_out, eager.h_out) and torch.equal(replayed.x_next, eager.x_next)
