@@ -67,12 +67,12 @@ lx_status lx_block_norm(const lx_norm_layer* layer, int32_t T, const void* h, co
                         void* stream);
 
 /* The gradients of lx_block_norm (without slots), from its inputs and from
- * h_out as it was stored: dx is the gradient of x (NULL exactly when w_pre
- * is), dh_out the gradient of h_out from elsewhere (NULL: zero). Outputs: dh
- * [T][d]; dy [T][d] (given exactly when y is); fp32 dgate [T], dw_pre [d],
- * dw_post [d], dscale [d], each given exactly when its input takes part.
- * Without y (no block) h_out is the stream h itself and dh its gradient. dh
- * may be dh_out. T = 0 writes zeros to the gradients of the weights.
+ * h_out as it was stored (without w_pre not read): dx is the gradient of x
+ * (NULL exactly when w_pre is), dh_out the gradient of h_out from elsewhere
+ * (NULL: zero). Outputs: dh [T][d]; dy [T][d] (given exactly when y is); fp32
+ * dgate [T], dw_pre [d], dw_post [d], dscale [d], each given exactly when its
+ * input takes part. Without y (no block) h_out is the stream h itself and dh
+ * its gradient. dh may be dh_out. T = 0 writes zeros to the gradients of the weights.
  * workspace 256-byte aligned, lx_block_norm_backward_workspace_bytes bytes. */
 size_t lx_block_norm_backward_workspace_bytes(int32_t T, int32_t d);
 lx_status lx_block_norm_backward(const lx_norm_layer* layer, int32_t T, const void* h_out, const void* y,
