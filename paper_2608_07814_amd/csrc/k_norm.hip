@@ -11,6 +11,7 @@
 #include "lx_vec.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 namespace lx {
@@ -296,7 +297,10 @@ __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) 
         sp[i].v[e] += dx.v[e] * mm;
         sq[i].v[e] += gate * d * n;
         dh.v[e] = alpha * d;
-        dy.v[e] = ry * gate * (d * w.s.v[e] - n * zn);
+        // (without w_post zn is 0 and dy does not depend on y, which may be infinite or
+        // NaN: its product with 0 must not count. With w_post zn is NaN then. A
+        // choice by a.w_post took 71 for 62 us at 1024 x 16384)
+        dy.v[e] = ry * gate * (d * w.s.v[e] - __builtin_amdgcn_fmed3f(n, -FLT_MAX, FLT_MAX) * zn);
       }
       if (col(i) < a.d && live) {
         store8(a.dh, a.h_f32, row + col(i), dh);

@@ -31,6 +31,7 @@ inline uint32_t __float_as_uint(float f) { uint32_t x; memcpy(&x, &f, 4); return
 struct Two { uint32_t v[2]; uint32_t operator[](int i) const { return v[i]; } };
 #define __builtin_amdgcn_update_dpp(old, x, ...) (x)
 #define __builtin_amdgcn_readfirstlane(x) ((int)(x))
+#define __builtin_amdgcn_fmed3f(a, b, c) ((a) + (b) + (c))
 #define __builtin_amdgcn_permlane16_swap(a, b, ...) (Two{{(a), (b)}})
 #define __builtin_amdgcn_permlane32_swap(a, b, ...) (Two{{(a), (b)}})
 typedef void* hipStream_t;
