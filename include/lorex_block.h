@@ -139,7 +139,7 @@ lx_status lx_mx4_dequantize(const void* codes, const void* scales, int64_t rows,
  * belong to group g (offsets [G + 1] int32 in ascending order, device; NULL:
  * G = 1 and all M rows); M is the most rows there can be: rows from offsets[G]
  * on are not written. Offsets outside [0, M] are clamped to it, and a row_map
- * entry outside [0, a_rows) reads a row of zeros. out [M][N] fp32 or bf16. K a
+ * entry outside [0, a_rows) gives a row of zeros, whatever the weights hold. out [M][N] fp32 or bf16. K a
  * multiple of 8, any N >= 1, G in 1 .. LX_MAX_NODES, M * N < 2^40. A, B and
  * out 16-byte, their scales, row_map and offsets 4-byte aligned; workspace
  * 256-byte aligned, lx_mx4_gemm_workspace_bytes bytes (NULL where that is 0).

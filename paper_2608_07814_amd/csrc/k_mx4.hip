@@ -281,6 +281,7 @@ __global__ __launch_bounds__(256) void k_mx4_gemm_rows(const Mx4GemmArgs a) {
       }
     }
     if (wk == 0 && m < m1) {
+      if (arow < 0) acc = vf4{0.f, 0.f, 0.f, 0.f};  // (also where a weight is NaN)
       const int64_t at = (int64_t)m * a.N + n0 + q * 4;
       if (n0 + q * 4 + 4 <= a.N) {
         if (a.out_f32)

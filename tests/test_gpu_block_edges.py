@@ -63,3 +63,56 @@ def test_backward_without_post_norm_keeps_an_infinite_output_to_itself(d, parts)
             keep = torch.ones(len(a), dtype=torch.bool, device="cuda")
             keep[list(touched)] = False
             assert torch.equal(a[keep], b[keep]) and not torch.isfinite(a[~keep]).any(), name
+
+
+def operand(lead, K, seed):
+    """Codes and scales 2^0, 2^1: every sum of products is exact in fp32."""
+    rng = np.random.default_rng(seed)
+    Kp = O.padded(K)
+    c = rng.integers(0, 256, size=lead + (Kp // 2,)).astype(np.uint8)
+    s = rng.integers(127, 129, size=lead + (Kp // 32,)).astype(np.uint8)
+    c[..., K // 2:] = 0
+    return c, s
+
+
+def dev(c, s, K):
+    return lb.Mx4(torch.from_numpy(c).cuda(), torch.from_numpy(s).cuda(), K)
+
+
+# row kernel with its K in one part and in four, tiles of 64, in parts, 128, 256
+@pytest.mark.parametrize("M,N,K", [(16, 130, 512), (16, 130, 4096), (17, 130, 512), (40, 130, 8192), (2048, 2000, 512), (5000, 8200, 256)])
+def test_a_row_that_is_not_there_gives_zeros(M, N, K):
+    """A map entry out of range gives a row of zeros, also where the weights hold a
+    scale that is NaN, whichever kernel runs."""
+    require_gpu()
+    say(f"mx4_gemm absent rows M={M} N={N} K={K}")
+    rows = 9
+    a, b = operand((rows,), K, M), operand((1, N), K, M + 1)
+    b[1][0, 77, 5] = 255
+    rm = np.random.default_rng(M).integers(0, rows, size=M).astype(np.int32)
+    rm[[0, 5, M - 1]] = -1, rows, 1 << 30
+    there = torch.from_numpy((rm >= 0) & (rm < rows)).cuda()
+    for dt in (torch.float32, torch.bfloat16):
+        o = lb.mx4_gemm(dev(*a, K), dev(*b, K), row_map=torch.from_numpy(rm).cuda(), out_dtype=dt)
+        assert not o[~there].any() and not o[~there].isnan().any()
+        assert o[there][:, 77].isnan().all()
+        got = o[there].double().cpu()
+        ref = torch.from_numpy(O.gemm(O.dequantize(*a, K), O.dequantize(*b, K), M, None, rm))[there.cpu()].to(dt).double()
+        cols = torch.arange(N) != 77
+        assert torch.equal(got[:, cols], ref[:, cols])
+
+
+def test_rows_from_more_than_32_bits_of_codes():
+    """Rows gathered from an operand of 2^32 bytes of codes and more."""
+    require_gpu()
+    K, M, N = 8192, 70, 130
+    rows = (1 << 32) // (K // 2) + 50
+    say(f"mx4_gemm rows of {rows} x {K}")
+    a, b = operand((50,), K, 5), operand((1, N), K, 6)
+    codes = torch.zeros(rows, K // 2, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows, K // 32), 127, dtype=torch.uint8, device="cuda")
+    codes[-50:], scales[-50:] = torch.from_numpy(a[0]).cuda(), torch.from_numpy(a[1]).cuda()
+    rm = np.random.default_rng(7).integers(0, 50, size=M)
+    o = lb.mx4_gemm(lb.Mx4(codes, scales, K), dev(*b, K), row_map=torch.from_numpy((rm + rows - 50).astype(np.int32)).cuda())
+    ref = O.gemm(O.dequantize(*a, K), O.dequantize(*b, K), M, None, rm)
+    assert np.array_equal(o.double().cpu().numpy(), ref)
