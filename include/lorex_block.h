@@ -129,7 +129,7 @@ typedef enum lx_mx4_act { LX_MX4_NONE = 0, LX_MX4_SWIGLU = 1 } lx_mx4_act;
 lx_status lx_mx4_quantize(const void* x, lx_dtype dtype, int64_t rows, int32_t K, lx_mx4_act act, void* codes,
                           void* scales, void* stream);
 
-/* codes, scales -> out [rows][K]; exact in both types. */
+/* codes, scales -> out [rows][K]; exact in both types (from 2^128 on infinite). */
 lx_status lx_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int32_t K, void* out,
                             lx_dtype dtype, void* stream);
 
@@ -139,11 +139,15 @@ lx_status lx_mx4_dequantize(const void* codes, const void* scales, int64_t rows,
  * belong to group g (offsets [G + 1] int32 in ascending order, device; NULL:
  * G = 1 and all M rows); M is the most rows there can be: rows from offsets[G]
  * on are not written. Offsets outside [0, M] are clamped to it, and a row_map
- * entry outside [0, a_rows) gives a row of zeros, whatever the weights hold. out [M][N] fp32 or bf16. K a
- * multiple of 8, any N >= 1, G in 1 .. LX_MAX_NODES, M * N < 2^40. A, B and
- * out 16-byte, their scales, row_map and offsets 4-byte aligned; workspace
- * 256-byte aligned, lx_mx4_gemm_workspace_bytes bytes (NULL where that is 0).
- * The order in which a sum is formed depends on M, N, K and G only. */
+ * entry outside [0, a_rows) gives a row of zeros, whatever the weights hold.
+ * out [M][N] fp32 or bf16. K a multiple of 8, any N >= 1, G in 1 ..
+ * LX_MAX_NODES, M * N < 2^40. A, B and out 16-byte, their scales, row_map and
+ * offsets 4-byte aligned; workspace 256-byte aligned,
+ * lx_mx4_gemm_workspace_bytes bytes (NULL where that is 0).
+ * The order in which a sum is formed depends on M, N, K, G and on whether A's
+ * codes reach 2^32 bytes (or a_rows is 0): from there on the kernel of few rows
+ * runs, which reads a group's weights once per 16 rows; rows that are gathered
+ * from that far are better copied together first. */
 size_t lx_mx4_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t G);
 lx_status lx_mx4_gemm(const void* a, const void* a_scales, int32_t a_rows, const int32_t* row_map, const void* b,
                       const void* b_scales, const int32_t* offsets, int32_t G, int32_t M, int32_t N, int32_t K,

@@ -319,7 +319,8 @@ lx_status lx_mx4_gemm(const void* a, const void* a_scales, int32_t a_rows, const
     if (!workspace || !al(workspace, 256)) return set_error(LX_ERR_INVALID_ARGUMENT, "workspace null or not 256-byte aligned");
     if (workspace_bytes < need) return set_error(LX_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than required");
   }
-  // the tile kernels address A and a tile's weights by 32-bit byte offsets
+  // the tile kernels address A by 32-bit byte offsets (and a tile's weights, at most
+  // 2^31 bytes)
   if (a_rows == 0 || (int64_t)a_rows * (LX_MX4_KP(K) / 2) >= ((int64_t)1 << 32)) g.plan = {Mx4GemmPlan::kRows, 1, 0};
   g.part = (float*)workspace;
   g.a = (const uint8_t*)a;
