@@ -140,8 +140,8 @@ lx_status lx_mx4_dequantize(const void* codes, const void* scales, int64_t rows,
  * G = 1 and all M rows); M is the most rows there can be: rows from offsets[G]
  * on are not written. Offsets outside [0, M] are clamped to it, and a row_map
  * entry outside [0, a_rows) gives a row of zeros, whatever the weights hold.
- * out [M][N] fp32 or bf16. K a multiple of 8, any N >= 1, G in 1 ..
- * LX_MAX_NODES, M * N < 2^40. A, B and out 16-byte, their scales, row_map and
+ * out [M][N] fp32 or bf16. K a multiple of 8, M and N at most 2^31 -
+ * 256, M * N < 2^40, G in 1 .. LX_MAX_NODES. A, B and out 16-byte, their scales, row_map and
  * offsets 4-byte aligned; workspace 256-byte aligned,
  * lx_mx4_gemm_workspace_bytes bytes (NULL where that is 0).
  * The order in which a sum is formed depends on M, N, K, G and on whether A's

@@ -87,6 +87,8 @@ lx_status check_mx4_gemm(int32_t M, int32_t N, int32_t K, int32_t G) {
   if (M < 0 || N < 1 || K < 1 || G < 1) return set_error(LX_ERR_INVALID_ARGUMENT, "M must be >= 0; N, K and G positive");
   if (K % 8 || K > (1 << 24)) return set_error(LX_ERR_UNSUPPORTED, "K must be a multiple of 8, at most 2^24");
   if (G > LX_MAX_NODES) return set_error(LX_ERR_UNSUPPORTED, "more groups than LX_MAX_NODES");
+  // (rows and columns are counted in 32 bits, up to a tile past the last one)
+  if (M > INT32_MAX - 255 || N > INT32_MAX - 255) return set_error(LX_ERR_UNSUPPORTED, "M and N must be at most 2^31 - 256");
   if ((int64_t)M * N >= ((int64_t)1 << 40)) return set_error(LX_ERR_UNSUPPORTED, "M * N must be below 2^40");
   return LX_OK;
 }
