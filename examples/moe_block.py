@@ -69,14 +69,15 @@ def main():
     # the router
     y = r(a.tokens, d).bfloat16()  # the experts' sum, as a training forward keeps it
     h_out, x_next = lb.block_norm(h, y, w_pre=w_next, w_post=w_post)
+    w_r32, x32 = w_r.float(), out.x.float()  # (the router's gradients are formed in fp32, as its logits are)
     dh_out, dx_next = r(a.tokens, d).bfloat16(), r(a.tokens, d).bfloat16()
 
     def step():
         after = lb.block_norm_backward(h_out, y, dx_next, dh_out, w_pre=w_next, w_post=w_post)
         dlogits = lb.balance_loss_backward(out.logits, out.balance.counts, out.balance.n_tokens, a.k, coef=0.01)
-        dx = dlogits @ w_r  # (the experts' own gradient would be added here)
+        dx = dlogits @ w_r32  # (the experts' own gradient would be added here)
         before = lb.block_norm_backward(h, None, dx, after.dh, w_pre=w_pre)
-        return before.dh, after, before, dlogits.t() @ out.x
+        return before.dh, after, before, dlogits.t() @ x32
 
     dh, after, before, dw_r = step()
     print(f"training: gradients of stream, norms and router in {timed(step):.0f} us; |dh| {dh.float().norm().item():.1f}, "

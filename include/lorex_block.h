@@ -81,7 +81,15 @@ lx_status lx_block_norm_backward(const lx_norm_layer* layer, int32_t T, const vo
                                  size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------ balance loss
- * For router logits [T][E] (fp32 or bf16) and the chosen experts topk_ids
+ * lx_route_topk that leaves its logits [T][E] (fp32, 16-byte aligned) too: the
+ * sums that ids and weights, which are those of lx_route_topk bit for bit, were
+ * chosen and formed from, for the loss below. The other arguments, the
+ * workspace among them, as there. */
+lx_status lx_route_topk_logits(const void* x, const void* w_r, lx_dtype dtype, int32_t T, int32_t d, int32_t E,
+                               int32_t k, int32_t* topk_ids, float* topk_weights, float* logits, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* For router logits [T][E] (fp32 or bf16) and the chosen experts topk_ids
  * [T][k] (as lx_route_topk writes them), over the N tokens whose mask byte is
  * not zero (mask NULL: all T):
  *

@@ -3,6 +3,7 @@
 
 * :func:`block_norm`, :func:`block_norm_backward`: the norms before and after a
   block with its gate and residual scale;
+* :func:`route_topk_logits`: the router with its logits;
 * :func:`balance_loss`, :func:`balance_loss_backward`: the router's balance
   loss, the tokens per expert, the gradient of the logits;
 * :func:`mx4_quantize`, :func:`mx4_dequantize`, :func:`mx4_gemm`: microscaled
@@ -45,6 +46,8 @@ EXPORTS = {
     "lx_block_norm": (_c_i32, [_c_void, _c_i32, _c_void, _c_void, _c_i32, _c_i32] + [_c_void] * 5),
     "lx_block_norm_backward_workspace_bytes": (_c_size, [_c_i32, _c_i32]),
     "lx_block_norm_backward": (_c_i32, [_c_void, _c_i32] + [_c_void] * 11 + [_c_size, _c_void]),
+    "lx_route_topk_logits": (_c_i32, [_c_void, _c_void, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32] + [_c_void] * 4
+                             + [_c_size, _c_void]),
     "lx_balance_loss_workspace_bytes": (_c_size, [_c_i32, _c_i32]),
     "lx_balance_loss": (_c_i32, [_c_void, _c_i32, _c_i32, _c_i32, _c_void, _c_i32, _c_void, _c_f32] + [_c_void] * 5
                         + [_c_size, _c_void]),
@@ -295,6 +298,28 @@ def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Opti
 
 
 # ------------------------------------------------------------ balance loss
+@_on_its_gpu
+def route_topk_logits(x: torch.Tensor, w_r: torch.Tensor, k: int, *, workspace: Optional[torch.Tensor] = None,
+                      stream=None):
+    """The router with its logits (lx_route_topk_logits): bf16 x [T][d], w_r [E][d]
+    -> (int32 ids [T][k], fp32 weights [T][k], fp32 logits [T][E])."""
+    if x.dim() != 2 or w_r.dim() != 2:
+        raise ValueError("x must be [T][d] and w_r [E][d]")
+    gpu = _gpu("x", x)
+    T, d = x.shape
+    E = w_r.shape[0]
+    ids, weights = x.new_empty((T, k), dtype=torch.int32), x.new_empty((T, k), dtype=torch.float32)
+    logits = x.new_empty((T, E), dtype=torch.float32)
+    L = lib()
+    keep, ws, n = _workspace(workspace, L.lx_route_workspace_bytes(T, d, E), x)
+    st = L.lx_route_topk_logits(_arg("x", x, (T, d), torch.bfloat16, gpu), _arg("w_r", w_r, (E, d), torch.bfloat16, gpu),
+                                LX_BF16, T, d, E, k, ids.data_ptr(), weights.data_ptr(), logits.data_ptr(), ws, n,
+                                _handle(stream, gpu))
+    if st:
+        _check(st)
+    return ids, weights, logits
+
+
 class BalanceLoss(NamedTuple):
     loss: torch.Tensor      # [1] fp32
     counts: torch.Tensor    # [E] int32: slots of unmasked tokens on each expert
@@ -467,7 +492,7 @@ class Mx4BlockOut(NamedTuple):
     x: torch.Tensor                  # [T][d] this block's input
     topk_ids: torch.Tensor
     topk_weights: torch.Tensor
-    logits: Optional[torch.Tensor]   # [T][E] (balance_coef given)
+    logits: Optional[torch.Tensor]   # [T][E] fp32, as the router chose by (balance_coef given)
     balance: Optional[BalanceLoss]
 
 
@@ -492,13 +517,16 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
     if w_r.get_device() != _gpu("h", h):
         raise ValueError(f"w_r is on {w_r.device}, h on {h.device}")
     _, x = block_norm(h, w_pre=w_pre, eps=eps)
-    if T:
-        ids, weights = lx.route_topk(x, w_r, k)
-    else:  # nothing to route
-        ids, weights = h.new_empty((0, k), dtype=torch.int32), h.new_empty((0, k), dtype=torch.float32)
     logits = balance = None
+    if not T:  # nothing to route
+        ids, weights = h.new_empty((0, k), dtype=torch.int32), h.new_empty((0, k), dtype=torch.float32)
+        if balance_coef is not None:
+            logits = h.new_empty((0, E), dtype=torch.float32)
+    elif balance_coef is not None:
+        ids, weights, logits = route_topk_logits(x, w_r, k)
+    else:
+        ids, weights = lx.route_topk(x, w_r, k)
     if balance_coef is not None:
-        logits = x @ w_r.t()
         balance = balance_loss(logits, ids, mask=mask, coef=balance_coef)
     if not T:
         h_out, x_next = block_norm(h, h.new_empty((0, d), dtype=torch.float32), w_pre=w_next, w_post=w_post, scale=scale,

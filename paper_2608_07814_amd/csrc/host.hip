@@ -1442,10 +1442,10 @@ size_t lx_route_workspace_bytes(int32_t T, int32_t d, int32_t E) {
   return route_plan(T, d, E).total;
 }
 
-lx_status lx_route_topk(const void* x, const void* w_r, lx_dtype dtype, int32_t T, int32_t d, int32_t E,
-                        int32_t k, int32_t* topk_ids, float* topk_weights, void* workspace,
-                        size_t workspace_bytes, void* stream) {
-  g_err.clear();
+// The router; with `logits` its logits are left there ([T][E]).
+static lx_status route_topk(const void* x, const void* w_r, lx_dtype dtype, int32_t T, int32_t d, int32_t E,
+                            int32_t k, int32_t* topk_ids, float* topk_weights, float* logits, void* workspace,
+                            size_t workspace_bytes, void* stream) {
   const lx_status st = check_route(dtype, T, d, E, k);
   if (st != LX_OK) return st;
   if (T == 0) return LX_OK;
@@ -1463,7 +1463,7 @@ lx_status lx_route_topk(const void* x, const void* w_r, lx_dtype dtype, int32_t 
   g.B[0] = g.B[1] = w_r;
   g.ncols[0] = E;
   g.K = d;
-  g.C = (float*)(W + P.logits);
+  g.C = logits ? logits : (float*)(W + P.logits);
   g.ldc = E;
   g.dense_rows = T;
   if (P.S > 1) {
@@ -1474,9 +1474,24 @@ lx_status lx_route_topk(const void* x, const void* w_r, lx_dtype dtype, int32_t 
   if (!gemm_big_ok(g, kSkinnyBN, T)) return fail(LX_ERR_UNSUPPORTED, "router shape not supported");
   hipStream_t lstream = s;
   LX_LAUNCH("router_logits", launch_gemm_skinny(g, OUT_F32, (T + kSkinnyBM - 1) / kSkinnyBM, lstream));
-  LX_LAUNCH("router_topk", launch_topk((const float*)(W + P.logits), (const float*)(W + P.part), P.S, T, E, k,
-                                       topk_ids, topk_weights, lstream));
+  LX_LAUNCH("router_topk", launch_topk((const float*)g.C, (const float*)(W + P.part), P.S, T, E, k, topk_ids,
+                                       topk_weights, lstream, P.S > 1 ? logits : nullptr));
   return LX_OK;
+}
+
+lx_status lx_route_topk(const void* x, const void* w_r, lx_dtype dtype, int32_t T, int32_t d, int32_t E,
+                        int32_t k, int32_t* topk_ids, float* topk_weights, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  g_err.clear();
+  return route_topk(x, w_r, dtype, T, d, E, k, topk_ids, topk_weights, nullptr, workspace, workspace_bytes, stream);
+}
+
+lx_status lx_route_topk_logits(const void* x, const void* w_r, lx_dtype dtype, int32_t T, int32_t d, int32_t E,
+                               int32_t k, int32_t* topk_ids, float* topk_weights, float* logits, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  g_err.clear();
+  if (T > 0 && (!logits || !aligned(logits, 16))) return fail(LX_ERR_INVALID_ARGUMENT, "null or misaligned logits");
+  return route_topk(x, w_r, dtype, T, d, E, k, topk_ids, topk_weights, logits, workspace, workspace_bytes, stream);
 }
 
 size_t lx_route_moe_tree_workspace_bytes(const lx_tree_layer* layer, int32_t T, int32_t k) {

@@ -21,17 +21,18 @@ namespace {
 
 constexpr int TK_WAVES = 4;
 
-template <int PER, bool SWAP>
+// KEEP: the sums of partial tiles are left in `sums` too.
+template <int PER, bool SWAP, bool KEEP>
 __global__ __launch_bounds__(TK_WAVES * 64) void k_topk(const float* __restrict__ logits,
                                                         const float* __restrict__ part, int S, int T, int E,
                                                         int k, int32_t* __restrict__ ids,
-                                                        float* __restrict__ weights) {
+                                                        float* __restrict__ weights, float* __restrict__ sums) {
   const int lane = threadIdx.x & 63;
   const int t = blockIdx.x * TK_WAVES + (threadIdx.x >> 6);
   if (t >= T) return;  // whole wavefront
   int id;
   float wt;
-  topk_token<PER, SWAP>(logits, part, S, E, k, t, id, wt);
+  topk_token<PER, SWAP>(logits, part, S, E, k, t, id, wt, KEEP ? sums : nullptr);
   if (lane < k) {
     ids[(int64_t)t * k + lane] = id;
     weights[(int64_t)t * k + lane] = wt;
@@ -106,12 +107,14 @@ hipError_t launch_topk_hist(const RouteIn& r, const BucketArgs& a, hipStream_t s
 }
 
 hipError_t launch_topk(const float* logits, const float* part, int S, int T, int E, int k, int32_t* ids,
-                       float* weights, hipStream_t s) {
+                       float* weights, hipStream_t s, float* sums) {
   if (T <= 0) return hipSuccess;
   const dim3 grid((T + TK_WAVES - 1) / TK_WAVES), thr(TK_WAVES * 64);
   return with_topk_shape(T, E, [&](auto per, auto swap) {
-    hipLaunchKernelGGL((k_topk<decltype(per)::value, decltype(swap)::value>), grid, thr, 0, s, logits, part, S, T, E, k,
-                       ids, weights);
+    constexpr int PER = decltype(per)::value;
+    constexpr bool SWAP = decltype(swap)::value;
+    const auto kernel = sums ? k_topk<PER, SWAP, true> : k_topk<PER, SWAP, false>;
+    hipLaunchKernelGGL(kernel, grid, thr, 0, s, logits, part, S, T, E, k, ids, weights, sums);
   });
 }
 

@@ -454,10 +454,11 @@ struct TokenArgs {
 // Top-k over router logits: logits [T][E] fp32 (S == 1), or the S partial
 // tiles per (32-row tile, 64-column tile) item that a deferred split-K
 // skinny GEMM left in part (slot (item * S + split), layout [wavefront][row]
-// [32 columns]). 1 <= k <= min(E, LX_MAX_K), E <= kRouteMaxE.
+// [32 columns]), whose sums are left in `sums` [T][E] where it is given. 1 <= k
+// <= min(E, LX_MAX_K), E <= kRouteMaxE.
 constexpr int kRouteMaxE = 512;
 hipError_t launch_topk(const float* logits, const float* part, int S, int T, int E, int k, int32_t* ids,
-                       float* weights, hipStream_t s);
+                       float* weights, hipStream_t s, float* sums = nullptr);
 
 // ---------------------------------------------------------------- clustering
 // Router profiling counts and the NPMI distance (fire [E], pair [E][E]

@@ -7,7 +7,8 @@
 // ([T][E] fp32, S <= 1) or S partial tiles per (32-row tile, 64-column tile)
 // item, added here in split order (run-to-run deterministic).
 // Lane l holds experts l, l + 64, ...; k rounds of a wavefront-wide (value,
-// lower index) maximum; lane j < k returns the j-th choice.
+// lower index) maximum; lane j < k returns the j-th choice. Sums of partial tiles
+// are left in `sums` ([T][E]) where it is given.
 #pragma once
 
 #include "lx_internal.h"
@@ -79,7 +80,8 @@ __device__ __forceinline__ void wave_best(float& bv, int& bi) {
 // (wavefront-wide shuffles).
 template <int PER, bool SWAP>
 __device__ __forceinline__ void topk_token(const float* __restrict__ logits, const float* __restrict__ part, int S,
-                                           int E, int k, int t, int& id, float& weight) {
+                                           int E, int k, int t, int& id, float& weight,
+                                           float* __restrict__ sums = nullptr) {
   const int lane = threadIdx.x & 63;
   const int ntn = (E + kSkinnyBN - 1) / kSkinnyBN;
   float v[PER];
@@ -108,6 +110,11 @@ __device__ __forceinline__ void topk_token(const float* __restrict__ logits, con
     for (int sp = 1; sp < S; ++sp) {
 #pragma unroll
       for (int j = 0; j < PER; ++j) v[j] += part[q[j] + sp * (kSkinnyBM * kSkinnyBN)];
+    }
+    if (sums) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+        if (lane + 64 * j < E) sums[(int64_t)t * E + lane + 64 * j] = v[j];
     }
   }
   uint32_t taken = 0;

@@ -122,6 +122,7 @@ def calls(world, gpu):
         "block_norm": lambda **kw: lb.block_norm(h, y, w_pre=w, w_post=w, **kw),
         "block_norm by names": lambda **kw: lb.block_norm(h=h, w_pre=w, **kw),
         "block_norm_backward": lambda **kw: lb.block_norm_backward(h, y, h, h, w_pre=w, w_post=w, gate=t(F32, 4), **kw),
+        "route_topk_logits": lambda **kw: lb.route_topk_logits(h, t(BF16, 8, 64), 2, **kw),
         "balance_loss": lambda **kw: lb.balance_loss(h, t(I32, 4, 2), **kw),
         "balance_loss_backward": lambda **kw: lb.balance_loss_backward(h, t(I32, 64), t(I32, 1), 2, **kw),
         "mx4_quantize": lambda **kw: lb.mx4_quantize(h, **kw),
