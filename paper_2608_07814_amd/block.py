@@ -532,9 +532,12 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
         h_out, x_next = block_norm(h, h.new_empty((0, d), dtype=torch.float32), w_pre=w_next, w_post=w_post, scale=scale,
                                    gate=gate, residual_scale=residual_scale, eps=eps)
         return Mx4BlockOut(h_out, x_next, x, ids, weights, logits, balance)
-    # rows of the experts: a tree without levels, whose weights bucketing does not read
+    # rows of the experts: a tree without levels, whose weights bucketing does not read.
+    # It takes a forward's workspace, so the tree is given small sizes: with the experts'
+    # own that is 2.9 GiB for 8192 tokens on 8 experts of 14336, with 64 (the smallest for
+    # which a decode batch has one table of tiles to build, not two) 16 MiB
     tree = lx.LxTreeLayer()
-    tree.E, tree.d, tree.f, tree.dtype, tree.n_anchors = E, d, f, LX_BF16, E
+    tree.E, tree.d, tree.f, tree.dtype, tree.n_anchors = E, 64, 64, LX_BF16, E
     tree.anchor_gate = tree.anchor_up = tree.anchor_down = experts.gate_up.codes.data_ptr()
     L = lib()
     n = L.lx_moe_tree_workspace_bytes(ctypes.byref(tree), T, k)

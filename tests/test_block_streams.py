@@ -2,6 +2,8 @@
 expert layer issue their work, on the CPU: tensors, streams and the library are
 stand-ins that record what happens."""
 import contextlib
+import ctypes
+import os
 
 import pytest
 import torch
@@ -108,6 +110,17 @@ def world(monkeypatch):
     monkeypatch.setattr(lb, "_current_raw_stream", lambda gpu: w.stream(gpu).cuda_stream)
     monkeypatch.setattr(lb, "_current_device", lambda: w.device, raising=False)
     return w
+
+
+def _library():
+    """The library itself, for sizes (no call of it reaches a launch)."""
+    if not os.path.exists(lx.LIB_PATH):
+        from paper_2608_07814_amd import build
+        build.build()
+    L = ctypes.CDLL(lx.LIB_PATH)
+    fn = L.lx_moe_tree_workspace_bytes
+    fn.restype, fn.argtypes = lx.EXPORTS["lx_moe_tree_workspace_bytes"]
+    return L
 
 
 F32, BF16, I32, U8 = torch.float32, torch.bfloat16, torch.int32, torch.uint8
@@ -222,3 +235,18 @@ def test_experts_are_rounded_in_one_stream(world, monkeypatch):
     assert {c[1] for c in world.calls[2:]} == {1} and all(s is world.current[1] for s in where)
     with pytest.raises(ValueError):
         lb.mx4_experts(w, w, w, side)
+
+
+@pytest.mark.parametrize("T,E,d,f,k", [(4096, 128, 2048, 768, 8), (8192, 8, 4096, 14336, 2)])
+def test_moe_block_reserves_what_bucketing_needs(world, monkeypatch, T, E, d, f, k):
+    """The block's workspace follows the slots, not the experts' sizes: a forward of
+    these layers would take up to 2.9 GiB."""
+    real = _library()
+    monkeypatch.setattr(World, "lx_moe_tree_workspace_bytes", lambda self, *a: real.lx_moe_tree_workspace_bytes(*a), raising=False)
+    monkeypatch.setattr(lx, "route_topk", lambda x, w_r, k, **kw: (x.new_empty((T, k), dtype=I32), x.new_empty((T, k), dtype=F32)))
+    t = lambda dtype, *shape: Tensor(world, shape, dtype, 0)  # noqa: E731
+    q = lambda *s: lb.Mx4(t(U8, *s[:-1], lb.mx4_padded(s[-1]) // 2), t(U8, *s[:-1], lb.mx4_padded(s[-1]) // 32), s[-1])  # noqa: E731
+    ex = lb.Mx4Experts(q(E, 2 * f, d), q(E, d, f))
+    lb.mx4_moe_block(t(BF16, T, d), t(BF16, d), t(BF16, E, d), ex, k)
+    (ws,) = [m for m in world.made if m.dtype == U8 and m.dim() == 1 and m.numel() != 4096]
+    assert ws.numel() <= 1200 * T * k + (8 << 20)
