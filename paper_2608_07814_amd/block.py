@@ -21,8 +21,6 @@ that one before it uses the outputs.
 from __future__ import annotations
 
 import ctypes
-import functools
-import inspect
 from typing import NamedTuple, Optional
 
 import torch
@@ -91,7 +89,7 @@ def _dtype(name: str, t: torch.Tensor) -> int:
 
 
 def _gpu(name: str, t: torch.Tensor) -> int:
-    """The index of the GPU that a call's first tensor is on."""
+    """The index of the GPU that a call's tensors are on."""
     i = t.get_device()
     if i < 0:
         raise ValueError(f"{name} must be on a GPU")
@@ -121,42 +119,28 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 _current_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _handle(stream, gpu: int) -> int:
-    return _current_raw_stream(gpu) if stream is None else stream.cuda_stream
-
-
 _current_device = torch._C._cuda_getDevice
 
 
-def _on_its_gpu(fn):
-    """Runs ``fn`` with the GPU of its first argument (a tensor or Mx4) as the
-    current one, where the library launches (the default stream's handle is the
-    same on every GPU), and with the call's stream as the current one, so that what
-    the call allocates is memory of that stream's order: memory of another
-    stream's pool may still be in use by that stream's pending work."""
-    names = list(inspect.signature(fn).parameters)
-    name, at = names[0], names.index("stream") if "stream" in names else len(names)
-
-    @functools.wraps(fn)
-    def call(*args, **kw):
-        first = args[0] if args else kw[name]
-        gpu = (first.codes if isinstance(first, Mx4) else first).get_device()
-        if gpu >= 0:  # (else refused by fn)
-            stream = args[at] if len(args) > at else kw.get("stream")
-            if stream is not None:
-                if stream.device_index != gpu:
-                    raise ValueError(f"stream is on cuda:{stream.device_index}, {name} on cuda:{gpu}")
-                caller = torch.cuda.current_stream(gpu)
-                with torch.cuda.stream(stream):
-                    out = fn(*args, **kw)
-                _record(out, caller)
-                return out
-            if gpu != _current_device():
-                with torch.cuda.device(gpu):
-                    return fn(*args, **kw)
-        return fn(*args, **kw)
-
-    return call
+def _there(fn, gpu: int, stream, args: dict):
+    """``fn`` again, of the same arguments (its locals(), ``gpu`` among them), with the
+    GPU of its tensors as the current one, where the library launches (the default
+    stream's handle is the same on every GPU), and with the call's stream as the
+    current one, so that what the call allocates is memory of that stream's order:
+    memory of another stream's pool may still be in use by that stream's pending
+    work."""
+    del args["gpu"]
+    if stream is None:
+        with torch.cuda.device(gpu):
+            return fn(**args)
+    if stream.device_index != gpu:
+        raise ValueError(f"stream is on cuda:{stream.device_index}, the tensors on cuda:{gpu}")
+    args["stream"] = None
+    caller = torch.cuda.current_stream(gpu)
+    with torch.cuda.stream(stream):
+        out = fn(**args)
+    _record(out, caller)
+    return out
 
 
 def _record(out, stream):
@@ -167,14 +151,6 @@ def _record(out, stream):
             _record(v, stream)
     elif hasattr(out, "record_stream"):
         out.record_stream(stream)
-
-
-class Mx4(NamedTuple):
-    """4-bit values: codes uint8 [..., Kp / 2], scales uint8 [..., Kp / 32], and
-    the K values of a row."""
-    codes: torch.Tensor
-    scales: torch.Tensor
-    K: int
 
 
 def _workspace(given: Optional[torch.Tensor], need: int, like: torch.Tensor):
@@ -198,7 +174,6 @@ def _norm_layer(h, y, x_dtype, w_pre, w_post, scale, gate, residual_scale, eps, 
                        _arg("scale", scale, (d,), wt, gpu), _arg("gate", gate, (T,), torch.float32, gpu))
 
 
-@_on_its_gpu
 def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Optional[torch.Tensor] = None,
                w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                gate: Optional[torch.Tensor] = None, slot_row: Optional[torch.Tensor] = None,
@@ -214,6 +189,8 @@ def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Opti
     if h.dim() != 2:
         raise ValueError("h must be [T][d]")
     gpu = _gpu("h", h)
+    if stream is not None or gpu != _current_device():
+        return _there(block_norm, gpu, stream, locals())
     T, d = shape = h.shape
     k = y_rows = 0
     yp = None
@@ -241,7 +218,7 @@ def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Opti
                              _arg("slot_row", slot_row, (T, k), torch.int32, gpu),
                              _arg("slot_weights", slot_weights, (T, k), torch.float32, gpu),
                              _arg("h_out", h_out, shape, h.dtype, gpu), _arg("x", x, shape, None, gpu),
-                             _handle(stream, gpu))
+                             _current_raw_stream(gpu))
     if st:
         _check(st)
     return (h if y is None else h_out), x
@@ -256,7 +233,6 @@ class BlockNormGrads(NamedTuple):
     dscale: Optional[torch.Tensor]
 
 
-@_on_its_gpu
 def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Optional[torch.Tensor],
                         dh_out: Optional[torch.Tensor] = None, *, w_pre: Optional[torch.Tensor] = None,
                         w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
@@ -270,6 +246,8 @@ def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Opti
     if h_out.dim() != 2:
         raise ValueError("h_out must be [T][d]")
     gpu = _gpu("h_out", h_out)
+    if stream is not None or gpu != _current_device():
+        return _there(block_norm_backward, gpu, stream, locals())
     T, d = shape = h_out.shape
     if (dx is None) != (w_pre is None):
         raise ValueError("dx goes with w_pre")
@@ -291,14 +269,13 @@ def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Opti
         ctypes.byref(s), T, _arg("h_out", h_out, shape, None, gpu), _arg("y", y, shape, None, gpu),
         _arg("dx", dx, shape, None, gpu), _arg("dh_out", dh_out, shape, h_out.dtype, gpu),
         _arg("dh", dh, shape, h_out.dtype, gpu), _arg("dy", dy, shape, None if y is None else y.dtype, gpu),
-        _ptr(dgate), _ptr(dw_pre), _ptr(dw_post), _ptr(dscale), ws, n, _handle(stream, gpu))
+        _ptr(dgate), _ptr(dw_pre), _ptr(dw_post), _ptr(dscale), ws, n, _current_raw_stream(gpu))
     if st:
         _check(st)
     return BlockNormGrads(dh, dy, dgate, dw_pre, dw_post, dscale)
 
 
 # ------------------------------------------------------------ balance loss
-@_on_its_gpu
 def route_topk_logits(x: torch.Tensor, w_r: torch.Tensor, k: int, *, workspace: Optional[torch.Tensor] = None,
                       stream=None):
     """The router with its logits (lx_route_topk_logits): bf16 x [T][d], w_r [E][d]
@@ -306,6 +283,8 @@ def route_topk_logits(x: torch.Tensor, w_r: torch.Tensor, k: int, *, workspace: 
     if x.dim() != 2 or w_r.dim() != 2:
         raise ValueError("x must be [T][d] and w_r [E][d]")
     gpu = _gpu("x", x)
+    if stream is not None or gpu != _current_device():
+        return _there(route_topk_logits, gpu, stream, locals())
     T, d = x.shape
     E = w_r.shape[0]
     ids, weights = x.new_empty((T, k), dtype=torch.int32), x.new_empty((T, k), dtype=torch.float32)
@@ -314,7 +293,7 @@ def route_topk_logits(x: torch.Tensor, w_r: torch.Tensor, k: int, *, workspace: 
     keep, ws, n = _workspace(workspace, L.lx_route_workspace_bytes(T, d, E), x)
     st = L.lx_route_topk_logits(_arg("x", x, (T, d), torch.bfloat16, gpu), _arg("w_r", w_r, (E, d), torch.bfloat16, gpu),
                                 LX_BF16, T, d, E, k, ids.data_ptr(), weights.data_ptr(), logits.data_ptr(), ws, n,
-                                _handle(stream, gpu))
+                                _current_raw_stream(gpu))
     if st:
         _check(st)
     return ids, weights, logits
@@ -333,7 +312,6 @@ def _mask_arg(mask, T, gpu):
     return _arg("mask", mask, (T,), torch.uint8, gpu)
 
 
-@_on_its_gpu
 def balance_loss(logits: torch.Tensor, topk_ids: torch.Tensor, *, mask: Optional[torch.Tensor] = None,
                  coef: float = 1.0, workspace: Optional[torch.Tensor] = None, stream=None) -> BalanceLoss:
     """The balance loss of router logits [T][E] (fp32 or bf16) and the chosen
@@ -342,6 +320,8 @@ def balance_loss(logits: torch.Tensor, topk_ids: torch.Tensor, *, mask: Optional
     if logits.dim() != 2 or topk_ids.dim() != 2:
         raise ValueError("logits must be [T][E] and topk_ids [T][k]")
     gpu = _gpu("logits", logits)
+    if stream is not None or gpu != _current_device():
+        return _there(balance_loss, gpu, stream, locals())
     T, E = logits.shape
     k = topk_ids.shape[1]
     r = BalanceLoss(logits.new_empty((1,), dtype=torch.float32), logits.new_empty((E,), dtype=torch.int32),
@@ -351,13 +331,12 @@ def balance_loss(logits: torch.Tensor, topk_ids: torch.Tensor, *, mask: Optional
     st = L.lx_balance_loss(_arg("logits", logits, (T, E), None, gpu), _dtype("logits", logits), T, E,
                            _arg("topk_ids", topk_ids, (T, k), torch.int32, gpu), k, _mask_arg(mask, T, gpu), coef,
                            r.loss.data_ptr(), r.counts.data_ptr(), r.prob.data_ptr(), r.n_tokens.data_ptr(), ws, n,
-                           _handle(stream, gpu))
+                           _current_raw_stream(gpu))
     if st:
         _check(st)
     return r
 
 
-@_on_its_gpu
 def balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_tokens: torch.Tensor, k: int, *,
                           mask: Optional[torch.Tensor] = None, coef: float = 1.0,
                           dloss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
@@ -368,6 +347,8 @@ def balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_tokens: 
     if logits.dim() != 2:
         raise ValueError("logits must be [T][E]")
     gpu = _gpu("logits", logits)
+    if stream is not None or gpu != _current_device():
+        return _there(balance_loss_backward, gpu, stream, locals())
     T, E = shape = logits.shape
     if dlogits is None:
         dlogits = logits.new_empty(shape, dtype=logits.dtype)
@@ -377,7 +358,7 @@ def balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_tokens: 
         _arg("logits", logits, shape, None, gpu), _dtype("logits", logits), T, E, k, _mask_arg(mask, T, gpu),
         _arg("counts", counts, (E,), torch.int32, gpu), _arg("n_tokens", n_tokens, (1,), torch.int32, gpu), coef,
         _arg("dloss", dloss, (1,), torch.float32, gpu), _arg("dlogits", dlogits, shape, logits.dtype, gpu),
-        _handle(stream, gpu))
+        _current_raw_stream(gpu))
     if st:
         _check(st)
     return dlogits
@@ -389,12 +370,21 @@ def mx4_padded(K: int) -> int:
     return -(-K // 128) * 128
 
 
-@_on_its_gpu
+class Mx4(NamedTuple):
+    """4-bit values: codes uint8 [..., Kp / 2], scales uint8 [..., Kp / 32], and
+    the K values of a row."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    K: int
+
+
 def mx4_quantize(x: torch.Tensor, *, act: int = MX4_NONE, out: Optional[Mx4] = None, stream=None) -> Mx4:
     """x [..., K] fp32 or bf16 -> 4-bit values (lx_mx4_quantize). With
     ``act=MX4_SWIGLU`` x is [..., 2K], the gate and up projections of a SwiGLU
     expert, and silu(gate) * up is rounded."""
     gpu = _gpu("x", x)
+    if stream is not None or gpu != _current_device():
+        return _there(mx4_quantize, gpu, stream, locals())
     if x.dim() < 1 or not x.is_contiguous():
         raise ValueError("x must be contiguous with at least one dimension")
     lead, K = x.shape[:-1], x.shape[-1]
@@ -410,17 +400,18 @@ def mx4_quantize(x: torch.Tensor, *, act: int = MX4_NONE, out: Optional[Mx4] = N
     elif out.K != K:
         raise ValueError("out.K does not fit x")
     st = lib().lx_mx4_quantize(x.data_ptr(), _dtype("x", x), rows, K, act, _arg("codes", out.codes, cs, torch.uint8, gpu),
-                               _arg("scales", out.scales, ss, torch.uint8, gpu), _handle(stream, gpu))
+                               _arg("scales", out.scales, ss, torch.uint8, gpu), _current_raw_stream(gpu))
     if st:
         _check(st)
     return out
 
 
-@_on_its_gpu
 def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, *, out: Optional[torch.Tensor] = None,
                    stream=None) -> torch.Tensor:
     """The values [..., K] of 4-bit codes (lx_mx4_dequantize), exact in both types."""
     gpu = _gpu("codes", q.codes)
+    if stream is not None or gpu != _current_device():
+        return _there(mx4_dequantize, gpu, stream, locals())
     lead, K = q.codes.shape[:-1], q.K
     Kp = mx4_padded(K)
     shape = (*lead, K)
@@ -428,13 +419,12 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, *, out: Optional
         out = q.codes.new_empty(shape, dtype=dtype)
     st = lib().lx_mx4_dequantize(_arg("codes", q.codes, (*lead, Kp // 2), torch.uint8, gpu),
                                  _arg("scales", q.scales, (*lead, Kp // 32), torch.uint8, gpu), lead.numel(), K,
-                                 _arg("out", out, shape, None, gpu), _dtype("out", out), _handle(stream, gpu))
+                                 _arg("out", out, shape, None, gpu), _dtype("out", out), _current_raw_stream(gpu))
     if st:
         _check(st)
     return out
 
 
-@_on_its_gpu
 def mx4_gemm(a: Mx4, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map: Optional[torch.Tensor] = None,
              out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
              workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -443,6 +433,8 @@ def mx4_gemm(a: Mx4, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map:
     group of all rows); row_map int32 [M] (None: row m of a). Rows past
     offsets[G] are left as they are."""
     gpu = _gpu("a", a.codes)
+    if stream is not None or gpu != _current_device():
+        return _there(mx4_gemm, gpu, stream, locals())
     ac, bc, K = a.codes, b.codes, a.K
     if ac.dim() != 2 or bc.dim() not in (2, 3):
         raise ValueError("a must be [rows][K] and b [G][N][K] or [N][K]")
@@ -463,7 +455,7 @@ def mx4_gemm(a: Mx4, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map:
                        _arg("b codes", bc, (*lead, Kp // 2), torch.uint8, gpu),
                        _arg("b scales", b.scales, (*lead, Kp // 32), torch.uint8, gpu),
                        _arg("offsets", offsets, (G + 1,), torch.int32, gpu), G, M, N, K,
-                       _arg("out", out, (M, N), None, gpu), _dtype("out", out), ws, n, _handle(stream, gpu))
+                       _arg("out", out, (M, N), None, gpu), _dtype("out", out), ws, n, _current_raw_stream(gpu))
     if st:
         _check(st)
     return out
@@ -477,13 +469,14 @@ class Mx4Experts(NamedTuple):
     down: Mx4
 
 
-@_on_its_gpu
 def mx4_experts(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, stream=None) -> Mx4Experts:
     """Experts w_gate, w_up [E][f][d], w_down [E][d][f] rounded to 4 bits, once
     when a model is loaded; all of it in ``stream``, the joining of the projections
     too."""
-    return Mx4Experts(mx4_quantize(torch.cat([w_gate, w_up], dim=1), stream=stream),
-                      mx4_quantize(w_down.contiguous(), stream=stream))
+    gpu = _gpu("w_gate", w_gate)
+    if stream is not None or gpu != _current_device():
+        return _there(mx4_experts, gpu, stream, locals())
+    return Mx4Experts(mx4_quantize(torch.cat([w_gate, w_up], dim=1)), mx4_quantize(w_down.contiguous()))
 
 
 class Mx4BlockOut(NamedTuple):
@@ -496,7 +489,6 @@ class Mx4BlockOut(NamedTuple):
     balance: Optional[BalanceLoss]
 
 
-@_on_its_gpu
 def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, experts: Mx4Experts, k: int, *,
                   w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                   gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0, eps: float = 1e-6,
@@ -509,12 +501,15 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
     [E][d] bf16 (d a multiple of 64, E of 4); the other arguments as in
     :func:`block_norm`. With ``balance_coef`` the router's logits and balance
     loss too (tokens whose ``mask`` is 0 left out)."""
+    gpu = _gpu("h", h)
+    if gpu != _current_device():
+        return _there(mx4_moe_block, gpu, None, locals())
     T, d = h.shape
     E = experts.gate_up.codes.shape[0]
     f = experts.down.K
     if w_r.shape != (E, d) or experts.down.codes.shape[:2] != (E, d) or experts.gate_up.codes.shape[1] != 2 * f:
         raise ValueError("w_r must be [E][d], the experts [E][2f][d] and [E][d][f] for h [T][d]")
-    if w_r.get_device() != _gpu("h", h):
+    if w_r.get_device() != gpu:
         raise ValueError(f"w_r is on {w_r.device}, h on {h.device}")
     _, x = block_norm(h, w_pre=w_pre, eps=eps)
     logits = balance = None
@@ -548,7 +543,7 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
     offsets = h.new_empty(E + 1, dtype=torch.int32)
     slot_row = h.new_empty((T, k), dtype=torch.int32)
     _check(L.lx_bucket(ctypes.byref(tree), T, k, ids.data_ptr(), 0, row_token.data_ptr(), offsets.data_ptr(),
-                       slot_row.data_ptr(), ws.data_ptr(), n, _handle(None, h.get_device())))
+                       slot_row.data_ptr(), ws.data_ptr(), n, _current_raw_stream(gpu)))
     gate_up = mx4_gemm(mx4_quantize(x), experts.gate_up, offsets=offsets, row_map=row_token, out_dtype=torch.bfloat16)
     y = mx4_gemm(mx4_quantize(gate_up, act=MX4_SWIGLU), experts.down, offsets=offsets, out_dtype=torch.float32)
     h_out, x_next = block_norm(h, y, w_pre=w_next, w_post=w_post, scale=scale, gate=gate, slot_row=slot_row,
