@@ -15,6 +15,10 @@ from paper_2608_07814_amd import lorex as lx
 class Stream:
     def __init__(self, gpu, handle):
         self.device_index, self.cuda_stream = gpu, handle
+        self.stream_id, self.device_type = handle, 1
+
+    def __eq__(self, other):
+        return (self.device_index, self.cuda_stream) == (other.device_index, other.cuda_stream)
 
 
 class Tensor:
@@ -78,12 +82,9 @@ class World:
         yield
         self.device = before
 
-    @contextlib.contextmanager
-    def on_stream(self, stream):
-        with self.on_device(stream.device_index):
-            before, self.current[stream.device_index] = self.current[stream.device_index], stream
-            yield
-            self.current[stream.device_index] = before
+    def set_stream(self, stream_id, device_index, device_type):
+        self.device = device_index
+        self.current[device_index] = Stream(device_index, stream_id)
 
     def __getattr__(self, name):  # the library
         if not name.startswith("lx_"):
@@ -105,8 +106,9 @@ def world(monkeypatch):
     monkeypatch.setattr(lb, "lib", lambda: w)
     monkeypatch.setattr(lx, "lib", lambda: w)
     monkeypatch.setattr(torch.cuda, "device", w.on_device)
-    monkeypatch.setattr(torch.cuda, "stream", w.on_stream)
-    monkeypatch.setattr(torch.cuda, "current_stream", w.stream)
+    monkeypatch.setattr(torch, "Stream", lambda stream_id, device_index, device_type: Stream(device_index, stream_id))
+    monkeypatch.setattr(lb, "_current_stream", lambda gpu: (w.stream(gpu).stream_id, gpu, 1))
+    monkeypatch.setattr(lb, "_set_stream", w.set_stream)
     monkeypatch.setattr(lb, "_current_raw_stream", lambda gpu: w.stream(gpu).cuda_stream)
     monkeypatch.setattr(lb, "_current_device", lambda: w.device, raising=False)
     return w
@@ -194,13 +196,13 @@ def test_memory_of_a_call_is_in_its_streams_order(world, entry):
     ((_, _, handle, used),) = world.calls
     assert handle == 77 and world.made
     for t in world.made:
-        assert t.pool is side
+        assert t.pool == side
     new = [t for t in out if t.pool is not None]
     assert new and all(caller in t.recorded for t in new)
     assert {id(t) for t in used if t.pool is not None} >= {id(t) for t in new}
     world.made.clear()
     calls(world, 0)[entry]()
-    assert world.made and all(t.pool is caller for t in world.made)
+    assert world.made and all(t.pool == caller for t in world.made)
 
 
 def test_experts_are_rounded_in_one_stream(world, monkeypatch):
@@ -222,17 +224,17 @@ def test_experts_are_rounded_in_one_stream(world, monkeypatch):
     w = Tensor(world, (8, 128, 128), BF16, 0)
     for give in (lambda: lb.mx4_experts(w, w, w, side), lambda: lb.mx4_experts(w, w, w, stream=side)):
         ex = give()
-        assert len(where) >= 2 and all(s is side for s in where)
-        assert [c[2] for c in world.calls] == [77, 77] and all(t.pool is side for t in world.made)
+        assert len(where) >= 2 and all(s == side for s in where)
+        assert [c[2] for c in world.calls] == [77, 77] and all(t.pool == side for t in world.made)
         assert all(caller in t.recorded for t in tensors(ex)) and len(tensors(ex)) == 4
         for v in (where, world.calls, world.made):
             v.clear()
     lb.mx4_experts(w, w, w)
-    assert all(s is caller for s in where) and [c[2] for c in world.calls] == [0, 0]
+    assert all(s == caller for s in where) and [c[2] for c in world.calls] == [0, 0]
     where.clear()
     w.gpu = 1
     lb.mx4_experts(w, w, w)
-    assert {c[1] for c in world.calls[2:]} == {1} and all(s is world.current[1] for s in where)
+    assert {c[1] for c in world.calls[2:]} == {1} and all(s == world.current[1] for s in where)
     with pytest.raises(ValueError):
         lb.mx4_experts(w, w, w, side)
 

@@ -55,3 +55,23 @@ def test_calls_leave_memory_of_pending_work_alone():
     assert torch.equal(got, ref)
     torch.cuda.synchronize()
     assert all(bool((t == 3).all()) for t in copies)
+
+
+def test_outputs_are_not_reused_before_the_callers_stream_is_done():
+    """An output that the caller's stream still reads when it is dropped is not given
+    to the call's stream's next allocation."""
+    require_gpu()
+    side = torch.cuda.Stream()
+    x, z = torch.randn(1 << 14, 1024, device="cuda"), torch.zeros(1 << 14, 1024, device="cuda")
+    busy = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    q = lb.mx4_quantize(x, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(20):
+        busy = busy @ busy * 1e-3
+    place, codes = q.codes.data_ptr(), q.codes.clone()  # (pending)
+    del q
+    again = lb.mx4_quantize(z, stream=side)
+    assert again.codes.data_ptr() != place
+    torch.cuda.synchronize()
+    assert torch.equal(codes, lb.mx4_quantize(x).codes)
