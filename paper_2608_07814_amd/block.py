@@ -16,7 +16,9 @@ are asynchronous on ``stream`` (a ``torch.cuda.Stream`` of that GPU; default: it
 current one). Outputs can be given; those that are not are allocated, as are
 workspaces, in the order of the call's stream: with ``stream`` the caller has
 that stream wait for inputs that another one makes, and its own stream wait for
-that one before it uses the outputs.
+that one before it uses the outputs. Autograd does not record these calls: their
+outputs have no graph, whatever requires gradients; the gradients are the
+``_backward`` calls.
 """
 from __future__ import annotations
 
@@ -549,6 +551,9 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
     slot_row = h.new_empty((T, k), dtype=torch.int32)
     _check(L.lx_bucket(ctypes.byref(tree), T, k, ids.data_ptr(), 0, row_token.data_ptr(), offsets.data_ptr(),
                        slot_row.data_ptr(), ws.data_ptr(), n, _current_raw_stream(gpu)))
+    # (gate and up projections are kept in bf16 on their way into SwiGLU: half of fp32's
+    # bytes of the block's widest rows, and their 2^-9 is small next to what follows,
+    # a rounding to 4 bits, whose steps are a quarter of a value and more)
     gate_up = mx4_gemm(mx4_quantize(x), experts.gate_up, offsets=offsets, row_map=row_token, out_dtype=torch.bfloat16)
     y = mx4_gemm(mx4_quantize(gate_up, act=MX4_SWIGLU), experts.down, offsets=offsets, out_dtype=torch.float32)
     h_out, x_next = block_norm(h, y, w_pre=w_next, w_post=w_post, scale=scale, gate=gate, slot_row=slot_row,

@@ -64,9 +64,11 @@ __device__ __forceinline__ void store_cols(void* p, bool f32, int64_t i, const C
 }
 
 // e^x for x <= 0 in fp32: the product with log2(e) is kept as a rounded value and
-// its remainder, so the relative error stays within a few 2^-24 for every x
-// (through the rounded product alone it grows to 100 times that at x = -80), at a
-// third of expf's instructions, which bound these kernels.
+// its remainder, so the relative error stays within a few 2^-24 where the result is a
+// normal number, x >= -87.3 (through the rounded product alone it grows to 100 times
+// that at x = -80), at a third of expf's instructions, which bound these kernels.
+// Below that the result is 0: the instruction gives no smaller numbers, and a
+// probability under 2^-126 is the choice of a softmax whose sum is at least 1.
 __device__ __forceinline__ float exp_down(float x) {
   constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596299e-8f, kLn2 = 0.693147181f;
   const float t = x * kLog2e;

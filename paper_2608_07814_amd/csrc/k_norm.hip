@@ -6,6 +6,7 @@
 // row sums go over lanes by DPP, over wavefronts through LDS. Workgroups stay
 // for many rows, so the weight vectors are read once per workgroup. Measured:
 // forward 8192 x 4096 (fp32 output of the block, bf16 streams) 68 us, 4.9 TB/s;
+// 4096 x 2048 with 8 experts' fp32 rows combined 57 us (319 MB, in part from cache);
 // backward 8192 x 4096 (fp32 stream) 126 us, 4.8 TB/s; a large copy reaches 5.45.
 #include "lx_block.h"
 #include "lx_vec.h"
