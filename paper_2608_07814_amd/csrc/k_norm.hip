@@ -221,9 +221,8 @@ __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) 
     r.m = r.y = r.D = r.dx = Raw{};
     if (col(i) < a.d && t < a.T) {
       const int64_t at = t * a.d + col(i);
-      // (without the second norm no gradient depends on h_out)
       if (a.y) r.y = load_as<Raw>(a.y, a.y_f32, at);
-      if (a.dx) {
+      if (a.dx) {  // (without the second norm no gradient depends on h_out)
         r.m = load_as<Raw>(a.h_out, a.h_f32, at);
         r.dx = load_as<Raw>(a.dx, a.x_f32, at);
       }
