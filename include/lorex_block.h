@@ -6,9 +6,13 @@
  *                  gate, its residual scale and the sum over a token's experts
  *   balance loss   the router's load-balance loss, the tokens per expert, and
  *                  the gradient of the logits
+ *   dropout        of the block's output inside these norms, from a
+ *                  counter-based generator: the mask is never stored
  *   4-bit values   rounding to OCP MXFP4 (blocks of 32 values with one
  *                  power-of-two scale), reading back, and products of two
  *                  4-bit operands, one weight matrix per group of rows
+ *   8-bit values   rounding to OCP MXFP8 (e4m3), also straight from the norms,
+ *                  and reading back
  *
  * The conventions of lorex.h hold: device pointers to dense row-major
  * caller-owned memory, asynchronous on `stream`, nothing allocated, no
@@ -79,6 +83,35 @@ lx_status lx_block_norm_backward(const lx_norm_layer* layer, int32_t T, const vo
                                  const void* dx, const void* dh_out, void* dh, void* dy, float* dgate,
                                  float* dw_pre, float* dw_post, float* dscale, void* workspace,
                                  size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------ dropout
+ * The block norms with the (normalised) block's output dropped out before gate
+ * and scale:
+ *
+ *   h_out  = residual_scale h + gate_t scale_c drop(v)_tc
+ *   drop(v)_tc = v_tc / (1 - q) if u_tc >= 65536 q, else 0 (whatever v_tc holds)
+ *
+ * with q = p rounded to a multiple of 2^-16, 0 <= q < 1 (p from 1 - 2^-17 on is
+ * refused), and 16 random bits u_tc from Philox4x32 of ten rounds: key = the
+ * seed (low word first), counter = (c / 8, t, offset low, offset high); u_tc is
+ * half c % 2 (0: the low one) of word (c % 8) / 2. rng: the seed and the offset,
+ * two 64-bit integers on the device, 8-byte aligned, read when the kernels run: a
+ * captured graph draws anew where the program moves the offset on between
+ * replays. Every (layer, step, rank) takes an offset or a seed of its own; the
+ * backward takes what the forward took and forms the mask again. p = 0 is the
+ * plain norm, rng is not read then. */
+typedef struct lx_dropout {
+  float p;
+  const int64_t* rng;        /* [2]: seed, offset */
+} lx_dropout;
+
+/* lx_block_norm without slots, lx_block_norm_backward; y must be given. */
+lx_status lx_block_norm_dropout(const lx_norm_layer* layer, const lx_dropout* dropout, int32_t T, const void* h,
+                                const void* y, void* h_out, void* x, void* stream);
+lx_status lx_block_norm_dropout_backward(const lx_norm_layer* layer, const lx_dropout* dropout, int32_t T,
+                                         const void* h_out, const void* y, const void* dx, const void* dh_out, void* dh,
+                                         void* dy, float* dgate, float* dw_pre, float* dw_post, float* dscale,
+                                         void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------ balance loss
  * lx_route_topk that leaves its logits [T][E] (fp32, 16-byte aligned) too: the
@@ -160,6 +193,37 @@ size_t lx_mx4_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t G);
 lx_status lx_mx4_gemm(const void* a, const void* a_scales, int32_t a_rows, const int32_t* row_map, const void* b,
                       const void* b_scales, const int32_t* offsets, int32_t G, int32_t M, int32_t N, int32_t K,
                       void* out, lx_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------ 8-bit values
+ * OCP Microscaling MXFP8: 32 consecutive values share the scale 2^(s - 127) (s an
+ * E8M0 byte, 255 = NaN) and are e4m3 codes. A row of K values (K a multiple of 8)
+ * is padded with zeros to Kp = LX_MX8_KP(K); its codes are Kp bytes, its scales
+ * Kp / 32. Rows follow each other without gaps. */
+#define LX_MX8_KP(K) (((K) + 127) / 128 * 128)
+
+/* x [rows][K] (LX_MX4_SWIGLU: [rows][2K]) -> codes [rows][Kp], scales
+ * [rows][Kp / 32], padding included. The scale is the smallest for which the
+ * block's largest magnitude is at most 448 scales, at least 2^-127: no value
+ * saturates. Values are rounded to the nearest code, ties to even. A block that
+ * holds an infinity or a NaN gets the scale NaN and codes 0. x 16-byte, codes
+ * 16-byte, scales 4-byte aligned. */
+lx_status lx_mx8_quantize(const void* x, lx_dtype dtype, int64_t rows, int32_t K, lx_mx4_act act, void* codes,
+                          void* scales, void* stream);
+
+/* codes, scales -> out [rows][K]: exact in both types (but for infinities from
+ * 2^128 on, and in bf16 for values below its smallest, 2^-133). */
+lx_status lx_mx8_dequantize(const void* codes, const void* scales, int64_t rows, int32_t K, void* out,
+                            lx_dtype dtype, void* stream);
+
+/* lx_block_norm whose x is rounded to 8 bits as lx_mx8_quantize rounds the
+ * unrounded fp32 x: codes [T][LX_MX8_KP(d)] (16-byte aligned) and scales
+ * [T][LX_MX8_KP(d) / 32] (4-byte aligned), padding included; both are given, as
+ * is w_pre, and layer.x_dtype is not looked at. Its gradients are
+ * lx_block_norm_backward's, from the gradient of the values (the rounding passes
+ * it on). */
+lx_status lx_block_norm_mx8(const lx_norm_layer* layer, int32_t T, const void* h, const void* y, int32_t y_rows,
+                            int32_t k, const int32_t* slot_row, const float* slot_weights, void* h_out, void* x_codes,
+                            void* x_scales, void* stream);
 
 #ifdef __cplusplus
 }

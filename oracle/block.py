@@ -20,8 +20,9 @@ def combine(Y, slot_row, slot_weights):
     return y, mag
 
 
-def block_norm(h, y, w_pre=None, w_post=None, scale=None, gate=None, residual_scale=1.0, eps=1e-6, y_mag=None):
-    """(h_out, x, magnitude of the terms of h_out, scale of x's error): fp64."""
+def block_norm(h, y, w_pre=None, w_post=None, scale=None, gate=None, residual_scale=1.0, eps=1e-6, y_mag=None, keep=None):
+    """(h_out, x, magnitude of the terms of h_out, scale of x's error): fp64. keep
+    [T][d]: the factors of dropout."""
     if y is None:
         out, mag = h, np.abs(h)
     else:
@@ -32,6 +33,8 @@ def block_norm(h, y, w_pre=None, w_post=None, scale=None, gate=None, residual_sc
             f = f * gate[:, None]
         if scale is not None:
             f = f * scale
+        if keep is not None:
+            f = f * keep
         out = residual_scale * h + f * y
         mag = np.abs(residual_scale * h) + np.abs(f) * (np.abs(y) if y_mag is None else y_mag)
     if w_pre is None:
@@ -40,7 +43,7 @@ def block_norm(h, y, w_pre=None, w_post=None, scale=None, gate=None, residual_sc
     return out, out * r * w_pre, mag, (mag + np.abs(out)) * r * np.abs(w_pre)
 
 
-def block_norm_grads(h_out, y, dx, dh_out, w_pre=None, w_post=None, scale=None, gate=None, residual_scale=1.0, eps=1e-6):
+def block_norm_grads(h_out, y, dx, dh_out, w_pre=None, w_post=None, scale=None, gate=None, residual_scale=1.0, eps=1e-6, keep=None):
     """{name: (gradient, sum of magnitudes of its terms)} in fp64."""
     D = np.zeros_like(h_out) if dh_out is None else dh_out.copy()
     A = np.abs(D)
@@ -56,22 +59,42 @@ def block_norm_grads(h_out, y, dx, dh_out, w_pre=None, w_post=None, scale=None, 
         return out
     out["dh"] = (residual_scale * D, abs(residual_scale) * A)
     g = 1.0 if gate is None else gate[:, None]
+    k = 1.0 if keep is None else keep
     s = 1.0 if scale is None else scale
     w = 1.0 if w_post is None else w_post
     ry = 1.0 if w_post is None else 1 / np.sqrt(np.mean(y * y, 1, keepdims=True) + eps)
     n = y * ry
     if gate is not None:
-        out["dgate"] = ((D * s * w * n).sum(1), (A * np.abs(s * w * n)).sum(1))
+        out["dgate"] = ((D * s * w * n * k).sum(1), (A * np.abs(s * w * n * k)).sum(1))
     if scale is not None:
-        out["dscale"] = ((D * g * w * n).sum(0), (A * np.abs(g * w * n)).sum(0))
-    dn = D * g * s * w
-    An = A * np.abs(g * s * w)
+        out["dscale"] = ((D * g * w * n * k).sum(0), (A * np.abs(g * w * n * k)).sum(0))
+    dn = D * g * s * w * k
+    An = A * np.abs(g * s * w * k)
     if w_post is not None:
-        out["dw_post"] = ((D * g * s * n).sum(0), (A * np.abs(g * s * n)).sum(0))
+        out["dw_post"] = ((D * g * s * n * k).sum(0), (A * np.abs(g * s * n * k)).sum(0))
         dn, An = (ry * (dn - n * np.mean(dn * n, 1, keepdims=True)),
                   ry * (An + np.abs(n) * np.mean(An * np.abs(n), 1, keepdims=True)))
     out["dy"] = (dn, An)
     return out
+
+
+# ---------------------------------------------------------------- dropout
+def dropout_keep(T, d, p, seed, offset):
+    """[T][d] factors: 0 where a value is dropped, 1 / (1 - q) where it is kept."""
+    q = int(p * 65536 + 0.5)
+    mask = (1 << 32) - 1
+    keep = np.empty((T, d))
+    for t in range(T):
+        for g in range(-(-d // 8)):
+            c = [g, t, offset & mask, offset >> 32 & mask]
+            k = [seed & mask, seed >> 32 & mask]
+            for _ in range(10):
+                a, b = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
+                c = [b >> 32 ^ c[1] ^ k[0], b & mask, a >> 32 ^ c[3] ^ k[1], a & mask]
+                k = [k[0] + 0x9E3779B9 & mask, k[1] + 0xBB67AE85 & mask]
+            for e in range(min(8, d - 8 * g)):
+                keep[t, 8 * g + e] = (c[e // 2] >> 16 * (e % 2) & 0xFFFF) >= q
+    return keep * (65536 / (65536 - q))
 
 
 # ---------------------------------------------------------------- balance loss
@@ -166,3 +189,38 @@ def gemm(a, b, M, offsets=None, row_map=None):
         if off[g + 1] > off[g]:
             out[off[g]:off[g + 1]] = A[off[g]:off[g + 1]] @ b[g].T
     return out
+
+
+# ---------------------------------------------------------------- 8-bit values
+GRID8 = np.array([c * 2.0 ** -9 if c < 8 else (8 + c % 8) * 2.0 ** (c // 8 - 10) for c in range(127)])  # e4m3 magnitudes
+MIDS8 = (GRID8[1:] + GRID8[:-1]) / 2
+
+
+def quantize8(x):
+    """fp64 [rows][K] -> (codes, scales, distance of each value to the nearest place
+    where its code changes, relative to the value)."""
+    rows, K = x.shape
+    b = np.zeros((rows, padded(K)))
+    b[:, :K] = x
+    b = b.reshape(rows, -1, 32)
+    top = np.abs(b).max(2)
+    bad = ~np.isfinite(top)
+    m, e = np.frexp(np.where(bad | (top == 0), 1.0, top))
+    s = np.where(top == 0, 0, np.clip(e - 9 + (m > 0.875) + 127, 0, 254))
+    q = np.where(bad[:, :, None], 0.0, b) / np.exp2(s - 127.0)[:, :, None]
+    a = np.abs(q)
+    assert a.max(initial=0) <= 448
+    lo, hi = np.searchsorted(MIDS8, a, side="left"), np.searchsorted(MIDS8, a, side="right")
+    code = np.where((lo != hi) & (lo % 2 == 1), hi, lo)  # on a midpoint the even one
+    near = np.clip(lo, 0, len(MIDS8) - 1)
+    dist = np.minimum(np.abs(a - MIDS8[near]), np.abs(a - MIDS8[np.maximum(near - 1, 0)]))
+    slack = dist / np.maximum(a, 2.0 ** -10)
+    code = np.where(np.signbit(q), code + 128, code)
+    code = np.where(bad[:, :, None], 0, code).reshape(rows, -1)
+    return code.astype(np.uint8), np.where(bad, 255, s).astype(np.uint8), slack.reshape(rows, -1)[:, :K]
+
+
+def dequantize8(codes, scales, K):
+    v = np.append(GRID8, np.nan)[codes & 127] * np.where(codes > 127, -1.0, 1.0)
+    s = np.where(scales == 255, np.nan, np.exp2(scales.astype(np.float64) - 127))
+    return (v * np.repeat(s, 32, -1))[..., :K]

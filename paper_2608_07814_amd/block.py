@@ -3,11 +3,15 @@
 
 * :func:`block_norm`, :func:`block_norm_backward`: the norms before and after a
   block with its gate and residual scale;
+* :func:`block_norm_dropout`, :func:`block_norm_dropout_backward`: the same with the
+  block's output dropped out;
+* :func:`block_norm_mx8`: the same with the next block's input in 8 bits;
 * :func:`route_topk_logits`: the router with its logits;
 * :func:`balance_loss`, :func:`balance_loss_backward`: the router's balance
   loss, the tokens per expert, the gradient of the logits;
 * :func:`mx4_quantize`, :func:`mx4_dequantize`, :func:`mx4_gemm`: microscaled
   4-bit values, and products of them per group of rows;
+* :func:`mx8_quantize`, :func:`mx8_dequantize`: microscaled 8-bit values;
 * :class:`Mx4Experts`, :func:`mx4_moe_block`: a MoE block whose experts are held
   in 4 bits, built from these and the library's router and bucketing.
 
@@ -42,7 +46,16 @@ class LxNormLayer(ctypes.Structure):
                 ("scale", _c_void), ("gate", _c_void)]
 
 
+class LxDropout(ctypes.Structure):
+    _fields_ = [("p", _c_f32), ("rng", _c_void)]
+
+
 EXPORTS = {
+    "lx_block_norm_mx8": (_c_i32, [_c_void, _c_i32, _c_void, _c_void, _c_i32, _c_i32] + [_c_void] * 6),
+    "lx_block_norm_dropout": (_c_i32, [_c_void, _c_void, _c_i32] + [_c_void] * 5),
+    "lx_block_norm_dropout_backward": (_c_i32, [_c_void, _c_void, _c_i32] + [_c_void] * 11 + [_c_size, _c_void]),
+    "lx_mx8_quantize": (_c_i32, [_c_void, _c_i32, _c_i64, _c_i32, _c_i32, _c_void, _c_void, _c_void]),
+    "lx_mx8_dequantize": (_c_i32, [_c_void, _c_void, _c_i64, _c_i32, _c_void, _c_i32, _c_void]),
     "lx_block_norm": (_c_i32, [_c_void, _c_i32, _c_void, _c_void, _c_i32, _c_i32] + [_c_void] * 5),
     "lx_block_norm_backward_workspace_bytes": (_c_size, [_c_i32, _c_i32]),
     "lx_block_norm_backward": (_c_i32, [_c_void, _c_i32] + [_c_void] * 11 + [_c_size, _c_void]),
@@ -171,6 +184,14 @@ def _workspace(given: Optional[torch.Tensor], need: int, like: torch.Tensor):
     return given, given.data_ptr(), given.numel()
 
 
+class Mx8(NamedTuple):
+    """8-bit values: codes uint8 [..., Kp], scales uint8 [..., Kp / 32], and the K
+    values of a row (Kp: :func:`mx4_padded`)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    K: int
+
+
 # ------------------------------------------------------------ block norms
 def _norm_layer(h, y, x_dtype, w_pre, w_post, scale, gate, residual_scale, eps, T, d, gpu) -> LxNormLayer:
     w = w_pre if w_pre is not None else w_post if w_post is not None else scale
@@ -198,6 +219,10 @@ def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Opti
     gpu = _gpu("h", h)
     if stream is not None or gpu != _current_device():
         return _there(block_norm, gpu, stream, locals())
+    return _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residual_scale, eps, h_out, x, x_dtype, None, gpu)
+
+
+def _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residual_scale, eps, h_out, x, x_dtype, dropout, gpu):
     T, d = shape = h.shape
     k = y_rows = 0
     yp = None
@@ -218,17 +243,73 @@ def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Opti
     if w_pre is None:
         if x is not None:
             raise ValueError("x goes with w_pre")
-    elif x is None:
+    elif x is None and x_dtype is not Mx8:
         x = h.new_empty(shape, dtype=x_dtype)
-    s = _norm_layer(h, y, LX_BF16 if x is None else _dtype("x", x), w_pre, w_post, scale, gate, residual_scale, eps, T, d, gpu)
-    st = lib().lx_block_norm(ctypes.byref(s), T, _arg("h", h, shape, None, gpu), yp, y_rows, k,
-                             _arg("slot_row", slot_row, (T, k), torch.int32, gpu),
-                             _arg("slot_weights", slot_weights, (T, k), torch.float32, gpu),
-                             _arg("h_out", h_out, shape, h.dtype, gpu), _arg("x", x, shape, None, gpu),
-                             _current_raw_stream(gpu))
+    s = _norm_layer(h, y, LX_BF16 if x is None or x_dtype is Mx8 else _dtype("x", x), w_pre, w_post, scale, gate, residual_scale, eps, T, d, gpu)
+    hp, op = _arg("h", h, shape, None, gpu), _arg("h_out", h_out, shape, h.dtype, gpu)
+    if x_dtype is Mx8:
+        Kp = mx4_padded(d)
+        if x is None:
+            x = Mx8(h.new_empty((T, Kp), dtype=torch.uint8), h.new_empty((T, Kp // 32), dtype=torch.uint8), d)
+        elif x.K != d:
+            raise ValueError("x.K does not fit h")
+        xp = _arg("x codes", x.codes, (T, Kp), torch.uint8, gpu), _arg("x scales", x.scales, (T, Kp // 32), torch.uint8, gpu)
+    else:
+        xp = (_arg("x", x, shape, None, gpu),)
+    if dropout is not None:
+        st = lib().lx_block_norm_dropout(ctypes.byref(s), ctypes.byref(dropout), T, hp, yp, op, *xp, _current_raw_stream(gpu))
+    else:
+        fn = lib().lx_block_norm_mx8 if x_dtype is Mx8 else lib().lx_block_norm
+        st = fn(ctypes.byref(s), T, hp, yp, y_rows, k, _arg("slot_row", slot_row, (T, k), torch.int32, gpu),
+                _arg("slot_weights", slot_weights, (T, k), torch.float32, gpu), op, *xp, _current_raw_stream(gpu))
     if st:
         _check(st)
     return (h if y is None else h_out), x
+
+
+def block_norm_mx8(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: torch.Tensor,
+                   w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                   gate: Optional[torch.Tensor] = None, slot_row: Optional[torch.Tensor] = None,
+                   slot_weights: Optional[torch.Tensor] = None, residual_scale: float = 1.0, eps: float = 1e-6,
+                   h_out: Optional[torch.Tensor] = None, x: Optional["Mx8"] = None, stream=None):
+    """:func:`block_norm` with x in 8 bits (lx_block_norm_mx8) -> (h_out, x): what
+    :func:`mx8_gemm` reads. In training its gradients are those of
+    :func:`block_norm_backward`, from the gradient of the values that x stands for."""
+    if h.dim() != 2:
+        raise ValueError("h must be [T][d]")
+    if w_pre is None:
+        raise ValueError("w_pre must be given")
+    gpu = _gpu("h", h)
+    if stream is not None or gpu != _current_device():
+        return _there(block_norm_mx8, gpu, stream, locals())
+    return _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residual_scale, eps, h_out, x, Mx8, None, gpu)
+
+
+def _dropout(p: float, rng: torch.Tensor, y, gpu) -> LxDropout:
+    if not 0 <= p < 1 - 2 ** -17:
+        raise ValueError("p must be in [0, 1 - 2^-17)")
+    if y is None:
+        raise ValueError("y must be given")
+    return LxDropout(p, _arg("rng", rng, (2,), torch.int64, gpu))
+
+
+def block_norm_dropout(h: torch.Tensor, y: torch.Tensor, p: float, rng: torch.Tensor, *, w_pre: Optional[torch.Tensor] = None,
+                       w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                       gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0, eps: float = 1e-6,
+                       h_out: Optional[torch.Tensor] = None, x: Optional[torch.Tensor] = None,
+                       x_dtype: torch.dtype = torch.bfloat16, stream=None):
+    """:func:`block_norm` without slots, the (normalised) block's output dropped out with
+    probability p before gate and scale (lx_block_norm_dropout). rng: int64 [2] on the
+    GPU, the generator's seed and offset, read when the kernel runs. Every layer, step
+    and rank takes an offset or a seed of its own (``rng[1] += 1`` between the replays of
+    a captured graph draws anew); the backward takes the same values."""
+    if h.dim() != 2:
+        raise ValueError("h must be [T][d]")
+    gpu = _gpu("h", h)
+    if stream is not None or gpu != _current_device():
+        return _there(block_norm_dropout, gpu, stream, locals())
+    return _block_norm(h, y, w_pre, w_post, scale, gate, None, None, residual_scale, eps, h_out, x, x_dtype,
+                       _dropout(p, rng, y, gpu), gpu)
 
 
 class BlockNormGrads(NamedTuple):
@@ -255,6 +336,10 @@ def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Opti
     gpu = _gpu("h_out", h_out)
     if stream is not None or gpu != _current_device():
         return _there(block_norm_backward, gpu, stream, locals())
+    return _block_norm_backward(h_out, y, dx, dh_out, w_pre, w_post, scale, gate, residual_scale, eps, dh, dy, workspace, None, gpu)
+
+
+def _block_norm_backward(h_out, y, dx, dh_out, w_pre, w_post, scale, gate, residual_scale, eps, dh, dy, workspace, dropout, gpu):
     T, d = shape = h_out.shape
     if (dx is None) != (w_pre is None):
         raise ValueError("dx goes with w_pre")
@@ -272,14 +357,35 @@ def block_norm_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], dx: Opti
     dw_pre, dw_post, dscale = (next(rows) if g else None for g in given)
     L = lib()
     keep, ws, n = _workspace(workspace, L.lx_block_norm_backward_workspace_bytes(T, d), h_out)
-    st = L.lx_block_norm_backward(
-        ctypes.byref(s), T, _arg("h_out", h_out, shape, None, gpu), _arg("y", y, shape, None, gpu),
+    fn, s = (L.lx_block_norm_backward, (ctypes.byref(s),)) if dropout is None else (
+        L.lx_block_norm_dropout_backward, (ctypes.byref(s), ctypes.byref(dropout)))
+    st = fn(
+        *s, T, _arg("h_out", h_out, shape, None, gpu), _arg("y", y, shape, None, gpu),
         _arg("dx", dx, shape, None, gpu), _arg("dh_out", dh_out, shape, h_out.dtype, gpu),
         _arg("dh", dh, shape, h_out.dtype, gpu), _arg("dy", dy, shape, None if y is None else y.dtype, gpu),
         _ptr(dgate), _ptr(dw_pre), _ptr(dw_post), _ptr(dscale), ws, n, _current_raw_stream(gpu))
     if st:
         _check(st)
     return BlockNormGrads(dh, dy, dgate, dw_pre, dw_post, dscale)
+
+
+def block_norm_dropout_backward(h_out: torch.Tensor, y: torch.Tensor, dx: Optional[torch.Tensor],
+                                dh_out: Optional[torch.Tensor], p: float, rng: torch.Tensor, *,
+                                w_pre: Optional[torch.Tensor] = None, w_post: Optional[torch.Tensor] = None,
+                                scale: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                                residual_scale: float = 1.0, eps: float = 1e-6, dh: Optional[torch.Tensor] = None,
+                                dy: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                stream=None) -> BlockNormGrads:
+    """Gradients of :func:`block_norm_dropout` (lx_block_norm_dropout_backward), with the
+    p and the values of rng that it took; the other arguments as in
+    :func:`block_norm_backward`."""
+    if h_out.dim() != 2:
+        raise ValueError("h_out must be [T][d]")
+    gpu = _gpu("h_out", h_out)
+    if stream is not None or gpu != _current_device():
+        return _there(block_norm_dropout_backward, gpu, stream, locals())
+    return _block_norm_backward(h_out, y, dx, dh_out, w_pre, w_post, scale, gate, residual_scale, eps, dh, dy, workspace,
+                                _dropout(p, rng, y, gpu), gpu)
 
 
 # ------------------------------------------------------------ balance loss
@@ -463,6 +569,53 @@ def mx4_gemm(a: Mx4, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map:
                        _arg("b scales", b.scales, (*lead, Kp // 32), torch.uint8, gpu),
                        _arg("offsets", offsets, (G + 1,), torch.int32, gpu), G, M, N, K,
                        _arg("out", out, (M, N), None, gpu), _dtype("out", out), ws, n, _current_raw_stream(gpu))
+    if st:
+        _check(st)
+    return out
+
+
+# ------------------------------------------------------------ 8-bit values
+def mx8_quantize(x: torch.Tensor, *, act: int = MX4_NONE, out: Optional[Mx8] = None, stream=None) -> Mx8:
+    """x [..., K] fp32 or bf16 -> 8-bit values (lx_mx8_quantize). With
+    ``act=MX4_SWIGLU`` x is [..., 2K], the gate and up projections of a SwiGLU
+    expert, and silu(gate) * up is rounded."""
+    gpu = _gpu("x", x)
+    if stream is not None or gpu != _current_device():
+        return _there(mx8_quantize, gpu, stream, locals())
+    if x.dim() < 1 or not x.is_contiguous():
+        raise ValueError("x must be contiguous with at least one dimension")
+    lead, K = x.shape[:-1], x.shape[-1]
+    if act == MX4_SWIGLU:
+        if K % 2:
+            raise ValueError("rows of gate and up projections have an even length")
+        K //= 2
+    Kp = mx4_padded(K)
+    cs, ss = (*lead, Kp), (*lead, Kp // 32)
+    if out is None:
+        out = Mx8(x.new_empty(cs, dtype=torch.uint8), x.new_empty(ss, dtype=torch.uint8), K)
+    elif out.K != K:
+        raise ValueError("out.K does not fit x")
+    st = lib().lx_mx8_quantize(x.data_ptr(), _dtype("x", x), lead.numel(), K, act, _arg("codes", out.codes, cs, torch.uint8, gpu),
+                               _arg("scales", out.scales, ss, torch.uint8, gpu), _current_raw_stream(gpu))
+    if st:
+        _check(st)
+    return out
+
+
+def mx8_dequantize(q: Mx8, dtype: torch.dtype = torch.bfloat16, *, out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """The values [..., K] of 8-bit codes (lx_mx8_dequantize)."""
+    gpu = _gpu("codes", q.codes)
+    if stream is not None or gpu != _current_device():
+        return _there(mx8_dequantize, gpu, stream, locals())
+    lead, K = q.codes.shape[:-1], q.K
+    Kp = mx4_padded(K)
+    shape = (*lead, K)
+    if out is None:
+        out = q.codes.new_empty(shape, dtype=dtype)
+    st = lib().lx_mx8_dequantize(_arg("codes", q.codes, (*lead, Kp), torch.uint8, gpu),
+                                 _arg("scales", q.scales, (*lead, Kp // 32), torch.uint8, gpu), lead.numel(), K,
+                                 _arg("out", out, shape, None, gpu), _dtype("out", out), _current_raw_stream(gpu))
     if st:
         _check(st)
     return out

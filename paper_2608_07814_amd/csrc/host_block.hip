@@ -6,6 +6,7 @@ namespace lx {
 namespace {
 
 bool al(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 bool dtype_ok(lx_dtype t) { return t == LX_F32 || t == LX_BF16; }
 
 template <class Args>
@@ -52,6 +53,85 @@ void norm_layer_args(A& a, const lx_norm_layer& p, int32_t T, bool block) {
   a.gate = block ? p.gate : nullptr;
 }
 
+lx_status norm_args(NormArgs& a, const lx_norm_layer* layer, int32_t T, const void* h, const void* y, int32_t y_rows,
+                    int32_t k, const int32_t* slot_row, const float* slot_weights, void* h_out, void* x) {
+  const lx_status st = check_norm(layer, T, y != nullptr);
+  if (st != LX_OK) return st;
+  if (!slot_row != !slot_weights) return set_error(LX_ERR_INVALID_ARGUMENT, "slot_row and slot_weights: both or neither");
+  if (slot_row && (k < 1 || k > LX_MAX_K || y_rows < 0))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "k must be in 1 .. LX_MAX_K and y_rows >= 0");
+  if (slot_row && (int64_t)T * k >= ((int64_t)1 << 31)) return set_error(LX_ERR_UNSUPPORTED, "T * k must be below 2^31");
+  if (!y && (slot_row || h_out)) return set_error(LX_ERR_INVALID_ARGUMENT, "slots and h_out need y");
+  if (T == 0) return LX_OK;
+  if (!y && !layer->w_pre) return set_error(LX_ERR_INVALID_ARGUMENT, "neither y nor w_pre is given");
+  if (!h || (y && !h_out) || !x != !layer->w_pre || !al(h, 16) || !al(y, 16) || !al(h_out, 16) || !al(x, 16) ||
+      !al(slot_row, 4) || !al(slot_weights, 4))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  norm_layer_args(a, *layer, T, y != nullptr);
+  a.h = h;
+  a.y = y;
+  a.y_rows = y_rows;
+  a.k = slot_row ? k : 0;
+  a.slot_row = slot_row;
+  a.slot_weights = slot_weights;
+  a.h_out = h_out;
+  a.x = x;
+  return LX_OK;
+}
+
+// A value is dropped where its 16 random bits are below p 65536, rounded.
+lx_status dropout_args(Dropout& d, const lx_dropout* p) {
+  if (!p || !(p->p >= 0.f) || !(p->p < 1.f - 1.f / 131072)) return set_error(LX_ERR_INVALID_ARGUMENT, "p must be in [0, 1 - 2^-17)");
+  if (!p->rng || !al(p->rng, 8)) return set_error(LX_ERR_INVALID_ARGUMENT, "rng null or misaligned");
+  d.below = (uint32_t)(p->p * 65536.f + 0.5f);
+  d.rng = d.below ? (const uint64_t*)p->rng : nullptr;
+  d.scale = 65536.f / (float)(65536 - d.below);
+  return LX_OK;
+}
+
+lx_status norm_backward(const lx_norm_layer* layer, const Dropout& drop, int32_t T, const void* h_out, const void* y,
+                        const void* dx, const void* dh_out, void* dh, void* dy, float* dgate, float* dw_pre,
+                        float* dw_post, float* dscale, void* workspace, size_t workspace_bytes, void* stream) {
+  const lx_status st = check_norm(layer, T, y != nullptr);
+  if (st != LX_OK) return st;
+  const lx_norm_layer& p = *layer;
+  if (!y && !p.w_pre) return set_error(LX_ERR_INVALID_ARGUMENT, "neither y nor w_pre is given");
+  if (!dw_pre != !p.w_pre || !dw_post != !(y && p.w_post) || !dscale != !(y && p.scale))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "dw_pre, dw_post and dscale go with w_pre, w_post and scale");
+  if (!al(dw_pre, 16) || !al(dw_post, 16) || !al(dscale, 16))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "misaligned pointer");
+  if (T > 0) {
+    if (!h_out || !dh || !dx != !p.w_pre || !dy != !y || !dgate != !(y && p.gate) || !al(h_out, 16) || !al(y, 16) ||
+        !al(dx, 16) || !al(dh_out, 16) || !al(dh, 16) || !al(dy, 16) || !al(dgate, 4))
+      return set_error(LX_ERR_INVALID_ARGUMENT, "null, superfluous or misaligned pointer");
+  }
+  if (!workspace || !al(workspace, 256)) return set_error(LX_ERR_INVALID_ARGUMENT, "workspace null or not 256-byte aligned");
+  NormGradArgs a{};
+  a.groups = norm_grad_groups(T, p.d);
+  if (workspace_bytes < up256((size_t)a.groups * 2 * p.d * sizeof(float)))
+    return set_error(LX_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than required");
+  norm_layer_args(a, p, T, y != nullptr);
+  a.drop = drop;
+  a.h_out = h_out;
+  a.y = y;
+  a.dx = dx;
+  a.dh_out = dh_out;
+  a.dh = dh;
+  a.dy = dy;
+  a.dgate = dgate;
+  a.dw_pre = dw_pre;
+  a.dw_post = dw_post;
+  a.dscale = dscale;
+  a.part = (float*)workspace;
+  if (T == 0) a.groups = 0;
+  if (T > 0) {
+    const lx_status s1 = run("block_norm_grad", launch_block_norm_grad, a, stream);
+    if (s1 != LX_OK) return s1;
+  }
+  if (!dw_pre && !dw_post && !dscale) return LX_OK;
+  return run("block_norm_grad_sum", launch_block_norm_grad_sum, a, stream);
+}
+
 lx_status check_balance(lx_dtype dtype, int32_t T, int32_t E, int32_t k) {
   if (T < 0) return set_error(LX_ERR_INVALID_ARGUMENT, "T must be >= 0");
   if (!dtype_ok(dtype)) return set_error(LX_ERR_INVALID_ARGUMENT, "bad dtype");
@@ -60,8 +140,6 @@ lx_status check_balance(lx_dtype dtype, int32_t T, int32_t E, int32_t k) {
   if ((int64_t)T * k >= ((int64_t)1 << 31)) return set_error(LX_ERR_UNSUPPORTED, "T * k must be below 2^31");
   return LX_OK;
 }
-
-size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 
 struct BalancePlan {
   int blocks;
@@ -108,29 +186,36 @@ lx_status lx_block_norm(const lx_norm_layer* layer, int32_t T, const void* h, co
                         int32_t k, const int32_t* slot_row, const float* slot_weights, void* h_out, void* x,
                         void* stream) {
   clear_error();
-  const lx_status st = check_norm(layer, T, y != nullptr);
-  if (st != LX_OK) return st;
-  if (!slot_row != !slot_weights) return set_error(LX_ERR_INVALID_ARGUMENT, "slot_row and slot_weights: both or neither");
-  if (slot_row && (k < 1 || k > LX_MAX_K || y_rows < 0))
-    return set_error(LX_ERR_INVALID_ARGUMENT, "k must be in 1 .. LX_MAX_K and y_rows >= 0");
-  if (slot_row && (int64_t)T * k >= ((int64_t)1 << 31)) return set_error(LX_ERR_UNSUPPORTED, "T * k must be below 2^31");
-  if (!y && (slot_row || h_out)) return set_error(LX_ERR_INVALID_ARGUMENT, "slots and h_out need y");
-  if (T == 0) return LX_OK;
-  if (!y && !layer->w_pre) return set_error(LX_ERR_INVALID_ARGUMENT, "neither y nor w_pre is given");
-  if (!h || (y && !h_out) || !x != !layer->w_pre || !al(h, 16) || !al(y, 16) || !al(h_out, 16) || !al(x, 16) ||
-      !al(slot_row, 4) || !al(slot_weights, 4))
-    return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
   NormArgs a{};
-  norm_layer_args(a, *layer, T, y != nullptr);
-  a.h = h;
-  a.y = y;
-  a.y_rows = y_rows;
-  a.k = slot_row ? k : 0;
-  a.slot_row = slot_row;
-  a.slot_weights = slot_weights;
-  a.h_out = h_out;
-  a.x = x;
-  return run("block_norm", launch_block_norm, a, stream);
+  const lx_status st = norm_args(a, layer, T, h, y, y_rows, k, slot_row, slot_weights, h_out, x);
+  return st != LX_OK || T == 0 ? st : run("block_norm", launch_block_norm, a, stream);
+}
+
+lx_status lx_block_norm_mx8(const lx_norm_layer* layer, int32_t T, const void* h, const void* y, int32_t y_rows,
+                            int32_t k, const int32_t* slot_row, const float* slot_weights, void* h_out, void* x_codes,
+                            void* x_scales, void* stream) {
+  clear_error();
+  if (!layer) return set_error(LX_ERR_INVALID_ARGUMENT, "layer is null");
+  lx_norm_layer l = *layer;
+  l.x_dtype = LX_BF16;
+  Norm8Args a{};
+  const lx_status st = norm_args(a, &l, T, h, y, y_rows, k, slot_row, slot_weights, h_out, x_codes);
+  if (st != LX_OK || T == 0) return st;
+  if (!l.w_pre) return set_error(LX_ERR_INVALID_ARGUMENT, "w_pre must be given");
+  if (!x_scales || !al(x_scales, 4)) return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  a.x_scales = (uint8_t*)x_scales;
+  return run("block_norm_mx8", launch_block_norm_mx8, a, stream);
+}
+
+lx_status lx_block_norm_dropout(const lx_norm_layer* layer, const lx_dropout* dropout, int32_t T, const void* h,
+                                const void* y, void* h_out, void* x, void* stream) {
+  clear_error();
+  NormArgs a{};
+  lx_status st = dropout_args(a.drop, dropout);
+  if (st == LX_OK) st = norm_args(a, layer, T, h, y, 0, 0, nullptr, nullptr, h_out, x);
+  if (st != LX_OK || T == 0) return st;
+  if (!y) return set_error(LX_ERR_INVALID_ARGUMENT, "y must be given");
+  return run("block_norm_dropout", launch_block_norm, a, stream);
 }
 
 size_t lx_block_norm_backward_workspace_bytes(int32_t T, int32_t d) {
@@ -147,43 +232,21 @@ lx_status lx_block_norm_backward(const lx_norm_layer* layer, int32_t T, const vo
                                  float* dw_pre, float* dw_post, float* dscale, void* workspace,
                                  size_t workspace_bytes, void* stream) {
   clear_error();
-  const lx_status st = check_norm(layer, T, y != nullptr);
+  return norm_backward(layer, Dropout{}, T, h_out, y, dx, dh_out, dh, dy, dgate, dw_pre, dw_post, dscale, workspace,
+                       workspace_bytes, stream);
+}
+
+lx_status lx_block_norm_dropout_backward(const lx_norm_layer* layer, const lx_dropout* dropout, int32_t T,
+                                         const void* h_out, const void* y, const void* dx, const void* dh_out, void* dh,
+                                         void* dy, float* dgate, float* dw_pre, float* dw_post, float* dscale,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  Dropout d{};
+  const lx_status st = dropout_args(d, dropout);
   if (st != LX_OK) return st;
-  const lx_norm_layer& p = *layer;
-  if (!y && !p.w_pre) return set_error(LX_ERR_INVALID_ARGUMENT, "neither y nor w_pre is given");
-  if (!dw_pre != !p.w_pre || !dw_post != !(y && p.w_post) || !dscale != !(y && p.scale))
-    return set_error(LX_ERR_INVALID_ARGUMENT, "dw_pre, dw_post and dscale go with w_pre, w_post and scale");
-  if (!al(dw_pre, 16) || !al(dw_post, 16) || !al(dscale, 16))
-    return set_error(LX_ERR_INVALID_ARGUMENT, "misaligned pointer");
-  if (T > 0) {
-    if (!h_out || !dh || !dx != !p.w_pre || !dy != !y || !dgate != !(y && p.gate) || !al(h_out, 16) || !al(y, 16) ||
-        !al(dx, 16) || !al(dh_out, 16) || !al(dh, 16) || !al(dy, 16) || !al(dgate, 4))
-      return set_error(LX_ERR_INVALID_ARGUMENT, "null, superfluous or misaligned pointer");
-  }
-  if (!workspace || !al(workspace, 256)) return set_error(LX_ERR_INVALID_ARGUMENT, "workspace null or not 256-byte aligned");
-  NormGradArgs a{};
-  a.groups = norm_grad_groups(T, p.d);
-  if (workspace_bytes < up256((size_t)a.groups * 2 * p.d * sizeof(float)))
-    return set_error(LX_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than required");
-  norm_layer_args(a, p, T, y != nullptr);
-  a.h_out = h_out;
-  a.y = y;
-  a.dx = dx;
-  a.dh_out = dh_out;
-  a.dh = dh;
-  a.dy = dy;
-  a.dgate = dgate;
-  a.dw_pre = dw_pre;
-  a.dw_post = dw_post;
-  a.dscale = dscale;
-  a.part = (float*)workspace;
-  if (T == 0) a.groups = 0;
-  if (T > 0) {
-    const lx_status s1 = run("block_norm_grad", launch_block_norm_grad, a, stream);
-    if (s1 != LX_OK) return s1;
-  }
-  if (!dw_pre && !dw_post && !dscale) return LX_OK;
-  return run("block_norm_grad_sum", launch_block_norm_grad_sum, a, stream);
+  if (T > 0 && !y) return set_error(LX_ERR_INVALID_ARGUMENT, "y must be given");
+  return norm_backward(layer, d, T, h_out, y, dx, dh_out, dh, dy, dgate, dw_pre, dw_post, dscale, workspace,
+                       workspace_bytes, stream);
 }
 
 size_t lx_balance_loss_workspace_bytes(int32_t T, int32_t E) {
@@ -293,6 +356,46 @@ lx_status lx_mx4_dequantize(const void* codes, const void* scales, int64_t rows,
   a.codes = (uint8_t*)codes;
   a.scales = (uint8_t*)scales;
   return run("mx4_dequantize", launch_mx4_dequantize, a, stream);
+}
+
+lx_status lx_mx8_quantize(const void* x, lx_dtype dtype, int64_t rows, int32_t K, lx_mx4_act act, void* codes,
+                          void* scales, void* stream) {
+  clear_error();
+  const lx_status st = check_mx4(rows, K);
+  if (st != LX_OK) return st;
+  if (!dtype_ok(dtype) || (act != LX_MX4_NONE && act != LX_MX4_SWIGLU))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "bad dtype or act");
+  if (rows == 0) return LX_OK;
+  if (!x || !codes || !scales || !al(x, 16) || !al(codes, 16) || !al(scales, 4))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  Mx4Args a{};
+  a.x = x;
+  a.rows = rows;
+  a.K = K;
+  a.f32 = dtype == LX_F32;
+  a.swiglu = act == LX_MX4_SWIGLU;
+  a.codes = (uint8_t*)codes;
+  a.scales = (uint8_t*)scales;
+  return run("mx8_quantize", launch_mx8_quantize, a, stream);
+}
+
+lx_status lx_mx8_dequantize(const void* codes, const void* scales, int64_t rows, int32_t K, void* out,
+                            lx_dtype dtype, void* stream) {
+  clear_error();
+  const lx_status st = check_mx4(rows, K);
+  if (st != LX_OK) return st;
+  if (!dtype_ok(dtype)) return set_error(LX_ERR_INVALID_ARGUMENT, "bad dtype");
+  if (rows == 0) return LX_OK;
+  if (!out || !codes || !scales || !al(out, 16) || !al(codes, 16) || !al(scales, 4))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  Mx4Args a{};
+  a.x = out;
+  a.rows = rows;
+  a.K = K;
+  a.f32 = dtype == LX_F32;
+  a.codes = (uint8_t*)codes;
+  a.scales = (uint8_t*)scales;
+  return run("mx8_dequantize", launch_mx8_dequantize, a, stream);
 }
 
 size_t lx_mx4_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t G) {

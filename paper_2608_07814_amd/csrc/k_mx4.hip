@@ -2,6 +2,8 @@
 // products on the block-scaled matrix instructions (layout and rules in
 // lorex_block.h).
 #include "lx_block.h"
+#include "lx_groups.h"
+#include "lx_rowwise.h"
 #include "lx_vec.h"
 
 #include <algorithm>
@@ -18,12 +20,6 @@ constexpr int kBlk = 32;  // values under one scale
 // quotient (32768 rows of 768 in bf16 42 us, 2.7 TB/s; 8192 of 14336 155, 3.4). A lane has 8 values of a row (4 lanes
 // share a block of 32), TPR lanes a row, and U rows under way at once; there is no
 // division by the row length.
-template <int U, class F>
-__device__ __forceinline__ void for_rows(int64_t rows, int vecs, int tpr, F&& f) {
-  const int lt = threadIdx.x & (tpr - 1), rpb = 256 / tpr;
-  for (int64_t r = (int64_t)blockIdx.x * rpb * U + (int)threadIdx.x / tpr; r < rows; r += (int64_t)gridDim.x * rpb * U)
-    for (int v = lt; v < vecs; v += tpr) f(r, rpb, v * 8);
-}
 
 // Rounding: the largest magnitude of a block goes over its 4 lanes as bits: as
 // unsigned integers magnitudes keep their order, and infinities and NaNs come
@@ -119,82 +115,6 @@ __global__ __launch_bounds__(256) void k_mx4_dequantize(const Mx4Args a, int tpr
 typedef int v8i __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ v8i frag(const uint4& q) { return v8i{(int)q.x, (int)q.y, (int)q.z, (int)q.w, 0, 0, 0, 0}; }
-
-// Inclusive prefix sum over the 64 lanes (all active): row shifts within 16
-// lanes, then the totals of the rows before.
-__device__ __forceinline__ int lane_prefix(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-  const int r0 = __builtin_amdgcn_readlane(x, 15), r1 = __builtin_amdgcn_readlane(x, 31),
-            r2 = __builtin_amdgcn_readlane(x, 47), row = (threadIdx.x & 63) >> 4;
-  return x + (row >= 1 ? r0 : 0) + (row >= 2 ? r1 : 0) + (row >= 3 ? r2 : 0);
-}
-
-// A group's rows, clamped to [0, M].
-__device__ __forceinline__ void group_rows(const Mx4GemmArgs& a, int g, int& lo, int& hi) {
-  lo = hi = 0;
-  if (g < a.G) {
-    lo = min(max(a.offsets[g], 0), a.M);
-    hi = min(max(a.offsets[g + 1], lo), a.M);
-  }
-}
-
-// Row tiles over all groups (tiles of BM rows counted group by group).
-template <int BM>
-__device__ __forceinline__ int count_tiles(const Mx4GemmArgs& a) {
-  if (!a.offsets) return (a.M + BM - 1) / BM;
-  int n = 0;
-#pragma unroll 4
-  for (int g0 = 0; g0 < a.G; g0 += 64) {
-    int lo, hi;
-    group_rows(a, g0 + (threadIdx.x & 63), lo, hi);
-    n += (hi - lo + BM - 1) / BM;
-  }
-  return __builtin_amdgcn_readlane(lane_prefix(n), 63);
-}
-
-// The group and the rows of row tile `tile`, found by each wavefront: 64 groups
-// at a time, a prefix sum of their tile counts over the lanes. false: there is no
-// such tile. All results are uniform.
-template <int BM>
-__device__ __forceinline__ bool find_tile(const Mx4GemmArgs& a, int tile, int& g, int& m0, int& m1) {
-  if (!a.offsets) {
-    g = 0;
-    m0 = tile * BM;
-    m1 = min(m0 + BM, a.M);
-    return m0 < a.M;
-  }
-#pragma unroll 4
-  for (int g0 = 0; g0 < a.G; g0 += 64) {
-    int lo, hi;
-    group_rows(a, g0 + (threadIdx.x & 63), lo, hi);
-    const int n = (hi - lo + BM - 1) / BM, sum = lane_prefix(n), all = __builtin_amdgcn_readlane(sum, 63);
-    if (tile < all) {
-      const int src = __builtin_ctzll(__ballot(tile < sum));
-      g = g0 + src;
-      m0 = __builtin_amdgcn_readlane(lo, src) + (tile - __builtin_amdgcn_readlane(sum - n, src)) * BM;
-      m1 = min(m0 + BM, __builtin_amdgcn_readlane(hi, src));
-      return true;
-    }
-    tile -= all;
-  }
-  return false;
-}
-
-// The work items of one workgroup: workgroups go round the 8 XCDs, and XCD x
-// takes a contiguous range of all items.
-struct Items {
-  int64_t at, end, step;
-  __device__ __forceinline__ Items(int64_t all) {
-    const int x = blockIdx.x & 7;
-    const int64_t per = all / 8, rest = all % 8, first = x * per + min((int64_t)x, rest);
-    at = first + (blockIdx.x >> 3);
-    end = first + per + (x < rest);
-    step = gridDim.x >> 3;
-  }
-};
 
 // ---------------------------------------------------------------- few rows
 // Four scale words of a row: 16 bytes at the words' own alignment. Read word by
@@ -306,30 +226,6 @@ __global__ __launch_bounds__(256) void k_mx4_gemm_rows(const Mx4GemmArgs a) {
 
 // ---------------------------------------------------------------- large tiles
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __attribute__((address_space(3))) void lds_void_t;
-
-// One direct memory -> LDS load per lane: lane i fills LDS bytes [dst + SIZE i,
-// + SIZE) from base + its own 32-bit byte offset (base and dst are uniform).
-// Inline asm, so that the only waits on it are the ones written below; M0 is
-// written here only, and the s_nop is the wait state that the load needs after
-// a write of M0.
-template <int SIZE>
-__device__ __forceinline__ void load_lds(const void* base, uint32_t off, const void* dst) {
-  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)dst);
-  if constexpr (SIZE == 16)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory");
-  else
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory");
-}
-
-// All of this wavefront's loads have landed and its LDS reads are done, then
-// every wavefront's.
-__device__ __forceinline__ void land_and_meet() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
 // BM x BN outputs per workgroup, a 2 x 2 grid of wavefronts (256 x 256: 2 x 4, two
 // wavefronts per SIMD: one multiplies while the other waits for LDS or the barrier,
 // and twice as many write results out; against 2 x 2 with twice the accumulators
@@ -708,17 +604,6 @@ __global__ __launch_bounds__(256) void k_mx4_gemm_sum(const Mx4GemmArgs a) {
 }
 
 }  // namespace
-
-// Lanes of a row for `vecs` groups of 8 values, workgroups for U rows at a time.
-static int row_lanes(int vecs) {
-  int n = 1;
-  while (n < vecs && n < 256) n *= 2;
-  return n;
-}
-static int row_grid(int64_t rows, int tpr, int U) {
-  const int64_t per = 256 / tpr * U;
-  return (int)std::min<int64_t>((rows + per - 1) / per, 1 << 16);
-}
 
 hipError_t launch_mx4_quantize(const Mx4Args& a, hipStream_t s) {
   const int tpr = row_lanes(LX_MX4_KP(a.K) / 8);

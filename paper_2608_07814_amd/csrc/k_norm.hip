@@ -9,6 +9,7 @@
 // 4096 x 2048 with 8 experts' fp32 rows combined 57 us (319 MB, in part from cache);
 // backward 8192 x 4096 (fp32 stream) 126 us, 4.8 TB/s; a large copy reaches 5.45.
 #include "lx_block.h"
+#include "lx_norm_rows.h"
 #include "lx_vec.h"
 
 #include <algorithm>
@@ -18,152 +19,12 @@
 namespace lx {
 namespace {
 
-// Sums of N values over the TPR lanes of a row. With more than one wavefront
-// per row each call takes LDS slots of its own (`lds`, N per wavefront of the
-// workgroup), so that one barrier per call is enough.
-template <int TPR, int N>
-__device__ __forceinline__ void row_sums(float (&x)[N], float* lds) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = lane_sum<64>(x[i]);
-  if constexpr (TPR > 64) {
-    constexpr int NW = TPR / 64;
-    const int wave = threadIdx.x >> 6, w0 = wave / NW * NW;
-    if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) lds[wave * N + i] = x[i];
-    }
-    __syncthreads();
-    // each lane takes one wavefront's sum
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = lds[(w0 + threadIdx.x % NW) * N + i];
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = lane_sum<NW>(x[i]);
-  }
-}
-
-__device__ __forceinline__ float rms(float sum, int d, float eps) { return 1.f / sqrtf(sum / (float)d + eps); }
-
-// Forward workgroups: 256 threads, or one row's if it needs more.
-template <int TPR>
-constexpr int kFwdThreads = TPR < 256 ? 256 : TPR;
-
-template <int TPR, int NV>
+template <int TPR, int NV, bool DROP = false>
 __global__ __launch_bounds__(kFwdThreads<TPR>) void k_block_norm(const NormArgs a) {
-  constexpr int RPB = kFwdThreads<TPR> / TPR, NW = kFwdThreads<TPR> / 64;
-  __shared__ float lds[2 * NW];
-  const int lt = threadIdx.x % TPR;
-  int col[NV];
-  bool in[NV];
-  F8 sw[NV], wp[NV];  // scale w_post; w_pre
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    col[i] = (i * TPR + lt) * 8;
-    in[i] = col[i] < a.d;
-    sw[i] = wp[i] = F8{{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}};
-    if (in[i]) {
-      if (a.w_pre) wp[i] = load8(a.w_pre, a.w_f32, col[i]);
-      if (a.w_post) sw[i] = load8(a.w_post, a.w_f32, col[i]);
-      if (a.scale) {
-        const F8 q = load8(a.scale, a.w_f32, col[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sw[i].v[e] *= q.v[e];
-      }
-    }
-  }
-  // (all rows of the workgroup run as many rounds: the barriers need them. The
-  // row's index stays one value per lane: uniform, the slots' loads go through the
-  // scalar cache, and one token's 8 slots at d = 1024 take 4.7 us for 4.3)
-  const int g = (int)threadIdx.x / TPR;
-  for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < a.T; t0 += (int64_t)gridDim.x * RPB) {
-    const int64_t t = t0 + g;
-    const bool live = RPB == 1 || t < a.T;
-    const int64_t row = t * a.d;
-    Raw8 rh[NV], ry[NV];
-    F8 h[NV], y[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      rh[i] = ry[i] = Raw8{};
-      if (in[i] && live) {
-        rh[i] = load_raw8(a.h, a.h_f32, row + col[i]);
-        if (a.y && !a.slot_row) ry[i] = load_raw8(a.y, a.y_f32, row + col[i]);
-      }
-    }
-    if (a.y) {
-      const float gate = a.gate && live ? a.gate[t] : 1.f;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) y[i] = a.slot_row ? F8{} : unpack8(ry[i], a.y_f32);
-      if (a.slot_row && a.y_rows > 0 && live) {
-        // four slots' rows at a time; a dropped slot reads row 0 and adds nothing
-        for (int j0 = 0; j0 < a.k; j0 += 4) {
-          int r[4];
-          float w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            r[j] = j0 + j < a.k ? a.slot_row[t * a.k + j0 + j] : -1;
-            w[j] = j0 + j < a.k ? a.slot_weights[t * a.k + j0 + j] : 0.f;
-            if (r[j] >= a.y_rows) r[j] = -1;
-          }
-#pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            Raw8 q[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              q[j] = Raw8{};
-              if (in[i]) q[j] = load_raw8(a.y, a.y_f32, (int64_t)max(r[j], 0) * a.d + col[i]);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (r[j] >= 0) {
-                const F8 v = unpack8(q[j], a.y_f32);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[i].v[e] += w[j] * v.v[e];
-              }
-          }
-        }
-      }
-      float f = gate;
-      if (a.w_post) {
-        float s[1] = {0.f};
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s[0] += y[i].v[e] * y[i].v[e];
-        row_sums<TPR>(s, lds);
-        f *= rms(s[0], a.d, a.eps);
-      }
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        h[i] = unpack8(rh[i], a.h_f32);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[i].v[e] = a.alpha * h[i].v[e] + f * (y[i].v[e] * sw[i].v[e]);
-        if (in[i] && live) store8(a.h_out, a.h_f32, row + col[i], h[i]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) h[i] = unpack8(rh[i], a.h_f32);
-    }
-    if (a.w_pre) {
-      float s[1] = {0.f};
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[0] += in[i] ? h[i].v[e] * h[i].v[e] : 0.f;
-      row_sums<TPR>(s, lds + NW);
-      const float r = rms(s[0], a.d, a.eps);
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (in[i] && live) {
-          F8 x;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x.v[e] = h[i].v[e] * r * wp[i].v[e];
-          store8(a.x, a.x_f32, row + col[i], x);
-        }
-    }
-    // without both sums a row has one barrier or none: the next row may only
-    // write the slots when all have read them
-    if constexpr (TPR > 64)
-      if (!(a.y && a.w_post && a.w_pre)) __syncthreads();
-  }
+  __shared__ float lds[2 * kFwdThreads<TPR> / 64];
+  block_norm_rows<TPR, NV, DROP>(a, lds, [&](int64_t t, int col, bool in, bool live, const F8& x) __attribute__((always_inline)) {
+    if (in && live) store8(a.x, a.x_f32, t * a.d + col, x);
+  });
 }
 
 // Backward. With m = h' r_h, n = y r_y (no w_post: n = y, r_y = 1), D the
@@ -188,7 +49,7 @@ constexpr int kBwd = 1024;
 __device__ __forceinline__ void again(RawB8& r) { asm volatile("" : "+v"(r.a)); }
 __device__ __forceinline__ void again(Raw8& r) { asm volatile("" : "+v"(r.a), "+v"(r.b)); }
 
-template <bool BF, int TPR, int NV, bool KEEP>
+template <bool BF, int TPR, int NV, bool KEEP, bool DROP = false>
 __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) {
   constexpr int RPB = kBwd / TPR, NW = kBwd / 64;
   using Raw = std::conditional_t<BF, RawB8, Raw8>;
@@ -230,6 +91,8 @@ __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) 
     }
     return r;
   };
+  DropoutKeys keys{};
+  if constexpr (DROP) keys = dropout_keys(a.drop);
   F8 sp[NV], sq[NV];
   Weights w[KEEP ? NV : 1];
 #pragma unroll
@@ -244,12 +107,22 @@ __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) 
   for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < a.T; t0 += stride, slots ^= 6 * NW) {
     const int64_t t = t0 + g, row = t * a.d;
     const bool live = t < a.T;
+    // with dropout: the columns that are kept, formed as in the forward; a dropped
+    // value counts as 0 whatever it holds
+    auto mask = [&](int i) __attribute__((always_inline)) {
+      if constexpr (DROP) return dropout_kept(a.drop, keys, col(i) / 8, (uint32_t)t);
+      return 0u;
+    };
+    auto drop = [&](float v, uint32_t kept, int e) __attribute__((always_inline)) {
+      if constexpr (DROP) return kept >> e & 1 ? v * a.drop.scale : 0.f;
+      return v;
+    };
     float s[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    auto add = [&](const Row& q, const Weights& w) __attribute__((always_inline)) {
+    auto add = [&](const Row& q, const Weights& w, uint32_t kept) __attribute__((always_inline)) {
       const F8 m = unpack8(q.m, a.h_f32), y = unpack8(q.y, a.y_f32), D = unpack8(q.D, a.h_f32), dx = unpack8(q.dx, a.x_f32);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float dm = dx.v[e] * w.pre.v[e], sy = w.s.v[e] * y.v[e];
+        const float dm = dx.v[e] * w.pre.v[e], sy = w.s.v[e] * drop(y.v[e], kept, e);
         s[0] += m.v[e] * m.v[e];
         s[1] += y.v[e] * y.v[e];
         s[2] += dm * m.v[e];
@@ -258,15 +131,16 @@ __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) 
         s[5] += m.v[e] * sy;
       }
     };
+    uint32_t kept[KEEP ? NV : 1];
     Row q[KEEP ? NV : 1];
     if constexpr (KEEP) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) q[i] = load(i, t);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) add(q[i], w[i]);
+      for (int i = 0; i < NV; ++i) add(q[i], w[i], kept[i] = mask(i));
     } else {
 #pragma unroll 1
-      for (int i = 0; i < NV; ++i) add(load(i, t), weights(i));
+      for (int i = 0; i < NV; ++i) add(load(i, t), weights(i), mask(i));
     }
     const float gate = a.gate && live ? a.gate[t] : 1.f;
     row_sums<TPR>(s, lds + slots);
@@ -288,19 +162,19 @@ __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) 
         again(q[i].dx);
       }
     }
-    auto give = [&](int i, const Row& q, const Weights& w) __attribute__((always_inline)) {
+    auto give = [&](int i, const Row& q, const Weights& w, uint32_t kept) __attribute__((always_inline)) {
       const F8 m = unpack8(q.m, a.h_f32), y = unpack8(q.y, a.y_f32), D = unpack8(q.D, a.h_f32), dx = unpack8(q.dx, a.x_f32);
       F8 dh, dy;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float mm = m.v[e] * rh, n = y.v[e] * ry, d = D.v[e] + rh * (dx.v[e] * w.pre.v[e] - mm * mean);
         sp[i].v[e] += dx.v[e] * mm;
-        sq[i].v[e] += gate * d * n;
+        sq[i].v[e] += gate * d * drop(n, kept, e);
         dh.v[e] = alpha * d;
         // (without w_post zn is 0 and dy does not depend on y, which may be infinite or
         // NaN: its product with 0 must not count. With w_post zn is NaN then. A
         // choice by a.w_post took 71 for 62 us at 1024 x 16384)
-        dy.v[e] = ry * gate * (d * w.s.v[e] - __builtin_amdgcn_fmed3f(n, -FLT_MAX, FLT_MAX) * zn);
+        dy.v[e] = ry * gate * (d * drop(w.s.v[e], kept, e) - __builtin_amdgcn_fmed3f(n, -FLT_MAX, FLT_MAX) * zn);
       }
       if (col(i) < a.d && live) {
         store8(a.dh, a.h_f32, row + col(i), dh);
@@ -310,10 +184,10 @@ __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if constexpr (KEEP) {
-        give(i, q[i], w[i]);
+        give(i, q[i], w[i], kept[i]);
       } else {
         asm volatile("" ::: "memory");  // (one group's loads at a time)
-        give(i, load(i, t), weights(i));
+        give(i, load(i, t), weights(i), mask(i));
       }
     }
   }
@@ -393,7 +267,10 @@ hipError_t launch_block_norm(const NormArgs& a, hipStream_t s) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, THR = kFwdThreads<TPR>;
     constexpr int RPB = THR / TPR;
     const int grid = (int)std::min<int64_t>(((int64_t)a.T + RPB - 1) / RPB, 256 * (2048 / THR));
-    k_block_norm<TPR, NV><<<grid, THR, 0, s>>>(a);
+    if (a.drop.rng)
+      k_block_norm<TPR, NV, true><<<grid, THR, 0, s>>>(a);
+    else
+      k_block_norm<TPR, NV><<<grid, THR, 0, s>>>(a);
     return hipGetLastError();
   });
 }
@@ -411,10 +288,13 @@ hipError_t launch_block_norm_grad(const NormGradArgs& a, hipStream_t s) {
   const bool bf = !a.h_f32 && (!a.y || !a.y_f32) && (!a.dx || !a.x_f32);
   return by_width(a.d, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
-    if (bf)
-      k_block_norm_grad<true, TPR, NV, NV == 1><<<a.groups, kBwd, 0, s>>>(a);
+    auto go = [&](auto b, auto drop) {
+      k_block_norm_grad<decltype(b)::value, TPR, NV, NV == 1, decltype(drop)::value><<<a.groups, kBwd, 0, s>>>(a);
+    };
+    if (a.drop.rng)
+      bf ? go(std::true_type{}, std::true_type{}) : go(std::false_type{}, std::true_type{});
     else
-      k_block_norm_grad<false, TPR, NV, NV == 1><<<a.groups, kBwd, 0, s>>>(a);
+      bf ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{});
     return hipGetLastError();
   });
 }

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "lx_internal.h"
+#include "lx_philox.h"
 #include "lorex_block.h"
 
 namespace lx {
@@ -27,8 +28,14 @@ struct NormArgs {
   const int32_t* slot_row;
   const float* slot_weights;
   void *h_out, *x;
+  Dropout drop;      // of the block's output (rng null: none)
 };
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t s);
+// The same with x in 8 bits: x the codes, x_scales their scales.
+struct Norm8Args : NormArgs {
+  uint8_t* x_scales;
+};
+hipError_t launch_block_norm_mx8(const Norm8Args& a, hipStream_t s);
 
 struct NormGradArgs {
   int32_t T, d;
@@ -41,6 +48,7 @@ struct NormGradArgs {
   float *dgate, *dw_pre, *dw_post, *dscale;
   float* part;       // [groups][2][d]: sums of dx m and of gate D n
   int32_t groups;
+  Dropout drop;      // as in the forward
 };
 // Workgroups of the backward, each with its partial weight gradients.
 int norm_grad_groups(int T, int d);
@@ -87,6 +95,9 @@ struct Mx4Args {
 hipError_t launch_mx4_quantize(const Mx4Args& a, hipStream_t s);
 // x is the output of the reading back
 hipError_t launch_mx4_dequantize(const Mx4Args& a, hipStream_t s);
+// The same with 8-bit values (LX_MX8_KP codes of a byte a row).
+hipError_t launch_mx8_quantize(const Mx4Args& a, hipStream_t s);
+hipError_t launch_mx8_dequantize(const Mx4Args& a, hipStream_t s);
 
 // Which kernel a product runs on, and into how many parts its K is split (each
 // but the last of split_steps steps of 256 values).
