@@ -11,6 +11,8 @@
  *   4-bit values   rounding to OCP MXFP4 (blocks of 32 values with one
  *                  power-of-two scale), reading back, and products of two
  *                  4-bit operands, one weight matrix per group of rows
+ *   few tokens     a whole layer of experts in 4 bits for decoding, in two
+ *                  launches
  *   8-bit values   rounding to OCP MXFP8 (e4m3), also straight from the norms,
  *                  and reading back
  *
@@ -193,6 +195,31 @@ size_t lx_mx4_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t G);
 lx_status lx_mx4_gemm(const void* a, const void* a_scales, int32_t a_rows, const int32_t* row_map, const void* b,
                       const void* b_scales, const int32_t* offsets, int32_t G, int32_t M, int32_t N, int32_t K,
                       void* out, lx_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------ few tokens
+ * A layer of experts in 4 bits for up to LX_MOE_FEW_MAX_T tokens, in two launches:
+ *
+ *   out[t] = sum_j weights[t][j] down_e (silu(gate_e x_t) * (up_e x_t)),  e = ids[t][j]
+ *
+ * x [T][d] (fp32 or bf16) is not rounded; ids [T][k] int32 and weights [T][k] fp32
+ * as lx_route_topk writes them: a slot whose id is outside [0, E) adds nothing,
+ * a token may name an expert more than once, a token without any slot gets
+ * zeros. gate_up: codes and scales of E x [2f][d] (gate rows first), down: of E
+ * x [d][f]. Only the chosen experts' weights are read, each once per 16 of its
+ * tokens; a NaN scale or an infinite activation reaches the tokens that it is
+ * multiplied for only. Weights below 2^-126 under a block's scale may count as 0.
+ * Sums are formed in fp32; with a bf16 out the activations between the two
+ * products keep 16 bits (next to the 8 of the result), with fp32 all 24. out
+ * [T][d]. d and f multiples of 8, at most 2^20, E in 1 .. LX_MAX_NODES, k in 1 ..
+ * LX_MAX_K (LX_ERR_UNSUPPORTED; T over the most as well). All 16-byte aligned but
+ * ids, weights and scales (4); workspace 256-byte aligned, as many bytes as the
+ * function before says. */
+#define LX_MOE_FEW_MAX_T 64
+size_t lx_mx4_moe_few_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t d, int32_t f);
+lx_status lx_mx4_moe_few(const void* x, lx_dtype x_dtype, int32_t T, int32_t d, const int32_t* topk_ids,
+                         const float* topk_weights, int32_t k, int32_t E, int32_t f, const void* gate_up,
+                         const void* gate_up_scales, const void* down, const void* down_scales, void* out,
+                         lx_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------ 8-bit values
  * OCP Microscaling MXFP8: 32 consecutive values share the scale 2^(s - 127) (s an

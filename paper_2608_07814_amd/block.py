@@ -36,6 +36,7 @@ from .lorex import LX_BF16, LX_F32, _check
 
 MX4_NONE, MX4_SWIGLU = 0, 1
 NORM_MAX_D = 32768
+MOE_FEW_MAX_T = 64
 
 _c_void, _c_i32, _c_i64, _c_f32, _c_size = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 
@@ -51,6 +52,9 @@ class LxDropout(ctypes.Structure):
 
 
 EXPORTS = {
+    "lx_mx4_moe_few_workspace_bytes": (_c_size, [_c_i32] * 5),
+    "lx_mx4_moe_few": (_c_i32, [_c_void, _c_i32, _c_i32, _c_i32, _c_void, _c_void, _c_i32, _c_i32, _c_i32] + [_c_void] * 5
+                       + [_c_i32, _c_void, _c_size, _c_void]),
     "lx_block_norm_mx8": (_c_i32, [_c_void, _c_i32, _c_void, _c_void, _c_i32, _c_i32] + [_c_void] * 6),
     "lx_block_norm_dropout": (_c_i32, [_c_void, _c_void, _c_i32] + [_c_void] * 5),
     "lx_block_norm_dropout_backward": (_c_i32, [_c_void, _c_void, _c_i32] + [_c_void] * 11 + [_c_size, _c_void]),
@@ -637,6 +641,42 @@ def mx4_experts(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, 
     if stream is not None or gpu != _current_device():
         return _there(mx4_experts, gpu, stream, locals())
     return Mx4Experts(mx4_quantize(torch.cat([w_gate, w_up], dim=1)), mx4_quantize(w_down.contiguous()))
+
+
+def mx4_moe_few(x: torch.Tensor, topk_ids: torch.Tensor, topk_weights: torch.Tensor, experts: Mx4Experts, *,
+                out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
+                workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The experts' layer for up to ``MOE_FEW_MAX_T`` tokens in two launches
+    (lx_mx4_moe_few): x [T][d] (fp32 or bf16, not rounded), topk_ids and topk_weights
+    [T][k] as the router gives them -> the weighted sum of the experts' outputs
+    [T][d]."""
+    if x.dim() != 2 or topk_ids.dim() != 2:
+        raise ValueError("x must be [T][d] and topk_ids [T][k]")
+    gpu = _gpu("x", x)
+    if stream is not None or gpu != _current_device():
+        return _there(mx4_moe_few, gpu, stream, locals())
+    T, d = x.shape
+    k = topk_ids.shape[1]
+    gu, down = experts
+    E, f = down.codes.shape[0], down.K
+    if gu.K != d:
+        raise ValueError(f"x has {d} values in a row, the experts {gu.K}")
+    dp, fp = mx4_padded(d), mx4_padded(f)
+    if out is None:
+        out = x.new_empty((T, d), dtype=out_dtype)
+    L = lib()
+    keep, ws, n = _workspace(workspace, L.lx_mx4_moe_few_workspace_bytes(T, k, E, d, f), x)
+    u8 = torch.uint8
+    st = L.lx_mx4_moe_few(_arg("x", x, (T, d), None, gpu), _dtype("x", x), T, d, _arg("topk_ids", topk_ids, (T, k), torch.int32, gpu),
+                          _arg("topk_weights", topk_weights, (T, k), torch.float32, gpu), k, E, f,
+                          _arg("gate_up codes", gu.codes, (E, 2 * f, dp // 2), u8, gpu),
+                          _arg("gate_up scales", gu.scales, (E, 2 * f, dp // 32), u8, gpu),
+                          _arg("down codes", down.codes, (E, d, fp // 2), u8, gpu),
+                          _arg("down scales", down.scales, (E, d, fp // 32), u8, gpu),
+                          _arg("out", out, (T, d), None, gpu), _dtype("out", out), ws, n, _current_raw_stream(gpu))
+    if st:
+        _check(st)
+    return out
 
 
 class Mx4BlockOut(NamedTuple):

@@ -2,6 +2,8 @@
 // launches. Nothing here allocates or throws.
 #include "lx_block.h"
 
+#include <algorithm>
+
 namespace lx {
 namespace {
 
@@ -169,6 +171,29 @@ lx_status check_mx4_gemm(int32_t M, int32_t N, int32_t K, int32_t G) {
   if (M > INT32_MAX - 255 || N > INT32_MAX - 255) return set_error(LX_ERR_UNSUPPORTED, "M and N must be at most 2^31 - 256");
   if ((int64_t)M * N >= ((int64_t)1 << 40)) return set_error(LX_ERR_UNSUPPORTED, "M * N must be below 2^40");
   return LX_OK;
+}
+
+lx_status check_few(int32_t T, int32_t k, int32_t E, int32_t d, int32_t f) {
+  if (T < 0 || d < 1 || f < 1) return set_error(LX_ERR_INVALID_ARGUMENT, "T must be >= 0; d and f positive");
+  if (T > LX_MOE_FEW_MAX_T) return set_error(LX_ERR_UNSUPPORTED, "T must be at most LX_MOE_FEW_MAX_T");
+  if (d % 8 || f % 8 || d > (1 << 20) || f > (1 << 20)) return set_error(LX_ERR_UNSUPPORTED, "d and f must be multiples of 8, at most 2^20");
+  if (E < 1 || E > LX_MAX_NODES || k < 1 || k > LX_MAX_K)
+    return set_error(LX_ERR_UNSUPPORTED, "E must be in 1 .. LX_MAX_NODES, k in 1 .. LX_MAX_K");
+  return LX_OK;
+}
+
+struct FewPlan {
+  int32_t units;
+  size_t mask, expert, row, hidden, total;
+};
+FewPlan few_plan(int32_t T, int32_t k, int32_t E, int32_t f) {
+  FewPlan p{};
+  p.units = std::min(E, T * k);
+  p.expert = p.mask + up256((size_t)p.units * 8);
+  p.row = p.expert + up256((size_t)p.units * 4);
+  p.hidden = p.row + up256((size_t)p.units * 64 * 4);
+  p.total = p.hidden + up256((size_t)T * k * 3 * f * 2);
+  return p;
 }
 
 size_t mx4_gemm_bytes(const Mx4GemmPlan& p, int M, int N) {
@@ -356,6 +381,54 @@ lx_status lx_mx4_dequantize(const void* codes, const void* scales, int64_t rows,
   a.codes = (uint8_t*)codes;
   a.scales = (uint8_t*)scales;
   return run("mx4_dequantize", launch_mx4_dequantize, a, stream);
+}
+
+size_t lx_mx4_moe_few_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t d, int32_t f) {
+  clear_error();
+  if (check_few(T, k, E, d, f) != LX_OK) return 0;
+  return few_plan(T, k, E, f).total;
+}
+
+lx_status lx_mx4_moe_few(const void* x, lx_dtype x_dtype, int32_t T, int32_t d, const int32_t* topk_ids,
+                         const float* topk_weights, int32_t k, int32_t E, int32_t f, const void* gate_up,
+                         const void* gate_up_scales, const void* down, const void* down_scales, void* out,
+                         lx_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  const lx_status st = check_few(T, k, E, d, f);
+  if (st != LX_OK) return st;
+  if (!dtype_ok(x_dtype) || !dtype_ok(out_dtype)) return set_error(LX_ERR_INVALID_ARGUMENT, "bad dtype");
+  if (T == 0) return LX_OK;
+  if (!x || !topk_ids || !topk_weights || !gate_up || !gate_up_scales || !down || !down_scales || !out || !al(x, 16) ||
+      !al(topk_ids, 4) || !al(topk_weights, 4) || !al(gate_up, 16) || !al(gate_up_scales, 4) || !al(down, 16) ||
+      !al(down_scales, 4) || !al(out, 16))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  if (!workspace || !al(workspace, 256)) return set_error(LX_ERR_INVALID_ARGUMENT, "workspace null or not 256-byte aligned");
+  const FewPlan P = few_plan(T, k, E, f);
+  if (workspace_bytes < P.total) return set_error(LX_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than required");
+  FewArgs a{};
+  a.x = x;
+  a.T = T;
+  a.k = k;
+  a.E = E;
+  a.d = d;
+  a.f = f;
+  a.x_f32 = x_dtype == LX_F32;
+  a.out_f32 = out_dtype == LX_F32;
+  a.ids = topk_ids;
+  a.weights = topk_weights;
+  a.gu = (const uint8_t*)gate_up;
+  a.gu_s = (const uint8_t*)gate_up_scales;
+  a.down = (const uint8_t*)down;
+  a.down_s = (const uint8_t*)down_scales;
+  a.out = out;
+  a.units = P.units;
+  uint8_t* const w = (uint8_t*)workspace;
+  a.unit_mask = (uint64_t*)(w + P.mask);
+  a.unit_expert = (int32_t*)(w + P.expert);
+  a.unit_row = (int32_t*)(w + P.row);
+  a.hidden = (uint16_t*)(w + P.hidden);
+  const lx_status s1 = run("moe_few_up", launch_few_up, a, stream);
+  return s1 != LX_OK ? s1 : run("moe_few_down", launch_few_down, a, stream);
 }
 
 lx_status lx_mx8_quantize(const void* x, lx_dtype dtype, int64_t rows, int32_t K, lx_mx4_act act, void* codes,

@@ -120,4 +120,24 @@ struct Mx4GemmArgs {
 hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s);
 hipError_t launch_mx4_gemm_sum(const Mx4GemmArgs& a, hipStream_t s);
 
+// ------------------------------------------------------------ a layer for a few tokens
+struct FewArgs {
+  const void* x;
+  int32_t T, k, E, d, f;
+  uint8_t x_f32, out_f32;
+  const int32_t* ids;
+  const float* weights;
+  const uint8_t *gu, *gu_s, *down, *down_s;
+  void* out;
+  int32_t units;         // min(E, T k): the experts, or the slots
+  // left by the first launch for the second, per unit: its tokens (0: none), its
+  // expert and the tokens' rows of hidden
+  uint64_t* unit_mask;   // [units]
+  int32_t* unit_expert;  // [units]
+  int32_t* unit_row;     // [units][64]
+  uint16_t* hidden;      // [T k][3][f]: bf16 terms
+};
+hipError_t launch_few_up(const FewArgs& a, hipStream_t s);
+hipError_t launch_few_down(const FewArgs& a, hipStream_t s);
+
 }  // namespace lx
