@@ -14,7 +14,8 @@
  *   few tokens     a whole layer of experts in 4 bits for decoding, in two
  *                  launches
  *   8-bit values   rounding to OCP MXFP8 (e4m3), also straight from the norms,
- *                  and reading back
+ *                  reading back, and products of 8-bit activations and 4-bit
+ *                  weights with a bias, an activation and a residual
  *
  * The conventions of lorex.h hold: device pointers to dense row-major
  * caller-owned memory, asynchronous on `stream`, nothing allocated, no
@@ -241,6 +242,42 @@ lx_status lx_mx8_quantize(const void* x, lx_dtype dtype, int64_t rows, int32_t K
  * 2^128 on, and in bf16 for values below its smallest, 2^-133). */
 lx_status lx_mx8_dequantize(const void* codes, const void* scales, int64_t rows, int32_t K, void* out,
                             lx_dtype dtype, void* stream);
+
+/* Products per group of rows like lx_mx4_gemm, of 8-bit activations and 4-bit
+ * weights, with what follows a projection:
+ *
+ *   z[m][n]   = sum_c A[row(m)][c] B[g][n][c] + bias[g][n]
+ *   out[m][n] = act(z[m][n]) + residual[m][n]
+ *
+ * LX_ACT_SWIGLU: B's N rows are N / 2 gate rows, then N / 2 up rows, and out [M][N
+ * / 2] = silu(z[m][n]) z[m][N / 2 + n] + residual[m][n]; GELU is z Phi(z). A: codes
+ * [a_rows][LX_MX8_KP(K)] and scales; B: as in lx_mx4_gemm; row_map, offsets, G, M,
+ * rows of no group and map entries out of range (a product of 0 then, bias,
+ * activation and residual as for any other row) as there. bias [G][N], residual
+ * [M][columns], fp32 or bf16 each, aligned to their type; epilogue NULL: neither,
+ * and no activation. Everything after the product is computed in fp32 and rounded
+ * once. out [M][columns] fp32 or bf16 (out_scales NULL), or 8-bit values with rows of
+ * `columns` (a multiple of 8) as lx_mx8_quantize rounds them: codes in out, scales
+ * in out_scales, padding included; out_dtype is not looked at then. residual may
+ * be out where their types agree.
+ * K a multiple of 8, at most 2^24, M and N at most 2^31 - 256, M * N < 2^40, G in 1 ..
+ * LX_MAX_NODES. A, B and out 16-byte, scales, row_map and offsets 4-byte aligned;
+ * workspace 256-byte aligned, lx_mx8_gemm_workspace_bytes bytes (NULL where that is
+ * 0). The order in which a sum is formed depends on the sizes, G and act, not on
+ * the values. */
+typedef enum lx_act { LX_ACT_NONE = 0, LX_ACT_SILU = 1, LX_ACT_GELU = 2, LX_ACT_SWIGLU = 3 } lx_act;
+typedef struct lx_epilogue {
+  lx_act act;
+  lx_dtype bias_dtype;
+  lx_dtype residual_dtype;
+  const void* bias;          /* or NULL */
+  const void* residual;      /* or NULL */
+} lx_epilogue;
+size_t lx_mx8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t G, lx_act act);
+lx_status lx_mx8_gemm(const void* a, const void* a_scales, int32_t a_rows, const int32_t* row_map, const void* b,
+                      const void* b_scales, const int32_t* offsets, int32_t G, int32_t M, int32_t N, int32_t K,
+                      const lx_epilogue* epilogue, void* out, lx_dtype out_dtype, void* out_scales, void* workspace,
+                      size_t workspace_bytes, void* stream);
 
 /* lx_block_norm whose x is rounded to 8 bits as lx_mx8_quantize rounds the
  * unrounded fp32 x: codes [T][LX_MX8_KP(d)] (16-byte aligned) and scales

@@ -11,9 +11,12 @@
   loss, the tokens per expert, the gradient of the logits;
 * :func:`mx4_quantize`, :func:`mx4_dequantize`, :func:`mx4_gemm`: microscaled
   4-bit values, and products of them per group of rows;
-* :func:`mx8_quantize`, :func:`mx8_dequantize`: microscaled 8-bit values;
+* :func:`mx8_quantize`, :func:`mx8_dequantize`, :func:`mx8_gemm`: microscaled 8-bit
+  values, and products of 8-bit activations and 4-bit weights with a bias, an
+  activation and a residual;
 * :class:`Mx4Experts`, :func:`mx4_moe_block`: a MoE block whose experts are held
-  in 4 bits, built from these and the library's router and bucketing.
+  in 4 bits, built from these and the library's router and bucketing;
+* :func:`mx4_moe_few`: the experts' layer for a few tokens in two launches.
 
 Tensors are contiguous and on one GPU, which need not be the current one. Calls
 are asynchronous on ``stream`` (a ``torch.cuda.Stream`` of that GPU; default: its
@@ -35,6 +38,7 @@ from . import lorex as lx
 from .lorex import LX_BF16, LX_F32, _check
 
 MX4_NONE, MX4_SWIGLU = 0, 1
+ACT_NONE, ACT_SILU, ACT_GELU, ACT_SWIGLU = 0, 1, 2, 3
 NORM_MAX_D = 32768
 MOE_FEW_MAX_T = 64
 
@@ -51,7 +55,14 @@ class LxDropout(ctypes.Structure):
     _fields_ = [("p", _c_f32), ("rng", _c_void)]
 
 
+class LxEpilogue(ctypes.Structure):
+    _fields_ = [("act", _c_i32), ("bias_dtype", _c_i32), ("residual_dtype", _c_i32), ("bias", _c_void), ("residual", _c_void)]
+
+
 EXPORTS = {
+    "lx_mx8_gemm_workspace_bytes": (_c_size, [_c_i32] * 5),
+    "lx_mx8_gemm": (_c_i32, [_c_void, _c_void, _c_i32, _c_void, _c_void, _c_void, _c_void, _c_i32, _c_i32, _c_i32, _c_i32,
+                             _c_void, _c_void, _c_i32, _c_void, _c_void, _c_size, _c_void]),
     "lx_mx4_moe_few_workspace_bytes": (_c_size, [_c_i32] * 5),
     "lx_mx4_moe_few": (_c_i32, [_c_void, _c_i32, _c_i32, _c_i32, _c_void, _c_void, _c_i32, _c_i32, _c_i32] + [_c_void] * 5
                        + [_c_i32, _c_void, _c_size, _c_void]),
@@ -620,6 +631,62 @@ def mx8_dequantize(q: Mx8, dtype: torch.dtype = torch.bfloat16, *, out: Optional
     st = lib().lx_mx8_dequantize(_arg("codes", q.codes, (*lead, Kp), torch.uint8, gpu),
                                  _arg("scales", q.scales, (*lead, Kp // 32), torch.uint8, gpu), lead.numel(), K,
                                  _arg("out", out, shape, None, gpu), _dtype("out", out), _current_raw_stream(gpu))
+    if st:
+        _check(st)
+    return out
+
+
+def mx8_gemm(a: Mx8, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map: Optional[torch.Tensor] = None,
+             bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, residual: Optional[torch.Tensor] = None,
+             out=None, out_dtype=torch.float32, workspace: Optional[torch.Tensor] = None, stream=None):
+    """out[m] = act(A[row(m)] B[g]^T + bias[g]) + residual[m] for the rows m of group g
+    (lx_mx8_gemm): a [rows][K] in 8 bits; b [G][N][K] (or [N][K]: one group) in 4; bias
+    [G][N] ([N] for one group) and residual [M][columns] fp32 or bf16; ``ACT_SWIGLU``
+    takes N / 2 gate and N / 2 up rows and gives N / 2 columns. offsets, row_map and
+    rows past offsets[G] as in :func:`mx4_gemm`. The result is a tensor of
+    ``out_dtype``, or with ``out_dtype="mx8"`` (or an :class:`Mx8` given as out) 8-bit
+    values."""
+    gpu = _gpu("a", a.codes)
+    if stream is not None or gpu != _current_device():
+        return _there(mx8_gemm, gpu, stream, locals())
+    ac, bc, K = a.codes, b.codes, a.K
+    if ac.dim() != 2 or bc.dim() not in (2, 3):
+        raise ValueError("a must be [rows][K] and b [G][N][K] or [N][K]")
+    if K != b.K:
+        raise ValueError(f"a has {K} values in a row and b {b.K}")
+    Kp = mx4_padded(K)
+    rows = ac.shape[0]
+    *lead, _ = bc.shape
+    G, N = lead if len(lead) == 2 else (1, lead[0])
+    M = rows if row_map is None else row_map.shape[0]
+    if act == ACT_SWIGLU and N % 2:
+        raise ValueError("SwiGLU needs an even number of weight rows")
+    cols = N // 2 if act == ACT_SWIGLU else N
+    mx8 = isinstance(out, Mx8) or (out is None and out_dtype == "mx8")
+    if mx8:
+        cp = mx4_padded(cols)
+        if out is None:
+            out = Mx8(ac.new_empty((M, cp), dtype=torch.uint8), ac.new_empty((M, cp // 32), dtype=torch.uint8), cols)
+        elif out.K != cols:
+            raise ValueError(f"out has {out.K} values in a row, the result {cols}")
+        to = _arg("out codes", out.codes, (M, cp), torch.uint8, gpu), 0, _arg("out scales", out.scales, (M, cp // 32), torch.uint8, gpu)
+    else:
+        if out is None:
+            out = ac.new_empty((M, cols), dtype=out_dtype)
+        to = _arg("out", out, (M, cols), None, gpu), _dtype("out", out), None
+    if bias is not None and bias.dim() == 1 and G == 1:
+        bias = bias.view(1, -1)
+    e = LxEpilogue(act, 0 if bias is None else _dtype("bias", bias), 0 if residual is None else _dtype("residual", residual),
+                   _arg("bias", bias, (G, N), None, gpu), _arg("residual", residual, (M, cols), None, gpu))
+    L = lib()
+    keep, ws, n = _workspace(workspace, L.lx_mx8_gemm_workspace_bytes(M, N, K, G, act), ac)
+    st = L.lx_mx8_gemm(_arg("a codes", ac, (rows, Kp), torch.uint8, gpu),
+                       _arg("a scales", a.scales, (rows, Kp // 32), torch.uint8, gpu), rows,
+                       _arg("row_map", row_map, (M,), torch.int32, gpu),
+                       _arg("b codes", bc, (*lead, Kp // 2), torch.uint8, gpu),
+                       _arg("b scales", b.scales, (*lead, Kp // 32), torch.uint8, gpu),
+                       _arg("offsets", offsets, (G + 1,), torch.int32, gpu), G, M, N, K, ctypes.byref(e), *to, ws, n,
+                       _current_raw_stream(gpu))
     if st:
         _check(st)
     return out

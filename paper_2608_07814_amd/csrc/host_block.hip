@@ -383,6 +383,59 @@ lx_status lx_mx4_dequantize(const void* codes, const void* scales, int64_t rows,
   return run("mx4_dequantize", launch_mx4_dequantize, a, stream);
 }
 
+size_t lx_mx8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t G, lx_act act) {
+  clear_error();
+  if (check_mx4_gemm(M, N, K, G) != LX_OK) return 0;
+  if (act < LX_ACT_NONE || act > LX_ACT_SWIGLU) set_error(LX_ERR_INVALID_ARGUMENT, "bad act");
+  return 0;
+}
+
+lx_status lx_mx8_gemm(const void* a, const void* a_scales, int32_t a_rows, const int32_t* row_map, const void* b,
+                      const void* b_scales, const int32_t* offsets, int32_t G, int32_t M, int32_t N, int32_t K,
+                      const lx_epilogue* epilogue, void* out, lx_dtype out_dtype, void* out_scales, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  clear_error();
+  const lx_status st = check_mx4_gemm(M, N, K, G);
+  if (st != LX_OK) return st;
+  const lx_epilogue e = epilogue ? *epilogue : lx_epilogue{};
+  if (e.act < LX_ACT_NONE || e.act > LX_ACT_SWIGLU || (e.bias && !dtype_ok(e.bias_dtype)) ||
+      (e.residual && !dtype_ok(e.residual_dtype)) || (!out_scales && !dtype_ok(out_dtype)))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "bad act or dtype");
+  if (e.act == LX_ACT_SWIGLU && N % 2) return set_error(LX_ERR_INVALID_ARGUMENT, "SwiGLU needs an even N");
+  const int32_t cols = e.act == LX_ACT_SWIGLU ? N / 2 : N;
+  if (out_scales && cols % 8) return set_error(LX_ERR_UNSUPPORTED, "rows of an 8-bit result must be a multiple of 8 long");
+  if (a_rows < 0 || (!row_map && a_rows < M)) return set_error(LX_ERR_INVALID_ARGUMENT, "a_rows must be >= M without a row map");
+  if (!offsets && G != 1) return set_error(LX_ERR_INVALID_ARGUMENT, "several groups need offsets");
+  if (M == 0) return LX_OK;
+  if (!a || !a_scales || !b || !b_scales || !out || !al(a, 16) || !al(b, 16) || !al(out, 16) || !al(a_scales, 4) ||
+      !al(b_scales, 4) || !al(row_map, 4) || !al(offsets, 4) || !al(out_scales, 4) ||
+      !al(e.bias, e.bias_dtype == LX_F32 ? 4 : 2) || !al(e.residual, e.residual_dtype == LX_F32 ? 4 : 2))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  Mx8GemmArgs g{};
+  g.a = (const uint8_t*)a;
+  g.as = (const uint8_t*)a_scales;
+  g.b = (const uint8_t*)b;
+  g.bs = (const uint8_t*)b_scales;
+  g.a_rows = a_rows;
+  g.row_map = row_map;
+  g.offsets = offsets;
+  g.G = G;
+  g.M = M;
+  g.N = N;
+  g.Kp = LX_MX8_KP(K);
+  g.cols = cols;
+  g.act = e.act;
+  g.bias = e.bias;
+  g.res = e.residual;
+  g.bias_f32 = e.bias_dtype == LX_F32;
+  g.res_f32 = e.residual_dtype == LX_F32;
+  g.out_f32 = out_dtype == LX_F32;
+  g.out = out;
+  g.out_scales = (uint8_t*)out_scales;
+  g.plan = mx8_gemm_plan(M, cols, g.Kp, G);
+  return run("mx8_gemm", launch_mx8_gemm, g, stream);
+}
+
 size_t lx_mx4_moe_few_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t d, int32_t f) {
   clear_error();
   if (check_few(T, k, E, d, f) != LX_OK) return 0;

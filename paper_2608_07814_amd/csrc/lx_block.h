@@ -120,6 +120,27 @@ struct Mx4GemmArgs {
 hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, hipStream_t s);
 hipError_t launch_mx4_gemm_sum(const Mx4GemmArgs& a, hipStream_t s);
 
+// Products of 8-bit activations and 4-bit weights.
+struct Mx8GemmPlan {
+  enum Kernel : int32_t { kRows, kRows4 } kernel;
+};
+Mx8GemmPlan mx8_gemm_plan(int M, int cols, int Kp, int G);
+struct Mx8GemmArgs {
+  const uint8_t *a, *as, *b, *bs;
+  int32_t a_rows;
+  const int32_t* row_map;
+  const int32_t* offsets;
+  int32_t G, M, N, Kp;
+  int32_t cols;          // of the result: N, N / 2 with SwiGLU
+  int32_t act;
+  const void *bias, *res;
+  uint8_t bias_f32, res_f32, out_f32;
+  void* out;
+  uint8_t* out_scales;   // not null: the result is in 8 bits
+  Mx8GemmPlan plan;
+};
+hipError_t launch_mx8_gemm(const Mx8GemmArgs& a, hipStream_t s);
+
 // ------------------------------------------------------------ a layer for a few tokens
 struct FewArgs {
   const void* x;

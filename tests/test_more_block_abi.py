@@ -92,6 +92,58 @@ def test_mx8_quantize_and_dequantize(L, call, code):
         assert L.lx_mx8_dequantize(a["codes"], a["scales"], a["rows"], a["K"], a["x"], a["dt"], None) == code
 
 
+FEW = dict(x=FAKE, dt=lx.LX_BF16, T=4, d=64, ids=FAKE, w=FAKE, k=2, E=8, f=32, gu=FAKE, gus=FAKE, dn=FAKE, dns=FAKE, out=FAKE, odt=lx.LX_F32,
+           ws=FAKE, n=1 << 40)
+
+
+@pytest.mark.parametrize("call,code", [
+    (dict(T=-1), BAD), (dict(T=65), UNS), (dict(d=0), BAD), (dict(d=60), UNS), (dict(f=20), UNS), (dict(f=0), BAD), (dict(d=1 << 21), UNS),
+    (dict(E=0), UNS), (dict(E=8193), UNS), (dict(k=0), UNS), (dict(k=33), UNS), (dict(dt=2), BAD), (dict(odt=-1), BAD), (dict(x=None), BAD),
+    (dict(x=FAKE + 8), BAD), (dict(ids=None), BAD), (dict(ids=FAKE + 2), BAD), (dict(w=None), BAD), (dict(gu=FAKE + 4), BAD), (dict(gus=None), BAD),
+    (dict(dn=None), BAD), (dict(dns=FAKE + 1), BAD), (dict(out=None), BAD), (dict(out=FAKE + 8), BAD), (dict(ws=None), BAD),
+    (dict(ws=FAKE + 128), BAD), (dict(n=64), SMALL), (dict(T=0, x=None, ws=None), OK),
+])
+def test_moe_few(L, call, code):
+    a = dict(FEW, **call)
+    st = L.lx_mx4_moe_few(*a.values(), None)
+    assert st == code, L.lx_last_error()
+    n = L.lx_mx4_moe_few_workspace_bytes(a["T"], a["k"], a["E"], a["d"], a["f"])
+    assert (n == 0) == (any(v in call for v in ("T", "d", "f", "E", "k"))), n
+
+
+GEMM = dict(a=FAKE, as_=FAKE, ar=4, rm=FAKE, b=FAKE, bs=FAKE, off=FAKE, G=2, M=4, N=16, K=64)
+
+
+@pytest.mark.parametrize("call,epi,to,code", [
+    (dict(M=-1), {}, {}, BAD), (dict(N=0), {}, {}, BAD), (dict(K=0), {}, {}, BAD), (dict(K=60), {}, {}, UNS), (dict(G=0), {}, {}, BAD),
+    (dict(G=8193), {}, {}, UNS), (dict(M=(1 << 31) - 255, ar=(1 << 31) - 1), {}, {}, UNS), (dict(N=(1 << 31) - 255), {}, {}, UNS),
+    (dict(M=1 << 30, N=1 << 11, ar=1 << 30), {}, {}, UNS), (dict(ar=3, rm=None), {}, {}, BAD), (dict(ar=-1), {}, {}, BAD), (dict(off=None), {}, {}, BAD),
+    (dict(a=None), {}, {}, BAD), (dict(a=FAKE + 8), {}, {}, BAD), (dict(as_=FAKE + 2), {}, {}, BAD), (dict(b=FAKE + 4), {}, {}, BAD),
+    (dict(bs=None), {}, {}, BAD), (dict(rm=FAKE + 2), {}, {}, BAD), (dict(off=FAKE + 1), {}, {}, BAD),
+    ({}, dict(act=4), {}, BAD), ({}, dict(act=-1), {}, BAD), ({}, dict(bias_dtype=2), {}, BAD), ({}, dict(residual_dtype=3), {}, BAD),
+    ({}, dict(bias=FAKE + 2), {}, BAD), ({}, dict(bias=FAKE + 1, bias_dtype=1), {}, BAD), ({}, dict(residual=FAKE + 2), {}, BAD),
+    (dict(N=17), dict(act=3), {}, BAD), ({}, {}, dict(out=None), BAD), ({}, {}, dict(out=FAKE + 8), BAD), ({}, {}, dict(dt=2), BAD),
+    ({}, {}, dict(scales=FAKE + 2), BAD), (dict(N=20), {}, dict(scales=FAKE), UNS), (dict(N=24), dict(act=3), dict(scales=FAKE), UNS),
+    (dict(M=0, a=None), {}, dict(out=None), OK),
+])
+def test_mx8_gemm(L, call, epi, to, code):
+    e = lb.LxEpilogue()
+    for n, v in dict(dict(act=0, bias_dtype=0, residual_dtype=0, bias=FAKE, residual=FAKE), **epi).items():
+        setattr(e, n, v)
+    t = dict(dict(out=FAKE, dt=lx.LX_F32, scales=None), **to)
+    st = L.lx_mx8_gemm(*dict(GEMM, **call).values(), ctypes.byref(e), *t.values(), FAKE, 1 << 60, None)
+    assert st == code, L.lx_last_error()
+    assert bool(L.lx_last_error()) == (code != OK)
+
+
+def test_the_largest_products_are_taken(L):
+    most = (1 << 31) - 256
+    for M, N in ((most, 1), (most, 8), (1, most), (8, most)):
+        L.lx_mx8_gemm_workspace_bytes(M, N, 64, 1, 0)
+        assert not L.lx_last_error()
+    assert L.lx_mx8_gemm_workspace_bytes(4, 8, 64, 1, 9) == 0 and L.lx_last_error()
+
+
 def test_wrappers_refuse_cpu_tensors():
     h, w = torch.zeros(2, 8), torch.zeros(8)
     rng = torch.zeros(2, dtype=torch.int64)
