@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void k_few_up(const FewArgs a) {
       const int n = n0 + q * 4;  // (f is a multiple of 8: all four columns exist or none)
       Terms h[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) h[j] = terms(ag[j] / (1.f + expf(-ag[j])) * au[j] * weight);
+      for (int j = 0; j < 4; ++j) h[j] = terms(silu(ag[j]) * au[j] * weight);
       if (col < count && n < a.f) {
         uint16_t* const p = a.hidden + (int64_t)row * 3 * a.f + n;
 #pragma unroll

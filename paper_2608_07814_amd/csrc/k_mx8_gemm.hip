@@ -27,18 +27,14 @@ __device__ __forceinline__ v8i frag8(const vu4& p, const vu4& q) {
 // with both operands e2m1 nothing is). Activations whose exponent field's top bit is
 // set (from 2 on under the block's scale) and the others are within the window among
 // themselves, so two instructions, one for each, drop nothing.
-struct Halves {
-  v8i hi, lo;
-};
-__device__ __forceinline__ Halves halves(const v8i& a) {
-  Halves r;
+template <bool HI>
+__device__ __forceinline__ v8i half_of(v8i a) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const uint32_t m = ((uint32_t)a[j] >> 6) & 0x01010101u, mask = (m << 8) - m;
-    r.hi[j] = a[j] & (int)mask;
-    r.lo[j] = a[j] & (int)~mask;
+    a[j] &= (int)(HI ? mask : ~mask);
   }
-  return r;
+  return a;
 }
 
 // ---------------------------------------------------------------- epilogue
@@ -70,14 +66,14 @@ __device__ __forceinline__ vf4 with_bias(const Mx8GemmArgs& a, int g, int c, int
 __device__ __forceinline__ vf4 activate(int act, vf4 z) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    if (act == LX_ACT_SILU) z[j] = z[j] / (1.f + expf(-z[j]));
+    if (act == LX_ACT_SILU) z[j] = silu(z[j]);
     if (act == LX_ACT_GELU) z[j] = 0.5f * z[j] * erfcf(z[j] * -0.70710678118654752f);
   }
   return z;
 }
 __device__ __forceinline__ vf4 swiglu(vf4 z, vf4 u) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) z[j] = z[j] / (1.f + expf(-z[j])) * u[j];
+  for (int j = 0; j < 4; ++j) z[j] = silu(z[j]) * u[j];
   return z;
 }
 
@@ -185,12 +181,12 @@ __global__ __launch_bounds__(WN* WK * 64) void k_mx8_gemm_rows(const Mx8GemmArgs
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const Halves v = halves(frag8(av[0][u], av[1][u]));
+        const v8i v = frag8(av[0][u], av[1][u]), lo = half_of<false>(v), hi = half_of<true>(v);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-          acc[p] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag4(w[p][u]), v.lo, acc[p], 4, 0, 0, ws[p][u] >> (8 * q), 0,
+          acc[p] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag4(w[p][u]), lo, acc[p], 4, 0, 0, ws[p][u] >> (8 * q), 0,
                                                                     as[u] >> (8 * q));
-          acc[p] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag4(w[p][u]), v.hi, acc[p], 4, 0, 0, ws[p][u] >> (8 * q), 0,
+          acc[p] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag4(w[p][u]), hi, acc[p], 4, 0, 0, ws[p][u] >> (8 * q), 0,
                                                                     as[u] >> (8 * q));
         }
       }
@@ -233,6 +229,337 @@ __global__ __launch_bounds__(WN* WK * 64) void k_mx8_gemm_rows(const Mx8GemmArgs
   }
 }
 
+// ---------------------------------------------------------------- large tiles
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// BM x BN products per workgroup, a WR x WC grid of wavefronts, 32x32x64 instructions.
+// Both operands go memory -> LDS directly: the activations in steps of 128 values, the
+// weights, half as wide, in steps of 256, so that a row is a whole cache line of 128
+// bytes in both; two stages each, one streaming in while the other is multiplied, the
+// weights' next step in two halves. Inside a stage the eight 16-byte chunks of a row
+// are XORed with (row / 2) % 8, so the 16 lanes that a read serves together hit 16
+// different bank groups; a lane fetches the chunk that belongs at its LDS place.
+// Scales come in groups of 512 values (16 bytes a row) through a ring of two. The
+// weights are the instruction's first operand: a lane ends with 4 consecutive columns
+// of one row, which get their bias and activation there (SwiGLU: a wavefront's columns
+// are half gate, half up, so that both are in the same lane) and go through LDS to
+// lanes of 8 columns.
+// Workgroups stay for several tiles: the next one's place and rows are looked up under
+// the first loads of the present one, and its first loads are under way while the
+// present one's results are written.
+template <int BM_, int BN_>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, THR = BM * BN > 128 * 128 ? 512 : 256, NW = THR / 64;
+  static constexpr int WR = BM == 256 ? 4 : 2, WC = NW / WR, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+  static constexpr int RA = BM * 8 / THR, RB = BN * 8 / THR;  // a thread's 16-byte loads per step of A, of B
+  static constexpr int SA = BM * 128, SB = BN * 128, STAGE = SA + SB, SGRP = (BM + BN) * 16;
+  static constexpr int NEXT = 2 * STAGE + 2 * SGRP, LDS = NEXT + (RA + 1) * THR * 4, PER_CU = THR == 512 ? 1 : 2;
+  static_assert(LDS * PER_CU <= 160 * 1024, "");
+  static_assert(MI <= 2, "");
+  static_assert(BM + BN <= THR && RB % 2 == 0 && NI % 2 == 0, "one row of scales per thread; halves");
+};
+
+template <class T, bool GLU, bool EXACT>
+__global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_tile(const Mx8GemmArgs a) {
+  constexpr int BM = T::BM, BN = T::BN, THR = T::THR, NW = T::NW, WC = T::WC, WM = T::WM, WN = T::WN, MI = T::MI, NI = T::NI;
+  constexpr int RA = T::RA, RB = T::RB, SA = T::SA, STAGE = T::STAGE, SGRP = T::SGRP;
+  constexpr int OC = GLU ? BN / 2 : BN, OW = GLU ? WN / 2 : WN;  // columns of the result: of a tile, of a wavefront
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDS];
+
+  const bool mx8 = a.out_scales != nullptr;
+  const int ntn = ((mx8 ? LX_MX8_KP(a.cols) : a.cols) + OC - 1) / OC;
+  const int rt = count_tiles<BM>(a);
+  Items it((int64_t)rt * ntn);
+  if (it.at >= it.end) return;
+
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int l32 = lane & 31, h = lane >> 5, wm = wave / WC, wn = wave % WC;
+  const int cp = a.Kp / 2, sp = a.Kp / 32, steps = a.Kp / 128;
+
+  struct Item {
+    int g, m0, m1, n0;
+    uint64_t there;          // which of this wavefront's rows have a row of A
+    uint32_t oa[RA];         // a thread's byte offsets from A (the host sees to it that they fit 32 bits)
+    uint32_t qs;             // its row of the scale groups: of A (threads below BM)
+  };
+  static_assert(WM <= 64, "");
+  // A's row for tile row r, -1 if there is none (past the tile, or a map entry out
+  // of range): its loads read A's first row (the host sees to it that there is
+  // one), its results are dropped or 0
+  auto row_of = [&](const Item& q, int r) __attribute__((always_inline)) {
+    const int m = q.m0 + r;
+    if (m >= q.m1) return -1;
+    const int src = a.row_map ? a.row_map[m] : m;
+    return src >= 0 && src < a.a_rows ? src : -1;
+  };
+  // Item L: column tiles in bands of 8, so that what an XCD runs together shares
+  // rows and weights in its L2.
+  auto look_up = [&](int64_t L, Item& q) __attribute__((always_inline)) {
+    const int64_t per_band = (int64_t)rt * 8;
+    const int band = (int)(L / per_band), w = min(8, ntn - band * 8);
+    const int rem = (int)(L - band * per_band), ti = rem / w;
+    q.n0 = (band * 8 + rem - ti * w) * OC;
+    q.g = q.m0 = q.m1 = 0;
+    find_tile<BM>(a, ti, q.g, q.m0, q.m1);
+#pragma unroll
+    for (int j = 0; j < RA; ++j) {
+      const int r = (j * THR + tid) >> 3;
+      q.oa[j] = (uint32_t)max(row_of(q, r), 0) * (uint32_t)a.Kp + ((tid ^ (r >> 1)) & 7) * 16;
+    }
+    q.qs = (uint32_t)max(row_of(q, tid % BM), 0) * (uint32_t)sp;
+    q.there = __ballot(lane < WM && row_of(q, wm * WM + lane) >= 0);
+  };
+  Item cur;
+  const uint8_t *B, *Bs;  // the group's weights and their scales
+  uint32_t ob[RB];        // a thread's byte offsets from B (the host sees to it that they fit 32 bits)
+  // the weight row of row r of the tile
+  auto brow = [&](int r) __attribute__((always_inline)) {
+    if constexpr (GLU) {
+      const int i = r % WN, c = cur.n0 + r / WN * OW + i % OW;
+      return min(c, a.cols - 1) + (i < OW ? 0 : a.cols);
+    } else {
+      return min(cur.n0 + r, a.N - 1);
+    }
+  };
+  auto from_b = [&]() __attribute__((always_inline)) {
+    B = a.b + (int64_t)cur.g * a.N * cp;
+    Bs = a.bs + (int64_t)cur.g * a.N * sp;
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+      const int r = (j * THR + tid) >> 3;
+      ob[j] = (uint32_t)brow(r) * (uint32_t)cp + ((tid ^ (r >> 1)) & 7) * 16;
+    }
+    if (wave >= NW - BN / 64) cur.qs = (uint32_t)brow(tid % BN) * (uint32_t)sp;
+  };
+  // Group q of the scales: words 4 q .. 4 q + 3 of every row, 16 bytes a row (a
+  // memory address need only be aligned to words). A row's last group holds its
+  // last four words, so a step finds its words `late` words further on.
+  auto late = [&](int q) __attribute__((always_inline)) { return steps < 4 ? 0 : max(q * 4 - (steps - 4), 0); };
+  auto issue_scales = [&](int q) __attribute__((always_inline)) {
+    uint8_t* const st = smem + 2 * STAGE + (q & 1) * SGRP;
+    if (steps >= 4) {
+      const int at = (q * 4 - late(q)) * 4;
+      if (wave < BM / 64) load_lds<16>(a.as + at, cur.qs, st + wave * 1024);
+      if (wave >= NW - BN / 64) load_lds<16>(Bs + at, cur.qs, st + BM * 16 + (wave - (NW - BN / 64)) * 1024);
+    } else {
+      // rows of fewer words: word by word, 16 rows x 4 words per load, the last
+      // one repeated
+      const int word = min(lane & 3, steps - 1) * 4;
+#pragma unroll 1
+      for (int r0 = wave * 16; r0 < BM + BN; r0 += NW * 16) {
+        const int r = r0 + (lane >> 2);
+        if (r0 < BM)
+          load_lds<4>(a.as, (uint32_t)max(row_of(cur, r), 0) * (uint32_t)sp + word, st + r0 * 16);
+        else
+          load_lds<4>(Bs, (uint32_t)brow(r - BM) * (uint32_t)sp + word, st + r0 * 16);
+      }
+    }
+  };
+  // load j of step t of A into stage t % 2
+  auto issue_a = [&](int t, int j) __attribute__((always_inline)) {
+    load_lds<16>(a.a + (int64_t)t * 128, cur.oa[j], smem + (t & 1) * STAGE + (j * NW + wave) * 1024);
+  };
+  // load j of step u of B (256 values) into stage u % 2; where only half of it is
+  // there the upper chunks repeat the lower ones (they are not multiplied)
+  auto issue_b = [&](int u, int j) __attribute__((always_inline)) {
+    const uint32_t back = 2 * u + 1 == steps ? ((tid ^ (((j * THR + tid) >> 3) >> 1)) & 4) * 16 : 0;
+    load_lds<16>(B + (int64_t)u * 128, ob[j] - back, smem + (u & 1) * STAGE + SA + (j * NW + wave) * 1024);
+  };
+  auto begin = [&]() __attribute__((always_inline)) {
+    issue_scales(0);
+#pragma unroll
+    for (int j = 0; j < RA; ++j) issue_a(0, j);
+#pragma unroll
+    for (int j = 0; j < RB; ++j) issue_b(0, j);
+  };
+
+  f32x16 acc[MI][NI];
+  const int swz = (l32 >> 1) & 7;
+  const uint32_t la = (wm * WM + l32) * 128 + (h ^ swz) * 16, lb = SA + (wn * WN + l32) * 128 + (h ^ swz) * 16;
+  const uint8_t* const lsa = smem + 2 * STAGE + (wm * WM + l32) * 16;
+  const uint8_t* const lsb = smem + 2 * STAGE + (BM + wn * WN + l32) * 16;
+  // a row's scales of a step are one word: a lane's block of instruction s is 2 s +
+  // h, so after a shift by h bytes its scale is byte 2 s
+  struct Scales {
+    uint32_t a[MI], b[NI];
+  };
+  struct Frags {
+    vu4 a[MI][2], b[NI];
+  };
+  auto read_scales = [&](int t) __attribute__((always_inline)) {
+    Scales q;
+    const int st = ((t >> 2) & 1) * SGRP + ((t & 3) + late(t >> 2)) * 4;
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) q.b[ni] = *(const uint32_t*)(lsb + st + ni * 512) >> (8 * h);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) q.a[mi] = *(const uint32_t*)(lsa + st + mi * 512) >> (8 * h);
+    return q;
+  };
+  // fragments of instruction s (64 values) of step t: of the activations 16 values
+  // from 16 h and from 32 + 16 h on, of the weights 32 from 32 h on
+  // (chunk c of a row lies at (c ^ swz) 16 of its 128 bytes: the address of h's chunk,
+  // XORed with the rest of c)
+  auto lds = [&](uint32_t first, int c) __attribute__((always_inline)) { return smem + (first ^ (uint32_t)(c * 16)); };
+  auto read_b = [&](Frags& f, int s, int t) __attribute__((always_inline)) {
+    const uint8_t* const p = lds(lb + ((t >> 1) & 1) * STAGE, (t & 1) * 4 + 2 * s);
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) f.b[ni] = *(const vu4*)(p + ni * 4096);
+  };
+  auto read_a = [&](Frags& f, auto blocks, int s, int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int mi = 0; mi < decltype(blocks)::value; ++mi)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) f.a[mi][c] = *(const vu4*)(lds(la + (t & 1) * STAGE, 4 * s + 2 * c) + mi * 4096);
+  };
+  // step t's loads: A's, and the half (t - 1) % 2 of the weights' step that begins at t or
+  // t + 1
+  auto issue = [&](int t, auto odd) __attribute__((always_inline)) {
+    constexpr int ODD = decltype(odd)::value;
+#pragma unroll
+    for (int j = 0; j < RA; ++j) issue_a(t, j);
+    const int u = (t + 1) >> 1;
+    if (2 * u < steps) {
+#pragma unroll
+      for (int j = 0; j < RB / 2; ++j) issue_b(u, (ODD ? 0 : RB / 2) + j);
+    }
+  };
+  auto multiply = [&](auto sv, auto blocks, const Frags& f, const Scales& q) __attribute__((always_inline)) {
+    constexpr int S = decltype(sv)::value;
+#pragma unroll
+    for (int mi = 0; mi < decltype(blocks)::value; ++mi) {
+      const v8i x = frag8(f.a[mi][0], f.a[mi][1]);
+      auto row = [&](const v8i& v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni)
+          acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag4(f.b[ni]), v, acc[mi][ni], 4, 0, 2 * S, q.b[ni],
+                                                                        2 * S, q.a[mi]);
+      };
+      if constexpr (EXACT) {
+        row(half_of<false>(x));
+        row(half_of<true>(x));
+      } else {
+        row(x);
+      }
+    }
+  };
+  using std::integral_constant;
+  constexpr integral_constant<int, 0> i0{};
+  constexpr integral_constant<int, 1> i1{};
+
+  look_up(it.at, cur);
+  from_b();
+  begin();
+  for (;;) {
+    it.at += it.step;
+    const bool more = it.at < it.end;
+    Item next;
+    // (a thread's offsets of the next item wait in LDS: next to the present one's they
+    // would not fit in registers)
+    uint32_t* const keep = (uint32_t*)(smem + T::NEXT) + tid;
+    if (more) {
+      look_up(it.at, next);
+#pragma unroll
+      for (int j = 0; j < RA; ++j) keep[j * THR] = next.oa[j];
+      keep[RA * THR] = next.qs;
+    }
+    land_and_meet();
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
+    const int live = min(max((cur.m1 - cur.m0 - wm * WM + 31) / 32, 0), MI);
+    // step t has landed, step t + 1 streams in under its products
+    auto step = [&](int t, auto odd) __attribute__((always_inline)) {
+      constexpr int ODD = decltype(odd)::value;
+      if (t + 1 < steps) {
+        if (ODD && (t & 3) == 3) issue_scales((t + 1) >> 2);
+        issue(t + 1, integral_constant<int, !ODD>{});
+      }
+      auto products = [&](auto blocks) __attribute__((always_inline)) {
+        const Scales q = read_scales(t);
+        Frags f0, f1;
+        read_b(f0, 0, t);
+        read_a(f0, blocks, 0, t);
+        read_b(f1, 1, t);
+        read_a(f1, blocks, 1, t);
+        multiply(i0, blocks, f0, q);
+        multiply(i1, blocks, f1, q);
+      };
+      // blocks of 32 rows past the tile's last are not multiplied (256 x 256: a wavefront's
+      // 64 rows are or are not, a second loop would not fit in registers)
+      if (live == MI || (THR == 512 && live > 0))
+        products(integral_constant<int, MI>{});
+      else if (THR != 512 && live > 0)
+        products(i1);
+      land_and_meet();
+    };
+    int t = 0;
+#pragma unroll 1
+    for (; t + 2 <= steps; t += 2) {
+      step(t, i0);
+      step(t + 1, i1);
+    }
+    if (t < steps) step(t, i0);
+
+    const int g = cur.g, m0 = cur.m0, m1 = cur.m1, c0 = cur.n0 + wn * OW;
+    const uint64_t there = cur.there;
+    if (more) {
+      cur = next;
+#pragma unroll
+      for (int j = 0; j < RA; ++j) cur.oa[j] = keep[j * THR];
+      cur.qs = keep[RA * THR];
+      from_b();
+      begin();
+    }
+    // 32 rows by CW columns at a time through this wavefront's part of the second stages
+    // (the next item's first step is on its way into the first ones), 16-byte chunks
+    // XORed by the row
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    constexpr int CW = OW >= 64 && STAGE / NW >= 32 * 64 * 4 ? 64 : 32, LPR = CW / 8;
+    static_assert(NW * 32 * CW * 4 <= STAGE, "");
+    uint8_t* const e = smem + STAGE + wave * 32 * CW * 4;
+    auto chunk = [](int r, int c) { return r * CW * 4 + (c ^ (CW == 32 ? (r >> 1) & 7 : r & 15)) * 16; };
+    auto four = [](const f32x16& v, int q) { return vf4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]}; };
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      if (mi >= live) break;
+      const bool has = there >> (mi * 32 + (ln & 31)) & 1;
+#pragma unroll
+      for (int cc = 0; cc < OW / CW; ++cc) {
+#pragma unroll
+        for (int nn = 0; nn < CW / 32; ++nn) {
+          constexpr int HALF = NI / 2;
+          const int ni = cc * (CW / 32) + nn;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int c = c0 + ni * 32 + 8 * q + 4 * (ln >> 5), n = min(a.cols - c, 4);
+            vf4 z = with_bias(a, g, c, n, has, four(acc[mi][ni], q));
+            if constexpr (GLU)
+              z = swiglu(z, with_bias(a, g, a.cols + c, n, has, four(acc[mi][(ni + HALF) % NI], q)));
+            else
+              z = activate(a.act, z);
+            *(vf4*)(e + chunk(ln & 31, nn * 8 + 2 * q + (ln >> 5))) = z;
+          }
+        }
+        asm volatile("" ::: "memory");  // (a wavefront's LDS accesses run in order)
+#pragma unroll 2
+        for (int r0 = 0; r0 < 32; r0 += 64 / LPR) {
+          const int r = r0 + ln / LPR, m = m0 + wm * WM + mi * 32 + r, c = c0 + cc * CW + ln % LPR * 8;
+          const vf4 u = *(const vf4*)(e + chunk(r, ln % LPR * 2)), v = *(const vf4*)(e + chunk(r, ln % LPR * 2 + 1));
+          const F8 x{{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]}};
+          if (mx8)
+            finish<true>(a, m, c, m < m1, x);
+          else
+            finish<false>(a, m, c, m < m1, x);
+        }
+        asm volatile("" ::: "memory");
+      }
+    }
+    if (!more) break;
+  }
+}
+
 template <int WN, int WK, bool GLU, bool MX8>
 hipError_t launch_rows(const Mx8GemmArgs& a, hipStream_t s) {
   constexpr int BM = 16, BN = 16 * WN;
@@ -242,28 +569,76 @@ hipError_t launch_rows(const Mx8GemmArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <bool GLU, bool MX8>
+template <class T, bool GLU>
+hipError_t launch_tile(const Mx8GemmArgs& a, hipStream_t s) {
+  constexpr int OC = GLU ? T::BN / 2 : T::BN;
+  const int64_t tiles = a.offsets ? std::min<int64_t>((int64_t)a.M / T::BM + a.G, a.M) : ((int64_t)a.M + T::BM - 1) / T::BM;
+  const int64_t cols = a.out_scales ? LX_MX8_KP((int64_t)a.cols) : a.cols, items = tiles * ((cols + OC - 1) / OC);
+  const unsigned grid = (unsigned)std::min<int64_t>((items + 7) / 8 * 8, 256 * T::PER_CU);
+  // a bf16 result is rounded by 2^-9: next to it what one instruction drops does not count
+  if (a.out_scales || a.out_f32)
+    k_mx8_gemm_tile<T, GLU, true><<<grid, T::THR, 0, s>>>(a);
+  else
+    k_mx8_gemm_tile<T, GLU, false><<<grid, T::THR, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <bool GLU>
 hipError_t launch(const Mx8GemmArgs& a, hipStream_t s) {
+  const bool mx8 = a.out_scales != nullptr;
   switch (a.plan.kernel) {
-    case Mx8GemmPlan::kRows4: return launch_rows<2, 4, GLU, MX8>(a, s);
-    default: return launch_rows<4, 1, GLU, MX8>(a, s);
+    case Mx8GemmPlan::kRows4: return mx8 ? launch_rows<2, 4, GLU, true>(a, s) : launch_rows<2, 4, GLU, false>(a, s);
+    case Mx8GemmPlan::kRows: return mx8 ? launch_rows<4, 1, GLU, true>(a, s) : launch_rows<4, 1, GLU, false>(a, s);
+    case Mx8GemmPlan::kTile64: return launch_tile<Tile<64, 128>, GLU>(a, s);
+    case Mx8GemmPlan::kTile128: return launch_tile<Tile<128, 128>, GLU>(a, s);
+    default: return launch_tile<Tile<256, 256>, GLU>(a, s);
   }
 }
 
 }  // namespace
 
-// Which kernel. Rows of a group are not known here, only their mean.
-Mx8GemmPlan mx8_gemm_plan(int M, int cols, int Kp, int G) {
+// Which kernel: the one with the least time by a model of rounds. A round is what
+// the compute units take at once, in us per 4096 values of K (measured alone on full
+// rounds, `half` where each compute unit has one workgroup at most, for results in
+// bf16 and for those of two instructions):
+//                         half          full            workgroups in a round
+//   16 x 32 (rows4)       7             7               256
+//   64 x 128              20, 25        22, 31          256, 512
+//   128 x 128             25, 40        37, 58          256, 512
+//   256 x 256             64, 107       64, 107         256
+// and 1 us per round besides, 6 with groups, whose tiles begin with two dependent
+// lookups. Rows of a group are not known here, only their mean: its last tile is taken
+// to be half full. Model and kernels: 100 x 4096 x 4096 rows4 28, 64 x 128 21, 128 x 128 24
+// us; 512 x 14336 x 4096 47, 34 (128 x 128), 51 (256 x 256); 2000 x 8192 x 4096 85, 69,
+// 62; 8192^3 825, 532, 432. Groups of at most 5 rows in the mean run on the row
+// kernel (64 tokens' slots on 128 experts of 1536 x 2048 with SwiGLU: 42 us, 64 x 128
+// 50; of 128 tokens 56 and 55).
+Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool exact) {
   Mx8GemmPlan p{};
-  const int64_t waves = ((int64_t)cols + 15) / 16 * std::min(M, G);
-  p.kernel = M <= 16 && waves <= 1024 ? Mx8GemmPlan::kRows4 : Mx8GemmPlan::kRows;
+  const int64_t groups = std::min(M, G);
+  if (G > 1 && M <= 5 * groups) {
+    p.kernel = Mx8GemmPlan::kRows;
+    return p;
+  }
+  p.kernel = Mx8GemmPlan::kTile64;
+  double best = 0;
+  auto offer = [&](Mx8GemmPlan::Kernel k, int64_t bm, int64_t bn, int at_once, double half, double full) {
+    const int64_t rows = G > 1 ? (M + groups * (bm / 2)) / bm : (M + bm - 1) / bm;
+    const int64_t tiles = rows * (((int64_t)N + bn - 1) / bn), whole = tiles / at_once, rest = tiles % at_once;
+    const double k4 = Kp / 4096., besides = G > 1 ? 6 : 1;
+    const double us = whole * (full * k4 + besides) + (rest == 0 ? 0 : (rest <= 256 ? half : full) * k4 + besides);
+    if (best == 0 || us < best) {
+      best = us;
+      p.kernel = k;
+    }
+  };
+  offer(Mx8GemmPlan::kTile64, 64, 128, 512, exact ? 25 : 20, exact ? 31 : 22);
+  offer(Mx8GemmPlan::kTile128, 128, 128, 512, exact ? 40 : 25, exact ? 58 : 37);
+  offer(Mx8GemmPlan::kTile256, 256, 256, 256, exact ? 107 : 64, exact ? 107 : 64);
+  offer(Mx8GemmPlan::kRows4, 16, 32, 256, 7, 7);
   return p;
 }
 
-hipError_t launch_mx8_gemm(const Mx8GemmArgs& a, hipStream_t s) {
-  const bool mx8 = a.out_scales != nullptr;
-  if (a.act == LX_ACT_SWIGLU) return mx8 ? launch<true, true>(a, s) : launch<true, false>(a, s);
-  return mx8 ? launch<false, true>(a, s) : launch<false, false>(a, s);
-}
+hipError_t launch_mx8_gemm(const Mx8GemmArgs& a, hipStream_t s) { return a.act == LX_ACT_SWIGLU ? launch<true>(a, s) : launch<false>(a, s); }
 
 }  // namespace lx

@@ -122,9 +122,10 @@ hipError_t launch_mx4_gemm_sum(const Mx4GemmArgs& a, hipStream_t s);
 
 // Products of 8-bit activations and 4-bit weights.
 struct Mx8GemmPlan {
-  enum Kernel : int32_t { kRows, kRows4 } kernel;
+  enum Kernel : int32_t { kRows, kRows4, kTile64, kTile128, kTile256 } kernel;
 };
-Mx8GemmPlan mx8_gemm_plan(int M, int cols, int Kp, int G);
+// exact: the result is in fp32 or 8 bits (two instructions per product).
+Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool exact);
 struct Mx8GemmArgs {
   const uint8_t *a, *as, *b, *bs;
   int32_t a_rows;
