@@ -182,17 +182,19 @@ lx_status check_few(int32_t T, int32_t k, int32_t E, int32_t d, int32_t f) {
   return LX_OK;
 }
 
-struct FewPlan {
-  int32_t units;
-  size_t mask, expert, row, hidden, total;
+struct FewLayout {
+  size_t unit, counter, part, hidden, total;
 };
-FewPlan few_plan(int32_t T, int32_t k, int32_t E, int32_t f) {
-  FewPlan p{};
-  p.units = std::min(E, T * k);
-  p.expert = p.mask + up256((size_t)p.units * 8);
-  p.row = p.expert + up256((size_t)p.units * 4);
-  p.hidden = p.row + up256((size_t)p.units * 64 * 4);
-  p.total = p.hidden + up256((size_t)T * k * 3 * f * 2);
+// Fills in a's split and the workspace's layout (for fp32 results, whose hidden
+// activations take more).
+FewLayout few_layout(FewArgs& a) {
+  a.units = std::min(a.E, a.T * a.k);
+  few_plan(a);
+  FewLayout p{};
+  p.counter = p.unit + up256((size_t)a.units * 16);
+  p.part = p.counter + up256((size_t)a.counters * 4);
+  p.hidden = p.part + (a.splits > 1 ? up256((size_t)((a.d + 15) / 16) * a.splits * a.T * 16 * 4) : 0);
+  p.total = p.hidden + up256((size_t)a.T * a.k * 3 * LX_MX4_KP(a.f) * 2);
   return p;
 }
 
@@ -442,7 +444,13 @@ lx_status lx_mx8_gemm(const void* a, const void* a_scales, int32_t a_rows, const
 size_t lx_mx4_moe_few_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t d, int32_t f) {
   clear_error();
   if (check_few(T, k, E, d, f) != LX_OK) return 0;
-  return few_plan(T, k, E, f).total;
+  FewArgs a{};
+  a.T = T;
+  a.k = k;
+  a.E = E;
+  a.d = d;
+  a.f = f;
+  return few_layout(a).total;
 }
 
 lx_status lx_mx4_moe_few(const void* x, lx_dtype x_dtype, int32_t T, int32_t d, const int32_t* topk_ids,
@@ -459,8 +467,6 @@ lx_status lx_mx4_moe_few(const void* x, lx_dtype x_dtype, int32_t T, int32_t d, 
       !al(down_scales, 4) || !al(out, 16))
     return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
   if (!workspace || !al(workspace, 256)) return set_error(LX_ERR_INVALID_ARGUMENT, "workspace null or not 256-byte aligned");
-  const FewPlan P = few_plan(T, k, E, f);
-  if (workspace_bytes < P.total) return set_error(LX_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than required");
   FewArgs a{};
   a.x = x;
   a.T = T;
@@ -470,6 +476,8 @@ lx_status lx_mx4_moe_few(const void* x, lx_dtype x_dtype, int32_t T, int32_t d, 
   a.f = f;
   a.x_f32 = x_dtype == LX_F32;
   a.out_f32 = out_dtype == LX_F32;
+  const FewLayout P = few_layout(a);
+  if (workspace_bytes < P.total) return set_error(LX_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than required");
   a.ids = topk_ids;
   a.weights = topk_weights;
   a.gu = (const uint8_t*)gate_up;
@@ -477,11 +485,10 @@ lx_status lx_mx4_moe_few(const void* x, lx_dtype x_dtype, int32_t T, int32_t d, 
   a.down = (const uint8_t*)down;
   a.down_s = (const uint8_t*)down_scales;
   a.out = out;
-  a.units = P.units;
   uint8_t* const w = (uint8_t*)workspace;
-  a.unit_mask = (uint64_t*)(w + P.mask);
-  a.unit_expert = (int32_t*)(w + P.expert);
-  a.unit_row = (int32_t*)(w + P.row);
+  a.unit = (int4*)(w + P.unit);
+  a.counter = (int32_t*)(w + P.counter);
+  a.part = (float*)(w + P.part);
   a.hidden = (uint16_t*)(w + P.hidden);
   const lx_status s1 = run("moe_few_up", launch_few_up, a, stream);
   return s1 != LX_OK ? s1 : run("moe_few_down", launch_few_down, a, stream);

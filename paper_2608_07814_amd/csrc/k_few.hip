@@ -9,8 +9,13 @@
 // 16 at a time; lane l holds row (token) l % 16 and, of the 128 values of a step,
 // block l / 16: 16 bytes of codes under one scale, which are four instructions'
 // operands. The sum over K does not mind that an instruction's 32 values are
-// then 8 of each block.
+// then 8 of each block. Loaded by these lanes, each quarter of a wavefront would touch
+// 16 rows for 16 bytes each (what the first-level cache looks up took two thirds of its
+// cycles, at 2.9 TB/s); so the codes go to LDS in whole lines first, to a place that is
+// the wavefront's own, and the scales, 16 bytes a row, to 16 lanes.
 #include "lx_block.h"
+#include "lx_device_once.h"
+#include "lx_groups.h"
 #include "lx_mx8.h"
 #include "lx_vec.h"
 
@@ -81,226 +86,385 @@ __device__ __forceinline__ vf4 mfma(bf8 w, const vu4& a, vf4 acc) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf8, a), acc, 0, 0, 0);
 }
 
-// Which tokens chose expert e: lane t looks at token t's k ids. The token's weight is
-// the sum over its slots of e (the same expert twice counts twice), its row of the
-// hidden activations the first of them.
+// kBatch steps of 16 rows of weights, on their way through LDS. `steps`: of a row.
+constexpr int kBatch = 4, kStage = 16 * kBatch * 64;
+
+// Asks for the codes of steps k .. k + n - 1 (n of 1 .. kBatch) of rows row .. row + 15 (of
+// rows up to `last`; later ones repeat it) into `stage`: two steps are a line of 128
+// bytes of a row, whose 16-byte chunks are XORed with (row / 2) % 8, so that the 16
+// lanes that a read serves together hit different banks. Of a single step the upper
+// chunks repeat the lower ones.
+__device__ __forceinline__ void ask_codes(const uint8_t* codes, int64_t row, int last, int steps, int k, int n, const uint8_t* stage) {
+  const int lane = threadIdx.x & 63;
+  const uint8_t* const base = codes + row * ((int64_t)steps * 64) + (int64_t)k * 64;
+#pragma unroll
+  for (int p = 0; p < kBatch / 2; ++p)
+    if (2 * p < n) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = 8 * j + lane / 8, c = (lane ^ (r >> 1)) & 7;
+        const uint32_t at = (uint32_t)min(r, last) * (uint32_t)(steps * 64) + (2 * p + 1 < n ? c : c & 3) * 16;
+        load_lds<16>(base + p * 128, at, stage + p * 2048 + j * 1024);
+      }
+    }
+}
+// This lane's codes of step i of the batch.
+__device__ __forceinline__ vu4 codes_of(const uint8_t* stage, int i) {
+  const int l16 = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
+  return *(const vu4*)(stage + (i >> 1) * 2048 + l16 * 128 + ((((i & 1) * 4 + q) ^ (l16 >> 1)) & 7) * 16);
+}
+
+// The scales of steps k .. k + n - 1: lanes 0 .. 15 of `lanes` load a row's (4 bytes a
+// step) and hand them on. A row's last 16 bytes are loaded where fewer are left.
+struct Scales {
+  vu4 w;
+};
+__device__ __forceinline__ Scales ask_scales(const uint8_t* row, int steps, int k, int n, bool lanes) {
+  Scales s{};
+  if (lanes) {
+    if (steps >= 4) {
+      s.w = *(const vu4w*)(row + min(k, steps - 4) * 4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < n) s.w[i] = *(const uint32_t*)(row + (k + i) * 4);
+    }
+  }
+  return s;
+}
+// What this lane's block of step i stands under; `from`: the lane that has its row.
+__device__ __forceinline__ float scale_of(const Scales& s, int steps, int k, int i, int from) {
+  const int late = steps >= 4 ? max(k - (steps - 4), 0) : 0, q = (threadIdx.x & 63) >> 4;
+  uint32_t w = s.w[0];
+#pragma unroll
+  for (int j = 1; j < 4; ++j) w = i + late == j ? s.w[j] : w;
+  return mx_scale((uint32_t)__builtin_amdgcn_ds_bpermute(from * 4, (int)w) >> (8 * q) & 255);
+}
+__device__ __forceinline__ void all_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void all_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Which tokens chose expert e: lane t looks at token t's k ids. Its hidden activations
+// are a row of their own: the tokens of an expert follow each other from `base` on, the
+// number of slots of lower experts.
 struct Chosen {
   uint64_t mask;  // uniform: tokens with a slot of e
-  float weight;   // this lane's token
-  int row;
+  int base;       // uniform
+  int slot;       // this lane's token's first slot of e, -1: none
 };
-__device__ __forceinline__ Chosen chosen(const FewArgs& a, int e) {
+// f(slot, id) for the slots of lane t's token, in order.
+template <class F>
+__device__ __forceinline__ void for_slots(const FewArgs& a, F&& f) {
   const int t = threadIdx.x & 63;
-  Chosen c{0, 0.f, -1};
-  if (t < a.T)
-    for (int j = a.k - 1; j >= 0; --j)
-      if (a.ids[t * a.k + j] == e) {
-        c.weight += a.weights[t * a.k + j];
-        c.row = t * a.k + j;
-      }
-  c.mask = __ballot(c.row >= 0);
+  if (t >= a.T) return;
+  int j = t * a.k;
+  const int end = j + a.k;
+  for (; j + 4 <= end; j += 4) {
+    const vu4w id = *(const vu4w*)(a.ids + j);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f(j + i, (int)id[i]);
+  }
+  for (; j < end; ++j) f(j, a.ids[j]);
+}
+__device__ __forceinline__ Chosen chosen(const FewArgs& a, int e) {
+  Chosen c{0, 0, -1};
+  int less = 0;
+  for_slots(a, [&](int slot, int id) __attribute__((always_inline)) {
+    if (id == e && c.slot < 0) c.slot = slot;
+    less += id >= 0 && id < e;
+  });
+  c.mask = __ballot(c.slot >= 0);
+  c.base = __builtin_amdgcn_readfirstlane((int)lane_sum<64>((float)less));  // (at most 2048)
   return c;
 }
 
-// Expert u of those that may have tokens, -1 if there is none: every expert in turn
-// where there are no more of them than slots, else the slots, each expert at the
-// first of its own.
-__device__ __forceinline__ int expert_of(const FewArgs& a, int u, Chosen& c) {
-  const bool by_slot = a.units != a.E;
-  const int e = __builtin_amdgcn_readfirstlane(by_slot ? a.ids[u] : u);
-  if (e < 0 || e >= a.E) return -1;
-  c = chosen(a, e);
-  if (!c.mask) return -1;
-  if (by_slot && __builtin_amdgcn_readlane(c.row, __builtin_ctzll(c.mask)) != u) return -1;
-  return e;
+// The tokens of a mask in order: lane i learns the i-th (the others follow).
+__device__ __forceinline__ int token_list(uint64_t mask) {
+  const int lane = threadIdx.x & 63, rank = __popcll(mask & ((1ull << lane) - 1));
+  return __builtin_amdgcn_ds_permute((mask >> lane & 1 ? rank : __popcll(mask) + lane - rank) * 4, lane);
+}
+
+// Where the hidden activations lie: those of up to 16 tokens of an expert (its tokens
+// from c0 on) together, term by term, step by step of 128, and within a step so that what
+// a load instruction of the second launch takes, 8 values of each block of every token,
+// is contiguous. `cols`: the tokens of the 16.
+__device__ __forceinline__ uint16_t* hidden_of(const FewArgs& a, int base, int c0) {
+  return a.hidden + (int64_t)(base + c0) * a.planes * LX_MX4_KP(a.f);
+}
+__device__ __forceinline__ int64_t hidden_at(int fp, int term, int step, int j, int q, int cols, int col) {
+  return ((int64_t)term * fp / 8 + ((step * 4 + j) * 4 + q)) * cols * 8 + col * 8;
 }
 
 // Gate and up projections, SwiGLU and the router's weight: 16 hidden columns of one
-// expert per workgroup, whose four wavefronts share K and add their sums in order.
-// The results go to a.hidden as three bf16 terms, row (token, first slot) by row.
+// expert per workgroup, whose four wavefronts share K and meet in LDS. A unit is an
+// expert where there are no more of them than slots, else a slot, of which each expert's
+// first does the work. Many short workgroups hide each other's waits: several tiles
+// to a workgroup, the next one's weights on their way, took 100 us for 73 (61 tokens on
+// 128 experts of 768 x 2048). The results go to a.hidden as bf16 terms.
 template <bool F32>
-__global__ __launch_bounds__(256) void k_few_up(const FewArgs a) {
+__global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
   constexpr int N = F32 ? 3 : 1;
-  __shared__ float part[3][2][256];
+  __shared__ __attribute__((aligned(16))) uint8_t stage[4][2][kStage];
+  __shared__ float weight[64];
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tiles = (a.f + 15) / 16, u = blockIdx.x / tiles, n0 = blockIdx.x % tiles * 16;
-  Chosen c{};
-  const int e = expert_of(a, u, c);
-  if (n0 == 0 && wave == 0) {  // for the second launch
-    if (lane == 0) a.unit_mask[u] = e < 0 ? 0 : c.mask, a.unit_expert[u] = e;
-    if (e >= 0 && c.row >= 0) a.unit_row[u * 64 + lane] = c.row;
+  const int fp = LX_MX4_KP(a.f), tiles = fp / 16, u = blockIdx.x / tiles, n0 = blockIdx.x % tiles * 16;
+  // (the second launch counts the workgroups that are done with a column tile)
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < a.counters; i += gridDim.x * 256) a.counter[i] = 0;
+  const bool by_slot = a.units != a.E;
+  const int e = __builtin_amdgcn_readfirstlane(by_slot ? a.ids[u] : u);
+  const bool valid = e >= 0 && e < a.E;
+  Chosen c{0, 0, -1};
+  if (valid) c = chosen(a, e);
+  const bool live = c.mask && !(by_slot && __builtin_amdgcn_readlane(c.slot, __builtin_ctzll(c.mask | 1ull << 63)) != u);
+  if (n0 == 0 && threadIdx.x == 0)  // for the second launch
+    a.unit[u] = make_int4(live ? e : -1, c.base, (int)c.mask, (int)(c.mask >> 32));
+  if (!live) return;
+  const int count = __popcll(c.mask), token = token_list(c.mask);
+  // a token's weight is the sum over its slots of e (the same expert twice counts twice)
+  if (wave == 0) {
+    float s = 0.f;
+    for_slots(a, [&](int slot, int id) __attribute__((always_inline)) {
+      const float w = a.weights[slot];
+      s += id == e ? w : 0.f;
+    });
+    if (c.slot >= 0) weight[__popcll(c.mask & ((1ull << lane) - 1))] = s;
   }
-  if (e < 0) return;
-  const int dp = LX_MX4_KP(a.d), cp = dp / 2, sp = dp / 32, steps = dp / 128;
-  const int rank = __popcll(c.mask & ((1ull << lane) - 1));
-  // the tokens in order, the chosen ones first: lane i learns the i-th
-  const int count = __popcll(c.mask);
-  const int token = __builtin_amdgcn_ds_permute((c.row >= 0 ? rank : count + lane - rank) * 4, lane);
-  const int64_t grow = (int64_t)e * 2 * a.f + min(n0 + l16, a.f - 1);
-  const uint8_t* const G = a.gu + grow * cp + q * 16;
-  const uint8_t* const Gs = a.gu_s + grow * sp + q;
-  const int64_t up = (int64_t)a.f * cp, ups = (int64_t)a.f * sp;
-  const int k0 = steps * wave / 4, k1 = steps * (wave + 1) / 4;
+  // (past f the rows are padded with zeros)
+  const bool padding = n0 >= a.f;
+  const int steps = LX_MX4_KP(a.d) / 128, sp = steps * 4, k0 = steps * wave / 4, k1 = steps * (wave + 1) / 4;
+  const int64_t row = (int64_t)e * 2 * a.f + (padding ? 0 : n0);
+  const int last = padding ? 0 : min(a.f - 1 - n0, 15);
+  // lanes 0 .. 15: scales of the gate rows, 16 .. 31: of the up rows
+  const uint8_t* const my_scales = a.gu_s + (row + (lane & 16 ? a.f : 0) + min(l16, last)) * sp;
+  uint8_t *const sg = stage[wave][0], *const su = stage[wave][1];
   for (int c0 = 0; c0 < count; c0 += 16) {
-    const int col = c0 + l16;
-    const int t = __builtin_amdgcn_ds_bpermute(min(col, count - 1) * 4, token);
-    const void* const x = col < count ? (const uint8_t*)a.x + (int64_t)t * a.d * (F32 ? 4 : 2) : nullptr;
+    const int t = __builtin_amdgcn_ds_bpermute(min(c0 + l16, count - 1) * 4, token);
+    const void* const x = c0 + l16 < count ? (const uint8_t*)a.x + (int64_t)t * a.d * (F32 ? 4 : 2) : nullptr;
     vf4 ag = {0.f, 0.f, 0.f, 0.f}, au = ag;
-    auto batch = [&](auto cnt, int k) __attribute__((always_inline)) {
-      constexpr int U = decltype(cnt)::value;
-      vu4 wg[U], wu[U];
-      uint32_t sg[U], su[U];
+    for (int k = k0; k < k1 && !padding; k += kBatch) {
+      const int n = min(k1 - k, kBatch);
+      all_read();  // (the batch before)
+      ask_codes(a.gu, row, last, steps, k, n, sg);
+      ask_codes(a.gu, row + a.f, last, steps, k, n, su);
+      const Scales sc = ask_scales(my_scales, steps, k, n, lane < 32);
+      // activations: of all steps (bf16), or step by step (fp32, whose terms take more)
+      constexpr int HELD = F32 ? 1 : kBatch;
+      Acts<N, F32> v[HELD][4];
+      auto acts = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        wg[i] = *(const vu4*)(G + (int64_t)(k + i) * 64);
-        wu[i] = *(const vu4*)(G + up + (int64_t)(k + i) * 64);
-        sg[i] = Gs[(k + i) * 4];
-        su[i] = Gs[ups + (k + i) * 4];
+        for (int j = 0; j < 4; ++j) v[i % HELD][j].load(x, (k + i) * 128 + q * 32 + j * 8, a.d);
+      };
+      if constexpr (HELD > 1) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          if (i < n) acts(i);
       }
+      all_landed();
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const float fg = mx_scale(sg[i]), fu = mx_scale(su[i]);
+      for (int i = 0; i < kBatch; ++i)
+        if (i < n) {
+          if constexpr (HELD == 1) acts(i);
+          const float fg = scale_of(sc, steps, k, i, l16), fu = scale_of(sc, steps, k, i, 16 + l16);
+          const vu4 wg = codes_of(sg, i), wu = codes_of(su, i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          Acts<N, F32> v;
-          v.load(x, (k + i) * 128 + q * 32 + j * 8, a.d);
-          const bf8 g = read8(wg[i][j], fg), w = read8(wu[i][j], fu);
+          for (int j = 0; j < 4; ++j) {
+            const bf8 g = read8(wg[j], fg), z = read8(wu[j], fu);
 #pragma unroll
-          for (int n = N - 1; n >= 0; --n) {
-            ag = mfma(g, v.t[n], ag);
-            au = mfma(w, v.t[n], au);
+            for (int m = N - 1; m >= 0; --m) {
+              ag = mfma(g, v[i % HELD][j].t[m], ag);
+              au = mfma(z, v[i % HELD][j].t[m], au);
+            }
           }
         }
-      }
-    };
-    int k = k0;
-    for (; k + 4 <= k1; k += 4) batch(std::integral_constant<int, 4>{}, k);
-    for (; k < k1; ++k) batch(std::integral_constant<int, 1>{}, k);
-    if (wave > 0) {
-      *(vf4*)&part[wave - 1][0][lane * 4] = ag;
-      *(vf4*)&part[wave - 1][1][lane * 4] = au;
     }
+    all_read();
+    // (the sums meet where the codes were)
+    float* const part = (float*)sg;
+    *(vf4*)(part + l16 * 16 + q * 4) = ag;
+    *(vf4*)(part + 256 + l16 * 16 + q * 4) = au;
     __syncthreads();
-    if (wave == 0) {
+    const int cols = min(count - c0, 16), e8 = threadIdx.x & 7, col = (int)threadIdx.x / 8 % 16, n = (int)threadIdx.x / 128 * 8 + e8;
+    if (col < cols) {
+      float g = 0.f, z = 0.f;
 #pragma unroll
-      for (int w = 0; w < 3; ++w) {
-        ag += *(const vf4*)&part[w][0][lane * 4];
-        au += *(const vf4*)&part[w][1][lane * 4];
+      for (int i = 0; i < 4; ++i) {
+        const float* const p = (const float*)stage[i][0] + col * 16 + n;
+        g += p[0];
+        z += p[256];
       }
-      const float weight = __uint_as_float(__builtin_amdgcn_ds_bpermute(t * 4, __float_as_uint(c.weight)));
-      const int row = __builtin_amdgcn_ds_bpermute(t * 4, c.row);
-      const int n = n0 + q * 4;  // (f is a multiple of 8: all four columns exist or none)
-      Terms h[4];
+      const int at = n0 + n;
+      const Terms h = terms(at < a.f ? silu(g) * z * weight[c0 + col] : 0.f);
+      uint16_t* const p = hidden_of(a, c.base, c0) + e8;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) h[j] = terms(silu(ag[j]) * au[j] * weight);
-      if (col < count && n < a.f) {
-        uint16_t* const p = a.hidden + (int64_t)row * 3 * a.f + n;
-#pragma unroll
-        for (int m = 0; m < 3; ++m)
-          *(vu2*)(p + m * a.f) = vu2{two(h[0].t[m], h[1].t[m]), two(h[2].t[m], h[3].t[m])};
-      }
+      for (int m = 0; m < 3; ++m)
+        if (m < a.planes) p[hidden_at(fp, m, at / 128, at / 8 % 4, at / 32 % 4, cols, col)] = (uint16_t)(h.t[m] >> 16);
     }
     __syncthreads();
   }
 }
 
-// Down projections and the sum over a token's experts: 16 columns of the output per
-// workgroup, for all tokens. The NW wavefronts share the steps of all chosen
-// experts, a contiguous part each, with sums of their own in LDS for every token,
-// which are added in order at the end. TERMS of the hidden activations are
-// multiplied: for a bf16 output two (2^-16 of a value at most, next to the 2^-9 that
-// the output is rounded by), for fp32 all three.
+// Device-scope coherent store and load: another XCD's workgroup that reads the place
+// after this access has completed sees its value.
+__device__ __forceinline__ void store_dev(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float load_dev(const float* p) {
+  return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Down projections and the sum over a token's experts: 16 columns of the output, for
+// all tokens, by a.splits workgroups. Their wavefronts share the steps of all chosen
+// experts, batch by batch in turn, with sums of their own in LDS for every token, which
+// are added in order at the end: first over a workgroup's wavefronts, then, by
+// the workgroup that is done last, over the workgroups. What workgroups hand each other is
+// stored and loaded coherently and complete before the counter is raised, which is all
+// the order that it needs (fences, which write back and empty whole caches, took the
+// launch from 93 to 205 us). TERMS of the hidden
+// activations are multiplied: for a bf16 output two (2^-16 of a value at most, next to
+// the 2^-9 that the output is rounded by), for fp32 all three.
 constexpr int kDownWaves = 16;
 template <int TERMS>
-__global__ __launch_bounds__(kDownWaves * 64) void k_few_down(const FewArgs a) {
-  extern __shared__ float sums[];  // [kDownWaves][T][16]
+__global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a) {
+  constexpr int U = kBatch;
+  __shared__ __attribute__((aligned(16))) uint8_t stage[kDownWaves][kStage];
+  // [kDownWaves][T][16] sums, then three words for each unit with tokens
+  extern __shared__ __attribute__((aligned(16))) float sums[];
+  int* const list = (int*)(sums + kDownWaves * a.T * 16);
+  __shared__ int done;
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n0 = blockIdx.x * 16;
+  const int split = blockIdx.x % a.splits, n0 = blockIdx.x / a.splits * 16;
   float* const mine = sums + wave * a.T * 16;
   for (int i = lane; i < a.T * 16; i += 64) mine[i] = 0.f;
-  const int fp = LX_MX4_KP(a.f), cp = fp / 2, sp = fp / 32, steps = fp / 128;
+  // every wavefront counts all units, each writes some
   int live = 0;
-  for (int u0 = 0; u0 < a.units; u0 += 64) live += __popcll(__ballot(u0 + lane < a.units && a.unit_mask[min(u0 + lane, a.units - 1)] != 0));
-  const int all = live * steps;
-  int at = (int)((int64_t)all * wave / kDownWaves);
-  const int end = (int)((int64_t)all * (wave + 1) / kDownWaves);
-  int before = 0;  // live units before u0
-  for (int u0 = 0; u0 < a.units && at < end; u0 += 64) {
-    const uint64_t m = u0 + lane < a.units ? a.unit_mask[u0 + lane] : 0;
-    uint64_t left = __ballot(m != 0);
-    const int here = __popcll(left);
-    for (int i = before; left && at < end; ++i, left &= left - 1) {
-      if (at >= (i + 1) * steps) continue;
-      const int src = __builtin_ctzll(left), u = u0 + src;
-      const uint64_t mask = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(m >> 32), src) << 32 |
-                            (uint32_t)__builtin_amdgcn_readlane((int)m, src);
-      const int e = __builtin_amdgcn_readfirstlane(a.unit_expert[u]);
-      const int k0 = at - i * steps, k1 = min(end - i * steps, steps);
-      at = i * steps + k1;
-      const int count = __popcll(mask), rank = __popcll(mask & ((1ull << lane) - 1));
-      const bool has = mask >> lane & 1;
-      const int token = __builtin_amdgcn_ds_permute((has ? rank : count + lane - rank) * 4, lane);
-      const int64_t brow = (int64_t)e * a.d + min(n0 + l16, a.d - 1);
-      const uint8_t* const D = a.down + brow * cp + q * 16;
-      const uint8_t* const Ds = a.down_s + brow * sp + q;
-      for (int c0 = 0; c0 < count; c0 += 16) {
-        const int col = c0 + l16;
-        const int t = __builtin_amdgcn_ds_bpermute(min(col, count - 1) * 4, token);
-        const int row = col < count ? a.unit_row[u * 64 + t] : -1;
-        const uint16_t* const h = row >= 0 ? a.hidden + (int64_t)row * 3 * a.f : nullptr;
-        vf4 acc = {0.f, 0.f, 0.f, 0.f};
-        auto batch = [&](auto cnt, int k) __attribute__((always_inline)) {
-          constexpr int U = decltype(cnt)::value;
-          vu4 w[U];
-          uint32_t s[U];
-#pragma unroll
-          for (int i = 0; i < U; ++i) {
-            w[i] = *(const vu4*)(D + (int64_t)(k + i) * 64);
-            s[i] = Ds[(k + i) * 4];
-          }
-#pragma unroll
-          for (int i = 0; i < U; ++i) {
-            const float f = mx_scale(s[i]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const bf8 v = read8(w[i][j], f);
-#pragma unroll
-              for (int n = TERMS - 1; n >= 0; --n) {
-                Acts<1, false> x;
-                x.load(h ? h + n * a.f : nullptr, (k + i) * 128 + q * 32 + j * 8, a.f);
-                acc = mfma(v, x.t[0], acc);
-              }
-            }
-          }
-        };
-        int k = k0;
-        for (; k + 4 <= k1; k += 4) batch(std::integral_constant<int, 4>{}, k);
-        for (; k < k1; ++k) batch(std::integral_constant<int, 1>{}, k);
-        if (col < count) *(vf4*)(mine + t * 16 + q * 4) += acc;
-      }
+#pragma unroll 2
+  for (int u0 = 0; u0 < a.units; u0 += 64) {
+    const int4 m = u0 + lane < a.units ? a.unit[u0 + lane] : make_int4(-1, 0, 0, 0);
+    const uint64_t there = __ballot(m.x >= 0);
+    if (m.x >= 0 && (u0 >> 6) % kDownWaves == wave) {
+      int* const at = list + 3 * (live + __popcll(there & ((1ull << lane) - 1)));
+      at[0] = m.x | m.y << 16;  // (E is at most 8192, a row below 2048)
+      at[1] = m.z;
+      at[2] = m.w;
     }
-    before += here;
+    live += __popcll(there);
   }
   __syncthreads();
+  const int fp = LX_MX4_KP(a.f), steps = fp / 128, sp = steps * 4;
+  // Batch b is steps kBatch (b % batches) .. of live unit b / batches: wavefronts that run
+  // together read neighbouring parts of the same rows.
+  const int batches = (steps + U - 1) / U, all = live * batches;
+  const int last = min(a.d - 1 - n0, 15);
+  int token = 0, count = 0, base = 0, expert = 0, unit = -1;
+  vf4 acc = {0.f, 0.f, 0.f, 0.f};
+  // acc into the sums of the tokens from c0 on
+  auto flush = [&](int c0) __attribute__((always_inline)) {
+    const int t = __builtin_amdgcn_ds_bpermute(min(c0 + l16, count - 1) * 4, token);
+    if (c0 + l16 < count) *(vf4*)(mine + t * 16 + q * 4) += acc;
+    acc = vf4{0.f, 0.f, 0.f, 0.f};
+  };
+  for (int b = split * kDownWaves + wave; b < all; b += a.splits * kDownWaves) {
+    const int i = b / batches, k = (b - i * batches) * U, n = min(steps - k, U);
+    if (i != unit) {
+      if (unit >= 0 && count <= 16) flush(0);
+      unit = i;
+      const int m = __builtin_amdgcn_readfirstlane(list[3 * i]);
+      expert = m & 0xFFFF;
+      base = m >> 16;
+      const uint64_t mask = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(list[3 * i + 2]) << 32 |
+                            (uint32_t)__builtin_amdgcn_readfirstlane(list[3 * i + 1]);
+      count = __popcll(mask);
+      token = token_list(mask);
+    }
+    const int64_t row = (int64_t)expert * a.d + n0;
+    all_read();  // (the batch before)
+    ask_codes(a.down, row, last, steps, k, n, stage[wave]);
+    const Scales sc = ask_scales(a.down_s + (row + min(l16, last)) * sp, steps, k, n, lane < 16);
+    for (int c0 = 0; c0 < count; c0 += 16) {
+      const int cols = min(count - c0, 16);
+      const uint8_t* const h = (const uint8_t*)hidden_of(a, base, c0);
+      const uint32_t own = (uint32_t)(q * cols + l16) * 16;  // (the rest of an address is uniform)
+      // activations step by step, with two terms the next step's on their way (all of them
+      // at once would leave room for half as many wavefronts)
+      constexpr int HELD = TERMS == 2 ? 2 : 1;
+      vu4 x[HELD][4][TERMS];
+      auto acts = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int m = 0; m < TERMS; ++m) {
+            x[i % HELD][j][m] = vu4{0, 0, 0, 0};
+            if (l16 < cols)
+              x[i % HELD][j][m] = *(const vu4*)(h + hidden_at(fp, m, k + i, j, 0, cols, 0) * 2 + own);
+          }
+      };
+      acts(0);
+      all_landed();  // (for the first tokens; it also keeps the codes from being read ahead of the loop)
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (i < n) {
+          if (HELD == 2 && i + 1 < n) acts(i + 1);
+          if (HELD == 1 && i > 0) acts(i);
+          const float f = scale_of(sc, steps, k, i, l16);
+          const vu4 w = codes_of(stage[wave], i);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bf8 v = read8(w[j], f);
+#pragma unroll
+            for (int m = TERMS - 1; m >= 0; --m) acc = mfma(v, x[i % HELD][j][m], acc);
+          }
+        }
+      if (count > 16) flush(c0);
+    }
+  }
+  if (unit >= 0 && count <= 16) flush(0);
+  __syncthreads();
+  auto put = [&](int i, float s) __attribute__((always_inline)) {
+    const int n = n0 + (i & 15);
+    if (n >= a.d) return;
+    const int64_t o = (int64_t)(i >> 4) * a.d + n;
+    if (a.out_f32)
+      ((float*)a.out)[o] = s;
+    else
+      ((uint16_t*)a.out)[o] = (uint16_t)pack_bf16(s, 0.f);
+  };
+  float* const parted = a.part + (int64_t)blockIdx.x / a.splits * a.splits * a.T * 16;
   for (int i = threadIdx.x; i < a.T * 16; i += kDownWaves * 64) {
     float s = 0.f;
 #pragma unroll
     for (int w = 0; w < kDownWaves; ++w) s += sums[w * a.T * 16 + i];
-    const int n = n0 + (i & 15);
-    if (n < a.d) {
-      const int64_t o = (int64_t)(i >> 4) * a.d + n;
-      if (a.out_f32)
-        ((float*)a.out)[o] = s;
-      else
-        ((uint16_t*)a.out)[o] = (uint16_t)pack_bf16(s, 0.f);
-    }
+    if (a.splits == 1)
+      put(i, s);
+    else
+      store_dev(parted + split * a.T * 16 + i, s);
+  }
+  if (a.splits == 1) return;
+  // the last of the workgroups adds up what they left (every one ends; none waits)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    done = __hip_atomic_fetch_add(&a.counter[blockIdx.x / a.splits], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (done != a.splits - 1) return;
+  for (int i = threadIdx.x; i < a.T * 16; i += kDownWaves * 64) {
+    float s = 0.f;
+    for (int w = 0; w < a.splits; ++w) s += load_dev(parted + w * a.T * 16 + i);
+    put(i, s);
   }
 }
 
 }  // namespace
 
+// Workgroups of a column tile of the second launch: so many that every compute unit has
+// one, but no more than leave a wavefront a batch (4 tokens on 128 experts of 768 x 2048:
+// 17 us on 256 workgroups, 19 on 128; 61 tokens: 42 on 256, 53 on 512).
+void few_plan(FewArgs& a) {
+  const int cols = (a.d + 15) / 16;
+  const int64_t steps = (int64_t)a.units * ((a.f + 127) / 128), most = (steps + kDownWaves * kBatch - 1) / (kDownWaves * kBatch);
+  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, 256 / cols, 8}));
+  a.counters = a.splits > 1 ? cols : 0;
+  a.planes = a.out_f32 ? 3 : 2;
+}
+
 hipError_t launch_few_up(const FewArgs& a, hipStream_t s) {
-  const unsigned grid = (unsigned)a.units * ((a.f + 15) / 16);
+  const unsigned grid = (unsigned)a.units * (LX_MX4_KP(a.f) / 16);
   if (a.x_f32)
     k_few_up<true><<<grid, 256, 0, s>>>(a);
   else
@@ -308,13 +472,24 @@ hipError_t launch_few_up(const FewArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_few_down(const FewArgs& a, hipStream_t s) {
-  const unsigned grid = (a.d + 15) / 16, lds = kDownWaves * a.T * 16 * sizeof(float);
-  if (a.out_f32)
-    k_few_down<3><<<grid, kDownWaves * 64, lds, s>>>(a);
-  else
-    k_few_down<2><<<grid, kDownWaves * 64, lds, s>>>(a);
+template <int TERMS>
+static hipError_t launch_down(const FewArgs& a, hipStream_t s) {
+  // next to the codes' 32 KB the sums and the units take more than 64 KB can hold
+  static DeviceOnce once;
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e == hipSuccess)
+    e = once.run(device, hipSuccess, [] {
+      return hipFuncSetAttribute((const void*)k_few_down<TERMS>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                 LX_MOE_FEW_MAX_T * (kDownWaves * 16 * (int)sizeof(float) + LX_MAX_K * 12));
+    });
+  if (e != hipSuccess) return e;
+  const unsigned grid = (unsigned)((a.d + 15) / 16) * a.splits;
+  const size_t lds = a.units * 12 + (size_t)kDownWaves * a.T * 16 * sizeof(float);
+  k_few_down<TERMS><<<grid, kDownWaves * 64, lds, s>>>(a);
   return hipGetLastError();
 }
+
+hipError_t launch_few_down(const FewArgs& a, hipStream_t s) { return a.out_f32 ? launch_down<3>(a, s) : launch_down<2>(a, s); }
 
 }  // namespace lx

@@ -95,7 +95,8 @@ def tokens(T, d, dtype, seed=0):
 
 SIZES = [(1, 1, 1, 8, 8), (1, 8, 128, 256, 64), (1, 2, 8, 2048, 768), (2, 3, 5, 136, 40), (5, 2, 8, 264, 1000), (16, 4, 16, 512, 96),
          (17, 1, 2, 128, 128), (33, 8, 64, 640, 72), (61, 8, 128, 256, 200), (64, 6, 6, 120, 24), (64, 32, 40, 64, 32), (3, 2, 300, 64, 48),
-         (64, 1, 1, 72, 520), (40, 2, 3, 1032, 8)]
+         (64, 1, 1, 72, 520), (40, 2, 3, 1032, 8), (64, 32, 2100, 64, 8), (9, 3, 7, 24, 4096),
+         (37, 5, 20, 2056, 776), (30, 8, 9, 768, 1544)]
 
 
 @pytest.mark.parametrize("T,k,E,d,f", SIZES)
