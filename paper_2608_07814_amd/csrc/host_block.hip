@@ -191,7 +191,7 @@ FewLayout few_layout(FewArgs& a) {
   a.units = std::min(a.E, a.T * a.k);
   few_plan(a);
   FewLayout p{};
-  p.counter = p.unit + up256((size_t)a.units * 16);
+  p.counter = p.unit + up256((size_t)a.units * sizeof(FewUnit));
   p.part = p.counter + up256((size_t)a.counters * 4);
   p.hidden = p.part + (a.splits > 1 ? up256((size_t)((a.d + 15) / 16) * a.splits * a.T * 16 * 4) : 0);
   p.total = p.hidden + up256((size_t)a.T * a.k * 3 * LX_MX4_KP(a.f) * 2);
@@ -486,7 +486,7 @@ lx_status lx_mx4_moe_few(const void* x, lx_dtype x_dtype, int32_t T, int32_t d, 
   a.down_s = (const uint8_t*)down_scales;
   a.out = out;
   uint8_t* const w = (uint8_t*)workspace;
-  a.unit = (int4*)(w + P.unit);
+  a.unit = (FewUnit*)(w + P.unit);
   a.counter = (int32_t*)(w + P.counter);
   a.part = (float*)(w + P.part);
   a.hidden = (uint16_t*)(w + P.hidden);

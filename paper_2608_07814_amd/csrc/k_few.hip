@@ -17,6 +17,7 @@
 #include "lx_device_once.h"
 #include "lx_groups.h"
 #include "lx_mx8.h"
+#include "lx_silu.h"
 #include "lx_vec.h"
 
 #include <algorithm>
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
   if (valid) c = chosen(a, e);
   const bool live = c.mask && !(by_slot && __builtin_amdgcn_readlane(c.slot, __builtin_ctzll(c.mask | 1ull << 63)) != u);
   if (n0 == 0 && threadIdx.x == 0)  // for the second launch
-    a.unit[u] = make_int4(live ? e : -1, c.base, (int)c.mask, (int)(c.mask >> 32));
+    a.unit[u] = FewUnit{live ? e : -1, c.base, c.mask};
   if (!live) return;
   const int count = __popcll(c.mask), token = token_list(c.mask);
   // a token's weight is the sum over its slots of e (the same expert twice counts twice)
@@ -336,13 +337,13 @@ __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a
   int live = 0;
 #pragma unroll 2
   for (int u0 = 0; u0 < a.units; u0 += 64) {
-    const int4 m = u0 + lane < a.units ? a.unit[u0 + lane] : make_int4(-1, 0, 0, 0);
-    const uint64_t there = __ballot(m.x >= 0);
-    if (m.x >= 0 && (u0 >> 6) % kDownWaves == wave) {
+    const FewUnit m = u0 + lane < a.units ? a.unit[u0 + lane] : FewUnit{-1, 0, 0};
+    const uint64_t there = __ballot(m.expert >= 0);
+    if (m.expert >= 0 && (u0 >> 6) % kDownWaves == wave) {
       int* const at = list + 3 * (live + __popcll(there & ((1ull << lane) - 1)));
-      at[0] = m.x | m.y << 16;  // (E is at most 8192, a row below 2048)
-      at[1] = m.z;
-      at[2] = m.w;
+      at[0] = m.expert | m.base << 16;  // (E is at most 8192, a row below 2048)
+      at[1] = (int)m.mask;
+      at[2] = (int)(m.mask >> 32);
     }
     live += __popcll(there);
   }

@@ -4,6 +4,7 @@
 #include "lx_block.h"
 #include "lx_groups.h"
 #include "lx_mx8.h"
+#include "lx_silu.h"
 #include "lx_vec.h"
 
 #include <algorithm>

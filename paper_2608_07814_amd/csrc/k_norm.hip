@@ -19,10 +19,10 @@
 namespace lx {
 namespace {
 
-template <int TPR, int NV, bool DROP = false>
+template <int TPR, int NV, bool DROP = false, bool LEAN = false>
 __global__ __launch_bounds__(kFwdThreads<TPR>) void k_block_norm(const NormArgs a) {
   __shared__ float lds[2 * kFwdThreads<TPR> / 64];
-  block_norm_rows<TPR, NV, DROP>(a, lds, [&](int64_t t, int col, bool in, bool live, const F8& x) __attribute__((always_inline)) {
+  block_norm_rows<TPR, NV, DROP, LEAN>(a, lds, [&](int64_t t, int col, bool in, bool live, const F8& x) __attribute__((always_inline)) {
     if (in && live) store8(a.x, a.x_f32, t * a.d + col, x);
   });
 }
@@ -267,10 +267,11 @@ hipError_t launch_block_norm(const NormArgs& a, hipStream_t s) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, THR = kFwdThreads<TPR>;
     constexpr int RPB = THR / TPR;
     const int grid = (int)std::min<int64_t>(((int64_t)a.T + RPB - 1) / RPB, 256 * (2048 / THR));
+    const bool lean = norm_lean(a);
     if (a.drop.rng)
-      k_block_norm<TPR, NV, true><<<grid, THR, 0, s>>>(a);
+      lean ? k_block_norm<TPR, NV, true, true><<<grid, THR, 0, s>>>(a) : k_block_norm<TPR, NV, true><<<grid, THR, 0, s>>>(a);
     else
-      k_block_norm<TPR, NV><<<grid, THR, 0, s>>>(a);
+      lean ? k_block_norm<TPR, NV, false, true><<<grid, THR, 0, s>>>(a) : k_block_norm<TPR, NV><<<grid, THR, 0, s>>>(a);
     return hipGetLastError();
   });
 }

@@ -11,12 +11,12 @@
 namespace lx {
 namespace {
 
-template <int TPR, int NV>
+template <int TPR, int NV, bool LEAN>
 __global__ __launch_bounds__(kFwdThreads<TPR>) void k_block_norm_mx8(const Norm8Args a) {
   __shared__ float lds[2 * kFwdThreads<TPR> / 64];
   const int Kp = LX_MX8_KP(a.d);
   uint8_t* const codes = (uint8_t*)a.x;
-  block_norm_rows<TPR, NV, false>(a, lds, [&](int64_t t, int col, bool in, bool live, F8 x) __attribute__((always_inline)) {
+  block_norm_rows<TPR, NV, false, LEAN>(a, lds, [&](int64_t t, int col, bool in, bool live, F8 x) __attribute__((always_inline)) {
     // (past d, where a zero may have met an infinite factor, the row is padded with zeros)
     if (!in) x = F8{};
     int s;
@@ -32,7 +32,10 @@ template <int TPR, int NV>
 hipError_t launch(const Norm8Args& a, hipStream_t s) {
   constexpr int THR = kFwdThreads<TPR>, RPB = THR / TPR;
   const int grid = (int)std::min<int64_t>(((int64_t)a.T + RPB - 1) / RPB, 256 * (2048 / THR));
-  k_block_norm_mx8<TPR, NV><<<grid, THR, 0, s>>>(a);
+  if (norm_lean(a))
+    k_block_norm_mx8<TPR, NV, true><<<grid, THR, 0, s>>>(a);
+  else
+    k_block_norm_mx8<TPR, NV, false><<<grid, THR, 0, s>>>(a);
   return hipGetLastError();
 }
 

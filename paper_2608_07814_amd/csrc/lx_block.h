@@ -30,6 +30,8 @@ struct NormArgs {
   void *h_out, *x;
   Dropout drop;      // of the block's output (rng null: none)
 };
+// Whether the forward has its lean form (lx_norm_rows.h).
+inline bool norm_lean(const NormArgs& a) { return !a.h_f32 && !a.w_f32 && !(a.y && a.y_f32) && !a.slot_row; }
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t s);
 // The same with x in 8 bits: x the codes, x_scales their scales.
 struct Norm8Args : NormArgs {
@@ -143,6 +145,10 @@ struct Mx8GemmArgs {
 hipError_t launch_mx8_gemm(const Mx8GemmArgs& a, hipStream_t s);
 
 // ------------------------------------------------------------ a layer for a few tokens
+struct FewUnit {
+  int32_t expert, base;
+  uint64_t mask;
+};
 struct FewArgs {
   const void* x;
   int32_t T, k, E, d, f;
@@ -155,7 +161,7 @@ struct FewArgs {
   int32_t splits, counters, planes;  // few_plan
   // left by the first launch for the second, per unit: its expert (-1: it has no
   // tokens), the first of its rows of hidden, and its tokens as bits
-  int4* unit;            // [units]
+  FewUnit* unit;         // [units]
   uint16_t* hidden;      // [T k][planes][LX_MX4_KP(f)]: bf16 terms
   int32_t* counter;      // [counters], cleared by the first launch
   float* part;           // splits > 1: [d / 16][splits][T][16]

@@ -3,6 +3,8 @@
 // input. Included after lx_block.h.
 #pragma once
 
+#include <type_traits>
+
 #include "lx_philox.h"
 #include "lx_vec.h"
 
@@ -39,10 +41,15 @@ constexpr int kFwdThreads = TPR < 256 ? 256 : TPR;
 
 // One workgroup's rows. put(t, column, whether the column exists, whether the row
 // does, 8 values) is called by all lanes; lds: 2 floats per wavefront. DROP: the
-// block's output is dropped out.
-template <int TPR, int NV, bool DROP, class Put>
+// block's output is dropped out. LEAN: h, y and
+// the weights are bf16 and there are no slots, which leaves room in registers for all
+// the wavefronts that a compute unit can hold.
+template <int TPR, int NV, bool DROP, bool LEAN, class Put>
 __device__ __forceinline__ void block_norm_rows(const NormArgs& a, float* lds, Put&& put) {
   constexpr int RPB = kFwdThreads<TPR> / TPR, NW = kFwdThreads<TPR> / 64;
+  using Raw = std::conditional_t<LEAN, RawB8, Raw8>;
+  const bool slots = !LEAN && a.slot_row;
+  const bool h_f32 = !LEAN && a.h_f32, y_f32 = !LEAN && a.y_f32, w_f32 = !LEAN && a.w_f32;
   DropoutKeys keys{};
   if constexpr (DROP) keys = dropout_keys(a.drop);
   const int lt = threadIdx.x % TPR;
@@ -55,10 +62,10 @@ __device__ __forceinline__ void block_norm_rows(const NormArgs& a, float* lds, P
     in[i] = col[i] < a.d;
     sw[i] = wp[i] = F8{{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}};
     if (in[i]) {
-      if (a.w_pre) wp[i] = load8(a.w_pre, a.w_f32, col[i]);
-      if (a.w_post) sw[i] = load8(a.w_post, a.w_f32, col[i]);
+      if (a.w_pre) wp[i] = load8(a.w_pre, w_f32, col[i]);
+      if (a.w_post) sw[i] = load8(a.w_post, w_f32, col[i]);
       if (a.scale) {
-        const F8 q = load8(a.scale, a.w_f32, col[i]);
+        const F8 q = load8(a.scale, w_f32, col[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sw[i].v[e] *= q.v[e];
       }
@@ -72,21 +79,21 @@ __device__ __forceinline__ void block_norm_rows(const NormArgs& a, float* lds, P
     const int64_t t = t0 + g;
     const bool live = RPB == 1 || t < a.T;
     const int64_t row = t * a.d;
-    Raw8 rh[NV], ry[NV];
+    Raw rh[NV], ry[NV];
     F8 h[NV], y[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      rh[i] = ry[i] = Raw8{};
+      rh[i] = ry[i] = Raw{};
       if (in[i] && live) {
-        rh[i] = load_raw8(a.h, a.h_f32, row + col[i]);
-        if (a.y && !a.slot_row) ry[i] = load_raw8(a.y, a.y_f32, row + col[i]);
+        rh[i] = load_as<Raw>(a.h, h_f32, row + col[i]);
+        if (a.y && !slots) ry[i] = load_as<Raw>(a.y, y_f32, row + col[i]);
       }
     }
     if (a.y) {
       const float gate = a.gate && live ? a.gate[t] : 1.f;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) y[i] = a.slot_row ? F8{} : unpack8(ry[i], a.y_f32);
-      if (a.slot_row && a.y_rows > 0 && live) {
+      for (int i = 0; i < NV; ++i) y[i] = slots ? F8{} : unpack8(ry[i], y_f32);
+      if (slots && a.y_rows > 0 && live) {
         // four slots' rows at a time; a dropped slot reads row 0 and adds nothing
         for (int j0 = 0; j0 < a.k; j0 += 4) {
           int r[4];
@@ -99,16 +106,16 @@ __device__ __forceinline__ void block_norm_rows(const NormArgs& a, float* lds, P
           }
 #pragma unroll
           for (int i = 0; i < NV; ++i) {
-            Raw8 q[4];
+            Raw q[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              q[j] = Raw8{};
-              if (in[i]) q[j] = load_raw8(a.y, a.y_f32, (int64_t)max(r[j], 0) * a.d + col[i]);
+              q[j] = Raw{};
+              if (in[i]) q[j] = load_as<Raw>(a.y, y_f32, (int64_t)max(r[j], 0) * a.d + col[i]);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               if (r[j] >= 0) {
-                const F8 v = unpack8(q[j], a.y_f32);
+                const F8 v = unpack8(q[j], y_f32);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[i].v[e] += w[j] * v.v[e];
               }
@@ -127,7 +134,7 @@ __device__ __forceinline__ void block_norm_rows(const NormArgs& a, float* lds, P
       }
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        h[i] = unpack8(rh[i], a.h_f32);
+        h[i] = unpack8(rh[i], h_f32);
         if constexpr (DROP) {
           const uint32_t kept = dropout_kept(a.drop, keys, col[i] / 8, (uint32_t)t);
 #pragma unroll
@@ -135,11 +142,11 @@ __device__ __forceinline__ void block_norm_rows(const NormArgs& a, float* lds, P
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[i].v[e] = a.alpha * h[i].v[e] + f * (y[i].v[e] * sw[i].v[e]);
-        if (in[i] && live) store8(a.h_out, a.h_f32, row + col[i], h[i]);
+        if (in[i] && live) store8(a.h_out, h_f32, row + col[i], h[i]);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) h[i] = unpack8(rh[i], a.h_f32);
+      for (int i = 0; i < NV; ++i) h[i] = unpack8(rh[i], h_f32);
     }
     if (a.w_pre) {
       float s[1] = {0.f};

@@ -98,13 +98,6 @@ __device__ __forceinline__ void store8_any(void* p, bool f32, int64_t i, const F
   }
 }
 
-// z / (1 + exp(-z)) by the exponential and reciprocal instructions (an ulp each, and
-// |z| 2^-24 from the product that is the exponent). Far below 0 the exponential is
-// infinite and the result -0.
-__device__ __forceinline__ float silu(float z) {
-  return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
-}
-
 // The value of the lane that DPP control C selects (all lanes active).
 template <int C>
 __device__ __forceinline__ float dpp(float x) {
