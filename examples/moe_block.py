@@ -1,7 +1,7 @@
 """A MoE block with its experts in 4 bits: a prompt, then single tokens from a HIP
 graph, then the gradients of a training step around the experts.
 
-    python examples/moe_block.py [--experts 128 --d 2048 --f 768 --k 8 --tokens 4096]
+    python examples/moe_block.py [--experts 128 --d 2048 --f 768 --k 8 --tokens 4096 --activations mx8]
 
 Random weights with the distributions of the library's synthetic layers.
 """
@@ -31,6 +31,9 @@ def main():
     p = argparse.ArgumentParser()
     for name, v in (("experts", 128), ("d", 2048), ("f", 768), ("k", 8), ("tokens", 4096), ("decode", 16)):
         p.add_argument("--" + name, type=int, default=v)
+    p.add_argument("--activations", choices=("mx4", "mx8"), default="mx4", help="of the prompt")
+    p.add_argument("--decode-activations", choices=("mx4", "mx8", "full"), default="mx4", help="of the single tokens")
+    p.add_argument("--dropout", type=float, default=0.0, help="of the experts' sum, in the training step")
     a = p.parse_args()
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
@@ -40,7 +43,8 @@ def main():
     experts = lb.mx4_experts(*w)
     del w
     w_r, w_pre, w_post, w_next = r(E, d).bfloat16(), *(1 + 0.1 * r(3, d)).bfloat16()
-    block = lambda h: lb.mx4_moe_block(h, w_pre, w_r, experts, a.k, w_post=w_post, w_next=w_next, balance_coef=0.01)  # noqa: E731
+    block = lambda h, activations=a.activations: lb.mx4_moe_block(  # noqa: E731
+        h, w_pre, w_r, experts, a.k, w_post=w_post, w_next=w_next, balance_coef=0.01, activations=activations)
 
     h = r(a.tokens, d).bfloat16()
     out = block(h)
@@ -53,11 +57,11 @@ def main():
     side.wait_stream(torch.cuda.current_stream())  # (the current stream makes hd)
     with torch.cuda.stream(side):
         for _ in range(2):
-            eager = block(hd)
+            eager = block(hd, a.decode_activations)
         side.synchronize()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=side):
-            replayed = block(hd)
+            replayed = block(hd, a.decode_activations)
     torch.cuda.current_stream().wait_stream(side)
     graph.replay()
     torch.cuda.synchronize()
@@ -68,12 +72,20 @@ def main():
     # the next block's input to those of the stream, the experts' sum, the norms and
     # the router
     y = r(a.tokens, d).bfloat16()  # the experts' sum, as a training forward keeps it
-    h_out, x_next = lb.block_norm(h, y, w_pre=w_next, w_post=w_post)
+    norms = dict(w_pre=w_next, w_post=w_post)
+    if a.dropout:
+        rng = torch.tensor([1234, 0], device="cuda")  # the generator's seed, and an offset that each step moves on
+        h_out, x_next = lb.block_norm_dropout(h, y, a.dropout, rng, **norms)
+    else:
+        h_out, x_next = lb.block_norm(h, y, **norms)
     w_r32, x32 = w_r.float(), out.x.float()  # (the router's gradients are formed in fp32, as its logits are)
     dh_out, dx_next = r(a.tokens, d).bfloat16(), r(a.tokens, d).bfloat16()
 
     def step():
-        after = lb.block_norm_backward(h_out, y, dx_next, dh_out, w_pre=w_next, w_post=w_post)
+        if a.dropout:
+            after = lb.block_norm_dropout_backward(h_out, y, dx_next, dh_out, a.dropout, rng, **norms)
+        else:
+            after = lb.block_norm_backward(h_out, y, dx_next, dh_out, **norms)
         dlogits = lb.balance_loss_backward(out.logits, out.balance.counts, out.balance.n_tokens, a.k, coef=0.01)
         dx = dlogits @ w_r32  # (the experts' own gradient would be added here)
         before = lb.block_norm_backward(h, None, dx, after.dh, w_pre=w_pre)

@@ -282,12 +282,13 @@ lx_status lx_mx8_gemm(const void* a, const void* a_scales, int32_t a_rows, const
 /* lx_block_norm whose x is rounded to 8 bits as lx_mx8_quantize rounds the
  * unrounded fp32 x: codes [T][LX_MX8_KP(d)] (16-byte aligned) and scales
  * [T][LX_MX8_KP(d) / 32] (4-byte aligned), padding included; both are given, as
- * is w_pre, and layer.x_dtype is not looked at. Its gradients are
+ * is w_pre. x NULL, or [T][d] of layer.x_dtype: it is written too (for a router).
+ * Its gradients are
  * lx_block_norm_backward's, from the gradient of the values (the rounding passes
  * it on). */
 lx_status lx_block_norm_mx8(const lx_norm_layer* layer, int32_t T, const void* h, const void* y, int32_t y_rows,
-                            int32_t k, const int32_t* slot_row, const float* slot_weights, void* h_out, void* x_codes,
-                            void* x_scales, void* stream);
+                            int32_t k, const int32_t* slot_row, const float* slot_weights, void* h_out, void* x,
+                            void* x_codes, void* x_scales, void* stream);
 
 #ifdef __cplusplus
 }

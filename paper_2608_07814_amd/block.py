@@ -66,7 +66,7 @@ EXPORTS = {
     "lx_mx4_moe_few_workspace_bytes": (_c_size, [_c_i32] * 5),
     "lx_mx4_moe_few": (_c_i32, [_c_void, _c_i32, _c_i32, _c_i32, _c_void, _c_void, _c_i32, _c_i32, _c_i32] + [_c_void] * 5
                        + [_c_i32, _c_void, _c_size, _c_void]),
-    "lx_block_norm_mx8": (_c_i32, [_c_void, _c_i32, _c_void, _c_void, _c_i32, _c_i32] + [_c_void] * 6),
+    "lx_block_norm_mx8": (_c_i32, [_c_void, _c_i32, _c_void, _c_void, _c_i32, _c_i32] + [_c_void] * 7),
     "lx_block_norm_dropout": (_c_i32, [_c_void, _c_void, _c_i32] + [_c_void] * 5),
     "lx_block_norm_dropout_backward": (_c_i32, [_c_void, _c_void, _c_i32] + [_c_void] * 11 + [_c_size, _c_void]),
     "lx_mx8_quantize": (_c_i32, [_c_void, _c_i32, _c_i64, _c_i32, _c_i32, _c_void, _c_void, _c_void]),
@@ -237,7 +237,8 @@ def block_norm(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: Opti
     return _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residual_scale, eps, h_out, x, x_dtype, None, gpu)
 
 
-def _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residual_scale, eps, h_out, x, x_dtype, dropout, gpu):
+def _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residual_scale, eps, h_out, x, x_dtype, dropout, gpu,
+                x_values=None):
     T, d = shape = h.shape
     k = y_rows = 0
     yp = None
@@ -260,7 +261,8 @@ def _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residu
             raise ValueError("x goes with w_pre")
     elif x is None and x_dtype is not Mx8:
         x = h.new_empty(shape, dtype=x_dtype)
-    s = _norm_layer(h, y, LX_BF16 if x is None or x_dtype is Mx8 else _dtype("x", x), w_pre, w_post, scale, gate, residual_scale, eps, T, d, gpu)
+    plain = x_values if x_dtype is Mx8 else x  # x as a tensor
+    s = _norm_layer(h, y, LX_BF16 if plain is None else _dtype("x", plain), w_pre, w_post, scale, gate, residual_scale, eps, T, d, gpu)
     hp, op = _arg("h", h, shape, None, gpu), _arg("h_out", h_out, shape, h.dtype, gpu)
     if x_dtype is Mx8:
         Kp = mx4_padded(d)
@@ -268,7 +270,7 @@ def _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residu
             x = Mx8(h.new_empty((T, Kp), dtype=torch.uint8), h.new_empty((T, Kp // 32), dtype=torch.uint8), d)
         elif x.K != d:
             raise ValueError("x.K does not fit h")
-        xp = _arg("x codes", x.codes, (T, Kp), torch.uint8, gpu), _arg("x scales", x.scales, (T, Kp // 32), torch.uint8, gpu)
+        xp = _arg("x_values", x_values, shape, None, gpu), _arg("x codes", x.codes, (T, Kp), torch.uint8, gpu), _arg("x scales", x.scales, (T, Kp // 32), torch.uint8, gpu)
     else:
         xp = (_arg("x", x, shape, None, gpu),)
     if dropout is not None:
@@ -286,10 +288,12 @@ def block_norm_mx8(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: 
                    w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                    gate: Optional[torch.Tensor] = None, slot_row: Optional[torch.Tensor] = None,
                    slot_weights: Optional[torch.Tensor] = None, residual_scale: float = 1.0, eps: float = 1e-6,
-                   h_out: Optional[torch.Tensor] = None, x: Optional["Mx8"] = None, stream=None):
+                   h_out: Optional[torch.Tensor] = None, x: Optional["Mx8"] = None,
+                   x_values: Optional[torch.Tensor] = None, stream=None):
     """:func:`block_norm` with x in 8 bits (lx_block_norm_mx8) -> (h_out, x): what
-    :func:`mx8_gemm` reads. In training its gradients are those of
-    :func:`block_norm_backward`, from the gradient of the values that x stands for."""
+    :func:`mx8_gemm` reads. ``x_values`` [T][d] (fp32 or bf16), if given, gets x as
+    :func:`block_norm` writes it (for a router). In training its gradients are those
+    of :func:`block_norm_backward`, from the gradient of the values that x stands for."""
     if h.dim() != 2:
         raise ValueError("h must be [T][d]")
     if w_pre is None:
@@ -297,7 +301,7 @@ def block_norm_mx8(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre: 
     gpu = _gpu("h", h)
     if stream is not None or gpu != _current_device():
         return _there(block_norm_mx8, gpu, stream, locals())
-    return _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residual_scale, eps, h_out, x, Mx8, None, gpu)
+    return _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residual_scale, eps, h_out, x, Mx8, None, gpu, x_values)
 
 
 def _dropout(p: float, rng: torch.Tensor, y, gpu) -> LxDropout:
@@ -760,14 +764,21 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
                   w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                   gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0, eps: float = 1e-6,
                   w_next: Optional[torch.Tensor] = None, balance_coef: Optional[float] = None,
-                  mask: Optional[torch.Tensor] = None) -> Mx4BlockOut:
+                  mask: Optional[torch.Tensor] = None, activations: str = "mx4") -> Mx4BlockOut:
     """One MoE block with its experts in 4 bits, on the current stream: norm,
     router (lx_route_topk), bucketing (lx_bucket), the experts' products per
     group of rows with SwiGLU and rounding between them, then the experts' sum,
     norm, gate, residual and the next block's norm in one kernel. h [T][d], w_r
     [E][d] bf16 (d a multiple of 64, E of 4); the other arguments as in
     :func:`block_norm`. With ``balance_coef`` the router's logits and balance
-    loss too (tokens whose ``mask`` is 0 left out)."""
+    loss too (tokens whose ``mask`` is 0 left out). ``activations`` says how the
+    products see theirs: "mx4" in 4 bits, "mx8" in 8 (the norm rounds them, SwiGLU and
+    its rounding are the first product's epilogue), "full" not rounded (at most
+    ``MOE_FEW_MAX_T`` tokens, :func:`mx4_moe_few`)."""
+    if activations not in ("mx4", "mx8", "full"):
+        raise ValueError('activations must be "mx4", "mx8" or "full"')
+    if activations == "full" and h.shape[0] > MOE_FEW_MAX_T:
+        raise ValueError(f'activations="full" takes at most {MOE_FEW_MAX_T} tokens')
     gpu = _gpu("h", h)
     if gpu != _current_device():
         return _there(mx4_moe_block, gpu, None, locals())
@@ -778,7 +789,11 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
         raise ValueError("w_r must be [E][d], the experts [E][2f][d] and [E][d][f] for h [T][d]")
     if w_r.get_device() != gpu:
         raise ValueError(f"w_r is on {w_r.device}, h on {h.device}")
-    _, x = block_norm(h, w_pre=w_pre, eps=eps)
+    if activations == "mx8":
+        x = h.new_empty((T, d), dtype=torch.bfloat16)
+        _, x8 = block_norm_mx8(h, w_pre=w_pre, eps=eps, x_values=x)
+    else:
+        _, x = block_norm(h, w_pre=w_pre, eps=eps)
     logits = balance = None
     if not T:  # nothing to route
         ids, weights = h.new_empty((0, k), dtype=torch.int32), h.new_empty((0, k), dtype=torch.float32)
@@ -793,6 +808,10 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
     if not T:
         h_out, x_next = block_norm(h, h.new_empty((0, d), dtype=torch.float32), w_pre=w_next, w_post=w_post, scale=scale,
                                    gate=gate, residual_scale=residual_scale, eps=eps)
+        return Mx4BlockOut(h_out, x_next, x, ids, weights, logits, balance)
+    if activations == "full":
+        y = mx4_moe_few(x, ids, weights, experts)
+        h_out, x_next = block_norm(h, y, w_pre=w_next, w_post=w_post, scale=scale, gate=gate, residual_scale=residual_scale, eps=eps)
         return Mx4BlockOut(h_out, x_next, x, ids, weights, logits, balance)
     # rows of the experts: a tree without levels, whose weights bucketing does not read.
     # It takes a forward's workspace, so the tree is given small sizes: with the experts'
@@ -811,11 +830,15 @@ def mx4_moe_block(h: torch.Tensor, w_pre: torch.Tensor, w_r: torch.Tensor, exper
     slot_row = h.new_empty((T, k), dtype=torch.int32)
     _check(L.lx_bucket(ctypes.byref(tree), T, k, ids.data_ptr(), 0, row_token.data_ptr(), offsets.data_ptr(),
                        slot_row.data_ptr(), ws.data_ptr(), n, _current_raw_stream(gpu)))
-    # (gate and up projections are kept in bf16 on their way into SwiGLU: half of fp32's
-    # bytes of the block's widest rows, and their 2^-9 is small next to what follows,
-    # a rounding to 4 bits, whose steps are a quarter of a value and more)
-    gate_up = mx4_gemm(mx4_quantize(x), experts.gate_up, offsets=offsets, row_map=row_token, out_dtype=torch.bfloat16)
-    y = mx4_gemm(mx4_quantize(gate_up, act=MX4_SWIGLU), experts.down, offsets=offsets, out_dtype=torch.float32)
+    if activations == "mx8":
+        hidden = mx8_gemm(x8, experts.gate_up, offsets=offsets, row_map=row_token, act=ACT_SWIGLU, out_dtype="mx8")
+        y = mx8_gemm(hidden, experts.down, offsets=offsets, out_dtype=torch.float32)
+    else:
+        # (gate and up projections are kept in bf16 on their way into SwiGLU: half of fp32's
+        # bytes of the block's widest rows, and their 2^-9 is small next to what follows,
+        # a rounding to 4 bits, whose steps are a quarter of a value and more)
+        gate_up = mx4_gemm(mx4_quantize(x), experts.gate_up, offsets=offsets, row_map=row_token, out_dtype=torch.bfloat16)
+        y = mx4_gemm(mx4_quantize(gate_up, act=MX4_SWIGLU), experts.down, offsets=offsets, out_dtype=torch.float32)
     h_out, x_next = block_norm(h, y, w_pre=w_next, w_post=w_post, scale=scale, gate=gate, slot_row=slot_row,
                                slot_weights=weights, residual_scale=residual_scale, eps=eps)
     return Mx4BlockOut(h_out, x_next, x, ids, weights, logits, balance)

@@ -219,17 +219,20 @@ lx_status lx_block_norm(const lx_norm_layer* layer, int32_t T, const void* h, co
 }
 
 lx_status lx_block_norm_mx8(const lx_norm_layer* layer, int32_t T, const void* h, const void* y, int32_t y_rows,
-                            int32_t k, const int32_t* slot_row, const float* slot_weights, void* h_out, void* x_codes,
-                            void* x_scales, void* stream) {
+                            int32_t k, const int32_t* slot_row, const float* slot_weights, void* h_out, void* x,
+                            void* x_codes, void* x_scales, void* stream) {
   clear_error();
   if (!layer) return set_error(LX_ERR_INVALID_ARGUMENT, "layer is null");
   lx_norm_layer l = *layer;
-  l.x_dtype = LX_BF16;
+  if (!x) l.x_dtype = LX_BF16;
   Norm8Args a{};
-  const lx_status st = norm_args(a, &l, T, h, y, y_rows, k, slot_row, slot_weights, h_out, x_codes);
+  const lx_status st = norm_args(a, &l, T, h, y, y_rows, k, slot_row, slot_weights, h_out, x ? x : x_codes);
   if (st != LX_OK || T == 0) return st;
   if (!l.w_pre) return set_error(LX_ERR_INVALID_ARGUMENT, "w_pre must be given");
-  if (!x_scales || !al(x_scales, 4)) return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  if (!x_codes || !x_scales || !al(x_codes, 16) || !al(x_scales, 4))
+    return set_error(LX_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  a.x = x;
+  a.x_codes = (uint8_t*)x_codes;
   a.x_scales = (uint8_t*)x_scales;
   return run("block_norm_mx8", launch_block_norm_mx8, a, stream);
 }

@@ -15,14 +15,14 @@ template <int TPR, int NV, bool LEAN>
 __global__ __launch_bounds__(kFwdThreads<TPR>) void k_block_norm_mx8(const Norm8Args a) {
   __shared__ float lds[2 * kFwdThreads<TPR> / 64];
   const int Kp = LX_MX8_KP(a.d);
-  uint8_t* const codes = (uint8_t*)a.x;
   block_norm_rows<TPR, NV, false, LEAN>(a, lds, [&](int64_t t, int col, bool in, bool live, F8 x) __attribute__((always_inline)) {
     // (past d, where a zero may have met an infinite factor, the row is padded with zeros)
     if (!in) x = F8{};
+    if (a.x && in && live) store8(a.x, a.x_f32, t * a.d + col, x);
     int s;
     const uint2 code = mx8_round(x, s);
     if (live && col < Kp) {
-      *(uint2*)(codes + t * Kp + col) = code;
+      *(uint2*)(a.x_codes + t * Kp + col) = code;
       if ((threadIdx.x & 3) == 0) a.x_scales[t * (Kp / 32) + col / 32] = (uint8_t)s;
     }
   });

@@ -33,9 +33,9 @@ struct NormArgs {
 // Whether the forward has its lean form (lx_norm_rows.h).
 inline bool norm_lean(const NormArgs& a) { return !a.h_f32 && !a.w_f32 && !(a.y && a.y_f32) && !a.slot_row; }
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t s);
-// The same with x in 8 bits: x the codes, x_scales their scales.
+// The same with x in 8 bits too (x itself null: only these).
 struct Norm8Args : NormArgs {
-  uint8_t* x_scales;
+  uint8_t *x_codes, *x_scales;
 };
 hipError_t launch_block_norm_mx8(const Norm8Args& a, hipStream_t s);
 

@@ -258,3 +258,17 @@ def test_empty():
     h_out, q = lb.block_norm_mx8(h, h, w_pre=w)
     assert h_out.shape == (0, 64) and q.codes.shape == (0, 128) and q.scales.shape == (0, 4)
     assert lb.mx8_quantize(h).codes.shape == (0, 128) and lb.mx8_dequantize(q).shape == (0, 64)
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_norm_with_its_values_too(x):
+    require_gpu()
+    for T, d in ((3, 40), (5, 1304), (2, 8200)):
+        p = make(T, d)
+        more = {n: p[n] for n in ("w_pre", "w_post", "scale", "gate")}
+        values = torch.empty(T, d, device="cuda", dtype=DT[x])
+        h_out, q = lb.block_norm_mx8(p["h"], p["y"], **more, x_values=values)
+        ref_h, ref = lb.block_norm(p["h"], p["y"], **more, x_dtype=DT[x])
+        _, only = lb.block_norm_mx8(p["h"], p["y"], **more)
+        assert torch.equal(h_out, ref_h) and torch.equal(values, ref)
+        assert torch.equal(q.codes, only.codes) and torch.equal(q.scales, only.scales)

@@ -30,13 +30,14 @@ def layer(**kw):
     return s
 
 
-NORM = dict(T=4, h=FAKE, y=FAKE, y_rows=4, k=2, slot_row=FAKE, slot_weights=FAKE, h_out=FAKE, codes=FAKE, scales=FAKE)
+NORM = dict(T=4, h=FAKE, y=FAKE, y_rows=4, k=2, slot_row=FAKE, slot_weights=FAKE, h_out=FAKE, x=None, codes=FAKE, scales=FAKE)
 
 
 @pytest.mark.parametrize("over,call,code", [
     (dict(d=60), {}, UNS), (dict(d=lb.NORM_MAX_D + 8), {}, UNS), (dict(eps=-1.0), {}, BAD), ({}, dict(T=-1), BAD),
     ({}, dict(h=None), BAD), ({}, dict(h_out=None), BAD), ({}, dict(codes=None), BAD), ({}, dict(codes=FAKE + 8), BAD),
-    ({}, dict(scales=None), BAD), ({}, dict(scales=FAKE + 2), BAD), (dict(w_pre=None), dict(codes=None), BAD), ({}, dict(k=33), BAD),
+    ({}, dict(scales=None), BAD), ({}, dict(scales=FAKE + 2), BAD), ({}, dict(x=FAKE, codes=None), BAD), ({}, dict(x=FAKE + 8), BAD),
+    (dict(x_dtype=7), dict(x=FAKE), BAD), (dict(w_pre=None), dict(x=FAKE), BAD), (dict(w_pre=None), dict(codes=None), BAD), ({}, dict(k=33), BAD),
     ({}, dict(slot_row=None), BAD), ({}, dict(y=None), BAD), ({}, dict(T=0, h=None, codes=None, scales=None), OK),
 ])
 def test_norm_mx8(L, over, call, code):
