@@ -151,6 +151,21 @@ def test_dropped_values_are_not_looked_at():
         assert torch.equal(again.dscale, grads.dscale) and torch.equal(again.dy, grads.dy) and torch.equal(again.dh, grads.dh)
 
 
+@pytest.mark.parametrize("case", ["nan", "zeros"])
+def test_dropped_values_are_0_where_the_row_has_no_norm(case):
+    """With w_post a NaN, or a row of zeros without eps, leaves the row without finite
+    normalised values: kept ones are NaN, dropped ones count as 0 all the same."""
+    require_gpu()
+    p = make(3, 520)
+    p["y"][1] = 0
+    if case == "nan":
+        p["y"][1, 77] = float("nan")
+    keep = torch.from_numpy(O.dropout_keep(3, 520, 0.5, SEED, OFFSET) > 0).cuda()
+    h_out, _ = lb.block_norm_dropout(p["h"], p["y"], 0.5, rng_of(), w_pre=p["w_pre"], w_post=p["w_post"], gate=p["gate"], eps=0.0)
+    assert torch.equal(torch.isnan(h_out[1]), keep[1]) and torch.equal(h_out[1][~keep[1]], p["h"][1][~keep[1]])
+    assert torch.isfinite(h_out[[0, 2]]).all()
+
+
 def test_gradients_against_differences():
     """Along random directions, the mask held fixed by its key."""
     require_gpu()
