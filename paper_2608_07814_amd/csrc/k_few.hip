@@ -59,17 +59,18 @@ __device__ __forceinline__ Terms terms(float x) {
 }
 __device__ __forceinline__ uint32_t two(uint32_t lo, uint32_t hi) { return lo >> 16 | (hi & 0xFFFF0000u); }
 
-// 8 activations from column c of a row (null: zeros) as N terms.
+// 8 activations from column c of the row that begins at byte `row` of x (T d is at most
+// 2^26; not `there`: zeros) as N terms.
 template <int N, bool F32>
 struct Acts {
   vu4 t[N];
-  __device__ __forceinline__ void load(const void* row, int c, int K) {
+  __device__ __forceinline__ void load(const void* x, uint32_t row, bool there, int c, int K) {
 #pragma unroll
     for (int n = 0; n < N; ++n) t[n] = vu4{0, 0, 0, 0};
-    if (!row || c >= K) return;
+    if (!there || c >= K) return;
     if constexpr (F32) {
       static_assert(N == 3, "");
-      const vu4* const p = (const vu4*)((const float*)row + c);
+      const vu4* const p = (const vu4*)((const uint8_t*)x + (row + (uint32_t)c * 4));
       const vu4 a = p[0], b = p[1];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -78,7 +79,7 @@ struct Acts {
         for (int n = 0; n < 3; ++n) t[n][j] = two(u.t[n], v.t[n]);
       }
     } else {
-      t[0] = *(const vu4*)((const uint16_t*)row + c);
+      t[0] = *(const vu4*)((const uint8_t*)x + (row + (uint32_t)c * 2));
     }
   }
 };
@@ -198,18 +199,22 @@ __device__ __forceinline__ int64_t hidden_at(int fp, int term, int step, int j, 
 // Gate and up projections, SwiGLU and the router's weight: 16 hidden columns of one
 // expert per workgroup, whose four wavefronts share K and meet in LDS. A unit is an
 // expert where there are no more of them than slots, else a slot, of which each expert's
-// first does the work. Many short workgroups hide each other's waits: several tiles
-// to a workgroup, the next one's weights on their way, took 100 us for 73 (61 tokens on
-// 128 experts of 768 x 2048). The results go to a.hidden as bf16 terms.
+// first does the work. Many short workgroups hide each other's waits: several tiles to
+// a workgroup in turn, the next one's weights on their way, took a third longer. The
+// results go to a.hidden as bf16 terms. 61 tokens on 128 experts of 768 x 2048: 52 us,
+// the weights at 4.1 TB/s; 5 tokens on experts of 14336 x 4096: 103 us, 4.0. Tried and
+// no faster: a tile of its own for each wavefront where rows are short, x through LDS
+// (64 tokens on 8 experts 182 for 205, most others a little slower).
 template <bool F32>
 __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
   constexpr int N = F32 ? 3 : 1;
   __shared__ __attribute__((aligned(16))) uint8_t stage[4][2][kStage];
   __shared__ float weight[64];
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int fp = LX_MX4_KP(a.f), tiles = fp / 16, u = blockIdx.x / tiles, n0 = blockIdx.x % tiles * 16;
+  const int fp = LX_MX4_KP(a.f), u = blockIdx.y, n0 = blockIdx.x * 16;
   // (the second launch counts the workgroups that are done with a column tile)
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < a.counters; i += gridDim.x * 256) a.counter[i] = 0;
+  if (n0 == 0 && u == 0)
+    for (int i = threadIdx.x; i < a.counters; i += 256) a.counter[i] = 0;
   const bool by_slot = a.units != a.E;
   const int e = __builtin_amdgcn_readfirstlane(by_slot ? a.ids[u] : u);
   const bool valid = e >= 0 && e < a.E;
@@ -239,7 +244,8 @@ __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
   uint8_t *const sg = stage[wave][0], *const su = stage[wave][1];
   for (int c0 = 0; c0 < count; c0 += 16) {
     const int t = __builtin_amdgcn_ds_bpermute(min(c0 + l16, count - 1) * 4, token);
-    const void* const x = c0 + l16 < count ? (const uint8_t*)a.x + (int64_t)t * a.d * (F32 ? 4 : 2) : nullptr;
+    const uint32_t x = (uint32_t)t * (uint32_t)a.d * (F32 ? 4 : 2);
+    const bool there = c0 + l16 < count;
     vf4 ag = {0.f, 0.f, 0.f, 0.f}, au = ag;
     for (int k = k0; k < k1 && !padding; k += kBatch) {
       const int n = min(k1 - k, kBatch);
@@ -252,7 +258,7 @@ __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
       Acts<N, F32> v[HELD][4];
       auto acts = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[i % HELD][j].load(x, (k + i) * 128 + q * 32 + j * 8, a.d);
+        for (int j = 0; j < 4; ++j) v[i % HELD][j].load(a.x, x, there, (k + i) * 128 + q * 32 + j * 8, a.d);
       };
       if constexpr (HELD > 1) {
 #pragma unroll
@@ -283,7 +289,9 @@ __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
     *(vf4*)(part + l16 * 16 + q * 4) = ag;
     *(vf4*)(part + 256 + l16 * 16 + q * 4) = au;
     __syncthreads();
-    const int cols = min(count - c0, 16), e8 = threadIdx.x & 7, col = (int)threadIdx.x / 8 % 16, n = (int)threadIdx.x / 128 * 8 + e8;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // (what follows from it is not kept over the products)
+    const int cols = min(count - c0, 16), e8 = tid & 7, col = tid / 8 % 16, n = tid / 128 * 8 + e8;
     if (col < cols) {
       float g = 0.f, z = 0.f;
 #pragma unroll
@@ -465,7 +473,7 @@ void few_plan(FewArgs& a) {
 }
 
 hipError_t launch_few_up(const FewArgs& a, hipStream_t s) {
-  const unsigned grid = (unsigned)a.units * (LX_MX4_KP(a.f) / 16);
+  const dim3 grid(LX_MX4_KP(a.f) / 16, a.units);  // (in one dimension its threads can pass 32 bits)
   if (a.x_f32)
     k_few_up<true><<<grid, 256, 0, s>>>(a);
   else
@@ -475,7 +483,7 @@ hipError_t launch_few_up(const FewArgs& a, hipStream_t s) {
 
 template <int TERMS>
 static hipError_t launch_down(const FewArgs& a, hipStream_t s) {
-  // next to the codes' 32 KB the sums and the units take more than 64 KB can hold
+  // next to the codes' 64 KB the sums and the units take up to 88 KB
   static DeviceOnce once;
   int device = 0;
   hipError_t e = hipGetDevice(&device);

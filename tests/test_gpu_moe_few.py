@@ -226,3 +226,31 @@ def test_empty_and_refusals():
                 lambda: lb.mx4_moe_few(x, ids, w, ex, out_dtype=torch.float16)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_more_workgroups_than_one_dimension_holds():
+    """256 slots times rows of 2^20: 2^32 threads in the first launch. One slot names an
+    expert; the weights of the others, which nothing reads, are not there."""
+    require_gpu()
+    T, k, E, d, f = 8, 32, 8192, 8, 1 << 20
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    u8 = lambda *s, lo, hi: torch.randint(lo, hi, s, device="cuda", generator=g, dtype=torch.uint8)  # noqa: E731
+    gu = lb.Mx4(u8(2 * f, 64, lo=0, hi=255), u8(2 * f, 4, lo=124, hi=127), d)
+    dn = lb.Mx4(u8(d, f // 2, lo=0, hi=255), u8(d, f // 32, lo=118, hi=121), f)
+    gu.codes[:, d // 2:] = 0
+    x = tokens(T, d, "f32")
+    ids, w = torch.full((T, k), -1, dtype=torch.int32, device="cuda"), torch.ones(T, k, device="cuda")
+    ids[5, 9], w[5, 9] = 0, 0.75
+    L = lb.lib()
+    n = L.lx_mx4_moe_few_workspace_bytes(T, k, E, d, f)
+    ws, out = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(T, d, device="cuda")
+    st = L.lx_mx4_moe_few(x.data_ptr(), lx.LX_F32, T, d, ids.data_ptr(), w.data_ptr(), k, E, f, gu.codes.data_ptr(), gu.scales.data_ptr(),
+                          dn.codes.data_ptr(), dn.scales.data_ptr(), out.data_ptr(), lx.LX_F32, ws.data_ptr(), n,
+                          torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert st == lx.LX_OK, L.lx_last_error()
+    one = [torch.tensor([[0]], dtype=torch.int32), torch.tensor([[0.75]])]
+    ex = lb.Mx4Experts(*(lb.Mx4(q.codes[None], q.scales[None], q.K) for q in (gu, dn)))
+    ref, tol = reference(x[5:6], *one, ex, torch.float32)
+    assert (np.abs(host(out[5:6]) - ref) <= tol).all() and not out[[0, 1, 2, 3, 4, 6, 7]].any()
