@@ -8,6 +8,7 @@
 #include "lx_vec.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace lx {
@@ -252,6 +253,13 @@ template <int BM_, int BN_>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, THR = BM * BN > 128 * 128 ? 512 : 256, NW = THR / 64;
   static constexpr int WR = BM == 256 ? 4 : 2, WC = NW / WR, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+  // A wavefront's blocks of 32 rows: first row of the first, rows from one to the next.
+  // Of a tile that is at most half full each SIMD has half the work: of four wavefronts
+  // each has one block less where their blocks alternate; of eight, two to a SIMD, one
+  // of the two has none where each one's blocks are neighbours (32768 rows in 128
+  // groups of 2048 x 768: 107 us in bf16, 256 x 256 161).
+  static constexpr bool SPREAD = THR == 256;
+  static constexpr int FIRST = SPREAD ? 32 : WM, NEXT_BLOCK = SPREAD ? 32 * WR : 32;
   static constexpr int RA = BM * 8 / THR, RB = BN * 8 / THR;  // a thread's 16-byte loads per step of A, of B
   static constexpr int SA = BM * 128, SB = BN * 128, STAGE = SA + SB, SGRP = (BM + BN) * 16;
   static constexpr int NEXT = 2 * STAGE + 2 * SGRP, LDS = NEXT + (RA + 1) * THR * 4, PER_CU = THR == 512 ? 1 : 2;
@@ -275,6 +283,7 @@ __global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_t
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int l32 = lane & 31, h = lane >> 5, wm = wave / WC, wn = wave % WC;
+  const int row0 = wm * T::FIRST;
   const int cp = a.Kp / 2, sp = a.Kp / 32, steps = a.Kp / 128;
 
   struct Item {
@@ -308,7 +317,7 @@ __global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_t
       q.oa[j] = (uint32_t)max(row_of(q, r), 0) * (uint32_t)a.Kp + ((tid ^ (r >> 1)) & 7) * 16;
     }
     q.qs = (uint32_t)max(row_of(q, tid % BM), 0) * (uint32_t)sp;
-    q.there = __ballot(lane < WM && row_of(q, wm * WM + lane) >= 0);
+    q.there = __ballot(lane < WM && row_of(q, row0 + (lane >> 5) * T::NEXT_BLOCK + l32) >= 0);
   };
   Item cur;
   const uint8_t *B, *Bs;  // the group's weights and their scales
@@ -376,8 +385,8 @@ __global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_t
 
   f32x16 acc[MI][NI];
   const int swz = (l32 >> 1) & 7;
-  const uint32_t la = (wm * WM + l32) * 128 + (h ^ swz) * 16, lb = SA + (wn * WN + l32) * 128 + (h ^ swz) * 16;
-  const uint8_t* const lsa = smem + 2 * STAGE + (wm * WM + l32) * 16;
+  const uint32_t la = (row0 + l32) * 128 + (h ^ swz) * 16, lb = SA + (wn * WN + l32) * 128 + (h ^ swz) * 16;
+  const uint8_t* const lsa = smem + 2 * STAGE + (row0 + l32) * 16;
   const uint8_t* const lsb = smem + 2 * STAGE + (BM + wn * WN + l32) * 16;
   // a row's scales of a step are one word: a lane's block of instruction s is 2 s +
   // h, so after a shift by h bytes its scale is byte 2 s
@@ -393,7 +402,7 @@ __global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_t
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) q.b[ni] = *(const uint32_t*)(lsb + st + ni * 512) >> (8 * h);
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) q.a[mi] = *(const uint32_t*)(lsa + st + mi * 512) >> (8 * h);
+    for (int mi = 0; mi < MI; ++mi) q.a[mi] = *(const uint32_t*)(lsa + st + mi * T::NEXT_BLOCK * 16) >> (8 * h);
     return q;
   };
   // fragments of instruction s (64 values) of step t: of the activations 16 values
@@ -410,7 +419,7 @@ __global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_t
 #pragma unroll
     for (int mi = 0; mi < decltype(blocks)::value; ++mi)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) f.a[mi][c] = *(const vu4*)(lds(la + (t & 1) * STAGE, 4 * s + 2 * c) + mi * 4096);
+      for (int c = 0; c < 2; ++c) f.a[mi][c] = *(const vu4*)(lds(la + (t & 1) * STAGE, 4 * s + 2 * c) + mi * T::NEXT_BLOCK * 128);
   };
   // step t's loads: A's, and the half (t - 1) % 2 of the weights' step that begins at t or
   // t + 1
@@ -468,7 +477,7 @@ __global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_t
     for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
-    const int live = min(max((cur.m1 - cur.m0 - wm * WM + 31) / 32, 0), MI);
+    const int live = min(max((cur.m1 - cur.m0 - row0 + T::NEXT_BLOCK - 1) / T::NEXT_BLOCK, 0), MI);
     // step t has landed, step t + 1 streams in under its products
     auto step = [&](int t, auto odd) __attribute__((always_inline)) {
       constexpr int ODD = decltype(odd)::value;
@@ -546,7 +555,7 @@ __global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_t
         asm volatile("" ::: "memory");  // (a wavefront's LDS accesses run in order)
 #pragma unroll 2
         for (int r0 = 0; r0 < 32; r0 += 64 / LPR) {
-          const int r = r0 + ln / LPR, m = m0 + wm * WM + mi * 32 + r, c = c0 + cc * CW + ln % LPR * 8;
+          const int r = r0 + ln / LPR, m = m0 + row0 + mi * T::NEXT_BLOCK + r, c = c0 + cc * CW + ln % LPR * 8;
           const vf4 u = *(const vf4*)(e + chunk(r, ln % LPR * 2)), v = *(const vf4*)(e + chunk(r, ln % LPR * 2 + 1));
           const F8 x{{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]}};
           if (mx8)
@@ -598,45 +607,47 @@ hipError_t launch(const Mx8GemmArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Which kernel: the one with the least time by a model of rounds. A round is what
-// the compute units take at once, in us per 4096 values of K (measured alone on full
-// rounds, `half` where each compute unit has one workgroup at most, for results in
-// bf16 and for those of two instructions):
-//                         half          full            workgroups in a round
-//   16 x 32 (rows4)       7             7               256
-//   64 x 128              20, 25        22, 31          256, 512
-//   128 x 128             25, 40        37, 58          256, 512
-//   256 x 256             64, 107       64, 107         256
-// and 1 us per round besides, 6 with groups, whose tiles begin with two dependent
-// lookups. Rows of a group are not known here, only their mean: its last tile is taken
-// to be half full. Model and kernels: 100 x 4096 x 4096 rows4 28, 64 x 128 21, 128 x 128 24
-// us; 512 x 14336 x 4096 47, 34 (128 x 128), 51 (256 x 256); 2000 x 8192 x 4096 85, 69,
-// 62; 8192^3 825, 532, 432. Groups of at most 5 rows in the mean run on the row
-// kernel (64 tokens' slots on 128 experts of 1536 x 2048 with SwiGLU: 42 us, 64 x 128
-// 50; of 128 tokens 56 and 55).
-Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool exact) {
+// Which kernel: the one with the least time by a model of rounds. A round is what the
+// compute units take at once, in us per 4096 values of K (`half` where there are so few
+// tiles that they share nothing) and besides, for filling and writing out; for results
+// in bf16, and for those of two instructions:
+//                  half      full      besides        tiles at once
+//   16 x 32        5.5       5.5       1.3            256          (rows4)
+//   16 x 64        16        27        3              512, 1024    (rows; with SwiGLU 16 x 128, 18, 45)
+//   64 x 128       17, 21    19, 27    3.5, 4.5       256, 512
+//   128 x 128      19, 33    30, 51    6, 7           256, 512
+//   256 x 256      47, 75    47, 75    22, 28         256          (with SwiGLU 12 besides)
+// Of groups' rows only the mean is known: their last tiles are taken to be half full. Of
+// those the wider tiles leave out what lies past them (`last`: the rows that they cost), up
+// to where they wait for the weights, at 0.8 of a full tile. Over 250 drawn sizes (17 .. 16384 rows,
+// 256 .. 14336 columns, K of 64 .. 14336, 1 .. 128 groups) the choice takes 1.5% longer
+// than the best of the five, 38% at worst. us of rows4, rows, 64, 128, 256:
+//   512 x 1536 x 2048, 128 groups, SwiGLU to 8 bits     74  44  50  56  83
+//   2048 x 1536 x 2048, 128 groups, the same           118  70  50  56  84
+//   32768 x 2048 x 768, 128 groups, fp32              1088   -  196 167 202
+//   3001 x 4096 x 14336, bf16                         1853   -  206 180 190
+//   8192 x 8192 x 8192, bf16                             -   -  825 532 432
+Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool exact, bool swiglu) {
   Mx8GemmPlan p{};
-  const int64_t groups = std::min(M, G);
-  if (G > 1 && M <= 5 * groups) {
-    p.kernel = Mx8GemmPlan::kRows;
-    return p;
-  }
+  const int64_t groups = G > 1 ? std::min(M, G) : 1;
   p.kernel = Mx8GemmPlan::kTile64;
   double best = 0;
-  auto offer = [&](Mx8GemmPlan::Kernel k, int64_t bm, int64_t bn, int at_once, double half, double full) {
-    const int64_t rows = G > 1 ? (M + groups * (bm / 2)) / bm : (M + bm - 1) / bm;
+  auto offer = [&](Mx8GemmPlan::Kernel k, int64_t bm, int64_t bn, double last, int at_once, int few, double half, double full, double besides) {
+    const double m = M, in_parts = G > 1 ? m + groups * (bm / 2) : m;  // rows with the last tiles full
+    const int64_t rows = std::max((int64_t)std::ceil(in_parts / bm), groups);
     const int64_t tiles = rows * (((int64_t)N + bn - 1) / bn), whole = tiles / at_once, rest = tiles % at_once;
-    const double k4 = Kp / 4096., besides = G > 1 ? 6 : 1;
-    const double us = whole * (full * k4 + besides) + (rest == 0 ? 0 : (rest <= 256 ? half : full) * k4 + besides);
+    const double k4 = Kp / 4096., share = G > 1 ? std::max((m + groups * last) / in_parts, 0.8) : 1;
+    const double us = share * (whole * (full * k4 + besides) + (rest == 0 ? 0 : (rest <= few ? half : full) * k4 + besides));
     if (best == 0 || us < best) {
       best = us;
       p.kernel = k;
     }
   };
-  offer(Mx8GemmPlan::kTile64, 64, 128, 512, exact ? 25 : 20, exact ? 31 : 22);
-  offer(Mx8GemmPlan::kTile128, 128, 128, 512, exact ? 40 : 25, exact ? 58 : 37);
-  offer(Mx8GemmPlan::kTile256, 256, 256, 256, exact ? 107 : 64, exact ? 107 : 64);
-  offer(Mx8GemmPlan::kRows4, 16, 32, 256, 7, 7);
+  offer(Mx8GemmPlan::kTile64, 64, 128, 32, 512, 256, exact ? 21 : 17, exact ? 27 : 19, exact ? 4.5 : 3.5);
+  offer(Mx8GemmPlan::kTile128, 128, 128, 32, 512, 256, exact ? 33 : 19, exact ? 51 : 30, exact ? 7 : 6);
+  offer(Mx8GemmPlan::kTile256, 256, 256, 64, 256, 256, exact ? 75 : 47, exact ? 75 : 47, swiglu ? 12 : exact ? 28 : 22);
+  offer(Mx8GemmPlan::kRows4, 16, 32, 8, 256, 256, 5.5, 5.5, 1.3);
+  if (G > 1) offer(Mx8GemmPlan::kRows, 16, swiglu ? 128 : 64, 8, 1024, 512, swiglu ? 18 : 16, swiglu ? 45 : 27, 3);
   return p;
 }
 
