@@ -331,7 +331,7 @@ __device__ __forceinline__ float load_dev(const float* p) {
 constexpr int kDownWaves = 16;
 template <int TERMS>
 __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a) {
-  constexpr int U = kBatch;
+  constexpr int U = kBatch, PACKED = 16 / TERMS;
   __shared__ __attribute__((aligned(16))) uint8_t stage[kDownWaves][kStage];
   // [kDownWaves][T][16] sums, then three words for each unit with tokens
   extern __shared__ __attribute__((aligned(16))) float sums[];
@@ -363,16 +363,23 @@ __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a
   const int last = min(a.d - 1 - n0, 15);
   int token = 0, count = 0, base = 0, expert = 0, unit = -1;
   vf4 acc = {0.f, 0.f, 0.f, 0.f};
-  // acc into the sums of the tokens from c0 on
-  auto flush = [&](int c0) __attribute__((always_inline)) {
+  // acc into the sums of tokens c0 .. to - 1
+  auto flush = [&](int c0, int to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {  // the terms' sums, the least first
+      float s = 0.f;
+#pragma unroll
+      for (int m = TERMS - 1; m > 0; --m) s += __uint_as_float(__builtin_amdgcn_ds_bpermute((lane + m * PACKED) * 4, (int)__float_as_uint(acc[r])));
+      acc[r] += s;
+    }
     const int t = __builtin_amdgcn_ds_bpermute(min(c0 + l16, count - 1) * 4, token);
-    if (c0 + l16 < count) *(vf4*)(mine + t * 16 + q * 4) += acc;
+    if (c0 + l16 < to) *(vf4*)(mine + t * 16 + q * 4) += acc;
     acc = vf4{0.f, 0.f, 0.f, 0.f};
   };
   for (int b = split * kDownWaves + wave; b < all; b += a.splits * kDownWaves) {
     const int i = b / batches, k = (b - i * batches) * U, n = min(steps - k, U);
     if (i != unit) {
-      if (unit >= 0 && count <= 16) flush(0);
+      if (unit >= 0 && count <= PACKED) flush(0, count);
       unit = i;
       const int m = __builtin_amdgcn_readfirstlane(list[3 * i]);
       expert = m & 0xFFFF;
@@ -386,44 +393,33 @@ __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a
     all_read();  // (the batch before)
     ask_codes(a.down, row, last, steps, k, n, stage[wave]);
     const Scales sc = ask_scales(a.down_s + (row + min(l16, last)) * sp, steps, k, n, lane < 16);
-    for (int c0 = 0; c0 < count; c0 += 16) {
-      const int cols = min(count - c0, 16);
-      const uint8_t* const h = (const uint8_t*)hidden_of(a, base, c0);
-      const uint32_t own = (uint32_t)(q * cols + l16) * 16;  // (the rest of an address is uniform)
-      // activations step by step, with two terms the next step's on their way (all of them
-      // at once would leave room for half as many wavefronts)
-      constexpr int HELD = TERMS == 2 ? 2 : 1;
-      vu4 x[HELD][4][TERMS];
-      auto acts = [&](int i) __attribute__((always_inline)) {
+    for (int c0 = 0, to; c0 < count; c0 = to) {
+      const int g = c0 & ~15, cols = min(count - g, 16);
+      to = min(min(c0 + PACKED, g + 16), count);
+      const uint8_t* const h = (const uint8_t*)hidden_of(a, base, g) + hidden_at(fp, 0, k, 0, 0, cols, c0 - g) * 2;
+      int l = lane;
+      asm volatile("" : "+v"(l));  // (what follows from it is not kept over the batches)
+      // (columns without a token, and steps past the last, repeat some that are there)
+      const int m = min((l & 15) / PACKED, TERMS - 1), col = min((l & 15) % PACKED, to - c0 - 1);
+      const uint32_t own = ((uint32_t)(m * (fp / 8) + (l >> 4)) * cols + col) * 16;
+      vu4 x[U][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+      for (int i = 0; i < U; ++i)
 #pragma unroll
-          for (int m = 0; m < TERMS; ++m) {
-            x[i % HELD][j][m] = vu4{0, 0, 0, 0};
-            if (l16 < cols)
-              x[i % HELD][j][m] = *(const vu4*)(h + hidden_at(fp, m, k + i, j, 0, cols, 0) * 2 + own);
-          }
-      };
-      acts(0);
+        for (int j = 0; j < 4; ++j) x[i][j] = *(const vu4*)(h + (own + (uint32_t)((min(i, n - 1) * 4 + j) * 64 * cols)));
       all_landed();  // (for the first tokens; it also keeps the codes from being read ahead of the loop)
 #pragma unroll
       for (int i = 0; i < U; ++i)
         if (i < n) {
-          if (HELD == 2 && i + 1 < n) acts(i + 1);
-          if (HELD == 1 && i > 0) acts(i);
           const float f = scale_of(sc, steps, k, i, l16);
           const vu4 w = codes_of(stage[wave], i);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const bf8 v = read8(w[j], f);
-#pragma unroll
-            for (int m = TERMS - 1; m >= 0; --m) acc = mfma(v, x[i % HELD][j][m], acc);
-          }
+          for (int j = 0; j < 4; ++j) acc = mfma(read8(w[j], f), x[i][j], acc);
         }
-      if (count > 16) flush(c0);
+      if (count > PACKED) flush(c0, to);
     }
   }
-  if (unit >= 0 && count <= 16) flush(0);
+  if (unit >= 0 && count <= PACKED) flush(0, count);
   __syncthreads();
   auto put = [&](int i, float s) __attribute__((always_inline)) {
     const int n = n0 + (i & 15);
