@@ -72,11 +72,25 @@ struct Acts {
       static_assert(N == 3, "");
       const vu4* const p = (const vu4*)((const uint8_t*)x + (row + (uint32_t)c * 4));
       const vu4 a = p[0], b = p[1];
+      // terms() of 8 values, whose infinities and NaN, if there are any, are put right
+      // afterwards: they leave a NaN in the sum of the rests
+      float all = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const Terms u = terms(__uint_as_float(j < 2 ? a[2 * j] : b[2 * j - 4])), v = terms(__uint_as_float(j < 2 ? a[2 * j + 1] : b[2 * j - 3]));
+        const uint32_t u = j < 2 ? a[2 * j] : b[2 * j - 4], v = j < 2 ? a[2 * j + 1] : b[2 * j - 3];
+        const float ru = __uint_as_float(u) - __uint_as_float(u & 0xFFFF0000u), rv = __uint_as_float(v) - __uint_as_float(v & 0xFFFF0000u);
+        all += ru + rv;
+        t[0][j] = two(u, v);
+        t[1][j] = pack_bf16(ru, rv);
+        t[2][j] = two(__float_as_uint(ru - __uint_as_float(t[1][j] << 16)), __float_as_uint(rv - __uint_as_float(t[1][j] & 0xFFFF0000u)));
+      }
+      if (!(all == all)) {
 #pragma unroll
-        for (int n = 0; n < 3; ++n) t[n][j] = two(u.t[n], v.t[n]);
+        for (int j = 0; j < 4; ++j) {
+          const Terms u = terms(__uint_as_float(j < 2 ? a[2 * j] : b[2 * j - 4])), v = terms(__uint_as_float(j < 2 ? a[2 * j + 1] : b[2 * j - 3]));
+#pragma unroll
+          for (int n = 0; n < 3; ++n) t[n][j] = two(u.t[n], v.t[n]);
+        }
       }
     } else {
       t[0] = *(const vu4*)((const uint8_t*)x + (row + (uint32_t)c * 2));
