@@ -59,25 +59,30 @@ __device__ __forceinline__ Terms terms(float x) {
 }
 __device__ __forceinline__ uint32_t two(uint32_t lo, uint32_t hi) { return lo >> 16 | (hi & 0xFFFF0000u); }
 
-// 8 activations from column c of the row that begins at byte `row` of x (T d is at most
-// 2^26; not `there`: zeros) as N terms.
-template <int N, bool F32>
+// 8 activations: as they are loaded, from column c of the row that begins at byte `row` of
+// x (T d is at most 2^26; not `there`: zeros), and as terms.
+template <bool F32>
 struct Acts {
-  vu4 t[N];
+  static constexpr int N = F32 ? 3 : 1, R = F32 ? 2 : 1;
+  vu4 r[R];
   __device__ __forceinline__ void load(const void* x, uint32_t row, bool there, int c, int K) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) t[n] = vu4{0, 0, 0, 0};
+    for (int i = 0; i < R; ++i) r[i] = vu4{0, 0, 0, 0};
     if (!there || c >= K) return;
-    if constexpr (F32) {
-      static_assert(N == 3, "");
-      const vu4* const p = (const vu4*)((const uint8_t*)x + (row + (uint32_t)c * 4));
-      const vu4 a = p[0], b = p[1];
-      // terms() of 8 values, whose infinities and NaN, if there are any, are put right
-      // afterwards: they leave a NaN in the sum of the rests
+    const vu4* const p = (const vu4*)((const uint8_t*)x + (row + (uint32_t)c * (F32 ? 4 : 2)));
+#pragma unroll
+    for (int i = 0; i < R; ++i) r[i] = p[i];
+  }
+  // terms() of 8 values, whose infinities and NaN, if there are any, are put right
+  // afterwards: they leave a NaN in the sum of the rests
+  __device__ __forceinline__ void split(vu4 (&t)[N]) const {
+    if constexpr (!F32) {
+      t[0] = r[0];
+    } else {
       float all = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t u = j < 2 ? a[2 * j] : b[2 * j - 4], v = j < 2 ? a[2 * j + 1] : b[2 * j - 3];
+        const uint32_t u = r[j / 2][j % 2 * 2], v = r[j / 2][j % 2 * 2 + 1];
         const float ru = __uint_as_float(u) - __uint_as_float(u & 0xFFFF0000u), rv = __uint_as_float(v) - __uint_as_float(v & 0xFFFF0000u);
         all += ru + rv;
         t[0][j] = two(u, v);
@@ -87,13 +92,11 @@ struct Acts {
       if (!(all == all)) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const Terms u = terms(__uint_as_float(j < 2 ? a[2 * j] : b[2 * j - 4])), v = terms(__uint_as_float(j < 2 ? a[2 * j + 1] : b[2 * j - 3]));
+          const Terms u = terms(__uint_as_float(r[j / 2][j % 2 * 2])), v = terms(__uint_as_float(r[j / 2][j % 2 * 2 + 1]));
 #pragma unroll
           for (int n = 0; n < 3; ++n) t[n][j] = two(u.t[n], v.t[n]);
         }
       }
-    } else {
-      t[0] = *(const vu4*)((const uint8_t*)x + (row + (uint32_t)c * 2));
     }
   }
 };
@@ -267,32 +270,34 @@ __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
       ask_codes(a.gu, row, last, steps, k, n, sg);
       ask_codes(a.gu, row + a.f, last, steps, k, n, su);
       const Scales sc = ask_scales(my_scales, steps, k, n, lane < 32);
-      // activations: of all steps (bf16), or step by step (fp32, whose terms take more)
-      constexpr int HELD = F32 ? 1 : kBatch;
-      Acts<N, F32> v[HELD][4];
-      auto acts = [&](int i) __attribute__((always_inline)) {
+      // activations: of all steps (bf16), or half a step's at a time, the next half's on
+      // their way (fp32)
+      Acts<F32> v[F32 ? 2 : kBatch][F32 ? 2 : 4];
+      auto acts = [&](int i, int j0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[i % HELD][j].load(a.x, x, there, (k + i) * 128 + q * 32 + j * 8, a.d);
+        for (int j = j0; j < (F32 ? j0 + 2 : 4); ++j)
+          v[F32 ? j0 / 2 : i][F32 ? j % 2 : j].load(a.x, x, there, (k + i) * 128 + q * 32 + j * 8, a.d);
       };
-      if constexpr (HELD > 1) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-          if (i < n) acts(i);
-      }
+      for (int i = 0; i < (F32 ? 1 : kBatch); ++i)
+        if (i < n) acts(i, 0);
       all_landed();
 #pragma unroll
       for (int i = 0; i < kBatch; ++i)
         if (i < n) {
-          if constexpr (HELD == 1) acts(i);
           const float fg = scale_of(sc, steps, k, i, l16), fu = scale_of(sc, steps, k, i, 16 + l16);
           const vu4 wg = codes_of(sg, i), wu = codes_of(su, i);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
+            if (F32 && j == 0) acts(i, 2);
+            if (F32 && j == 2 && i + 1 < n) acts(i + 1, 0);
             const bf8 g = read8(wg[j], fg), z = read8(wu[j], fu);
+            vu4 t[N];
+            v[F32 ? j / 2 : i][F32 ? j % 2 : j].split(t);
 #pragma unroll
             for (int m = N - 1; m >= 0; --m) {
-              ag = mfma(g, v[i % HELD][j].t[m], ag);
-              au = mfma(z, v[i % HELD][j].t[m], au);
+              ag = mfma(g, t[m], ag);
+              au = mfma(z, t[m], au);
             }
           }
         }
