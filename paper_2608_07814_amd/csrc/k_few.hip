@@ -218,10 +218,12 @@ __device__ __forceinline__ int64_t hidden_at(int fp, int term, int step, int j, 
 // expert where there are no more of them than slots, else a slot, of which each expert's
 // first does the work. Many short workgroups hide each other's waits: several tiles to
 // a workgroup in turn, the next one's weights on their way, took a third longer. The
-// results go to a.hidden as bf16 terms. 61 tokens on 128 experts of 768 x 2048: 52 us,
-// the weights at 4.1 TB/s; 5 tokens on experts of 14336 x 4096: 103 us, 4.0. Tried and
-// no faster: a tile of its own for each wavefront where rows are short, x through LDS
-// (64 tokens on 8 experts 182 for 205, most others a little slower).
+// results go to a.hidden as bf16 terms. Experts of 14336 x 4096, 5 tokens on 6 or 7 of
+// them: 97 us, the weights at 4.2 TB/s; of 768 x 2048, 61 tokens on 90 of 128: 48 us, 3.1
+// (a workgroup reads 50 KB, behind two dependent loads of ids and codes). fp32 activations
+// take 20 to 40% longer, for the instructions that split them. Tried and no faster: a
+// tile of its own for each wavefront where rows are short, x through LDS (64 tokens on 8
+// experts 182 for 205, most others a little slower).
 template <bool F32>
 __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
   constexpr int N = F32 ? 3 : 1;
@@ -344,9 +346,15 @@ __device__ __forceinline__ float load_dev(const float* p) {
 // the workgroup that is done last, over the workgroups. What workgroups hand each other is
 // stored and loaded coherently and complete before the counter is raised, which is all
 // the order that it needs (fences, which write back and empty whole caches, took the
-// launch from 93 to 205 us). TERMS of the hidden
-// activations are multiplied: for a bf16 output two (2^-16 of a value at most, next to
-// the 2^-9 that the output is rounded by), for fp32 all three.
+// launch from 93 to 205 us).
+// TERMS of the hidden activations are multiplied: for a bf16 output two (2^-16 of a value
+// at most, next to the 2^-9 that the output is rounded by), for fp32 all three. They are
+// columns of one instruction side by side, PACKED tokens at a time, so that a batch's
+// activations fit in registers and are asked for together with its codes: there is one
+// wait to a batch (term by term, a step ahead: 87 for 66 us, 5 tokens on experts of 14336
+// x 4096; 42 for 36, 61 tokens on 90 experts of 768 x 2048; 11.2 for 8.3, one token on 8
+// of these). Weights at 3.1 and 2.0 TB/s. A workgroup to an expert and 16 to 64 columns,
+// its products joined by the last one or by a third launch, took 30% or 0 to 20% longer.
 constexpr int kDownWaves = 16;
 template <int TERMS>
 __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a) {
