@@ -101,6 +101,16 @@ struct Acts {
   }
 };
 
+// Lane l of each 16 gets what lane l + R of them has.
+template <int R>
+__device__ __forceinline__ vu4 from_right(const vu4& x) {
+  if constexpr (R == 0) return x;
+  vu4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x[i], 0x120 + (16 - R) % 16, 0xF, 0xF, false);
+  return r;
+}
+
 __device__ __forceinline__ vf4 mfma(bf8 w, const vu4& a, vf4 acc) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf8, a), acc, 0, 0, 0);
 }
@@ -220,10 +230,12 @@ __device__ __forceinline__ int64_t hidden_at(int fp, int term, int step, int j, 
 // a workgroup in turn, the next one's weights on their way, took a third longer. The
 // results go to a.hidden as bf16 terms. Experts of 14336 x 4096, 5 tokens on 6 or 7 of
 // them: 97 us, the weights at 4.2 TB/s; of 768 x 2048, 61 tokens on 90 of 128: 48 us, 3.1
-// (a workgroup reads 50 KB, behind two dependent loads of ids and codes). fp32 activations
-// take 20 to 40% longer, for the instructions that split them. Tried and no faster: a
-// tile of its own for each wavefront where rows are short, x through LDS (64 tokens on 8
-// experts 182 for 205, most others a little slower).
+// (the first-level cache is asked for something in every cycle: by 16 loads of activations
+// a batch, most of whose lanes have no token, next to 8 of codes). Both launches with fp32
+// activations take 20 to 35% longer, for the instructions that split them. Tried and no
+// faster: a tile of its own for each wavefront where rows are short; x through LDS (64
+// tokens on 8 experts 182 for 205, most others a little slower); four sets of 16 tokens
+// on the same codes (64 tokens on 8 experts 338 for 349, 61 on 128 89 for 85).
 template <bool F32>
 __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
   constexpr int N = F32 ? 3 : 1;
@@ -262,9 +274,7 @@ __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
   const uint8_t* const my_scales = a.gu_s + (row + (lane & 16 ? a.f : 0) + min(l16, last)) * sp;
   uint8_t *const sg = stage[wave][0], *const su = stage[wave][1];
   for (int c0 = 0; c0 < count; c0 += 16) {
-    const int t = __builtin_amdgcn_ds_bpermute(min(c0 + l16, count - 1) * 4, token);
-    const uint32_t x = (uint32_t)t * (uint32_t)a.d * (F32 ? 4 : 2);
-    const bool there = c0 + l16 < count;
+    const int cols = min(count - c0, 16);
     vf4 ag = {0.f, 0.f, 0.f, 0.f}, au = ag;
     for (int k = k0; k < k1 && !padding; k += kBatch) {
       const int n = min(k1 - k, kBatch);
@@ -272,37 +282,73 @@ __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
       ask_codes(a.gu, row, last, steps, k, n, sg);
       ask_codes(a.gu, row + a.f, last, steps, k, n, su);
       const Scales sc = ask_scales(my_scales, steps, k, n, lane < 32);
-      // activations: of all steps (bf16), or half a step's at a time, the next half's on
-      // their way (fp32)
-      Acts<F32> v[F32 ? 2 : kBatch][F32 ? 2 : 4];
-      auto acts = [&](int i, int j0) __attribute__((always_inline)) {
+      // At most G tokens: the lanes of the columns that they leave load, and split into
+      // terms, what the following 16 / G - 1 instructions take. (fp32: 5 tokens on experts
+      // of 14336 x 4096 181 us for 212, both launches; in bf16, with nothing to split, 100 for
+      // 97 in this one.)
+      auto products = [&](auto most) __attribute__((always_inline)) {
+        constexpr int G = decltype(most)::value, PER = 16 / G, L = 4 / PER;
+        int l16 = lane & 15;
+        if (F32) asm volatile("" : "+v"(l16));  // (what follows from it is not kept over the batches)
+        const int t = __builtin_amdgcn_ds_bpermute(min(c0 + l16 % G, count - 1) * 4, token);
+        const uint32_t x = (uint32_t)t * (uint32_t)a.d * (F32 ? 4 : 2);
+        const bool there = l16 % G < cols;
+        // activations: of all steps (bf16), or two loads at a time, the next two on their
+        // way (fp32)
+        constexpr int C = F32 ? 2 : 4 * L, CHUNKS = 4 * L / C;
+        Acts<F32> v[F32 ? 2 : 1][C];
+        auto ask = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = j0; j < (F32 ? j0 + 2 : 4); ++j)
-          v[F32 ? j0 / 2 : i][F32 ? j % 2 : j].load(a.x, x, there, (k + i) * 128 + q * 32 + j * 8, a.d);
-      };
+          for (int s = 0; s < C; ++s) {
+            const int i = (c * C + s) / L, l = (c * C + s) % L;
+            if (i < n) v[c % 2][s].load(a.x, x, there, (k + i) * 128 + q * 32 + (l * PER + l16 / G) * 8, a.d);
+          }
+        };
+        ask(0);
+        all_landed();
+        float fg = 0.f, fu = 0.f;
+        vu4 wg = {0, 0, 0, 0}, wu = wg;
 #pragma unroll
-      for (int i = 0; i < (F32 ? 1 : kBatch); ++i)
-        if (i < n) acts(i, 0);
-      all_landed();
+        for (int c = 0; c < CHUNKS; ++c) {
+          if (c + 1 < CHUNKS) ask(c + 1);
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-        if (i < n) {
-          const float fg = scale_of(sc, steps, k, i, l16), fu = scale_of(sc, steps, k, i, 16 + l16);
-          const vu4 wg = codes_of(sg, i), wu = codes_of(su, i);
+          for (int s = 0; s < C; ++s) {
+            const int i = (c * C + s) / L, l = (c * C + s) % L;
+            if (i < n) {
+              if (l == 0) {
+                fg = scale_of(sc, steps, k, i, l16);
+                fu = scale_of(sc, steps, k, i, 16 + l16);
+                wg = codes_of(sg, i);
+                wu = codes_of(su, i);
+              }
+              vu4 t[N];
+              v[c % 2][s].split(t);
+              auto one = [&](auto jj) __attribute__((always_inline)) {
+                constexpr int J = decltype(jj)::value;
+                if constexpr (J < PER) {
+                  const bf8 g = read8(wg[l * PER + J], fg), z = read8(wu[l * PER + J], fu);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (F32 && j == 0) acts(i, 2);
-            if (F32 && j == 2 && i + 1 < n) acts(i + 1, 0);
-            const bf8 g = read8(wg[j], fg), z = read8(wu[j], fu);
-            vu4 t[N];
-            v[F32 ? j / 2 : i][F32 ? j % 2 : j].split(t);
-#pragma unroll
-            for (int m = N - 1; m >= 0; --m) {
-              ag = mfma(g, t[m], ag);
-              au = mfma(z, t[m], au);
+                  for (int m = N - 1; m >= 0; --m) {
+                    const vu4 u = from_right<J * G>(t[m]);
+                    ag = mfma(g, u, ag);
+                    au = mfma(z, u, au);
+                  }
+                }
+              };
+              one(std::integral_constant<int, 0>{});
+              one(std::integral_constant<int, 1>{});
+              one(std::integral_constant<int, 2>{});
+              one(std::integral_constant<int, 3>{});
             }
           }
         }
+      };
+      if (F32 && cols <= 4)
+        products(std::integral_constant<int, 4>{});
+      else if (F32 && cols <= 8)
+        products(std::integral_constant<int, 8>{});
+      else
+        products(std::integral_constant<int, 16>{});
     }
     all_read();
     // (the sums meet where the codes were)
@@ -312,7 +358,7 @@ __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
     __syncthreads();
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // (what follows from it is not kept over the products)
-    const int cols = min(count - c0, 16), e8 = tid & 7, col = tid / 8 % 16, n = tid / 128 * 8 + e8;
+    const int e8 = tid & 7, col = tid / 8 % 16, n = tid / 128 * 8 + e8;
     if (col < cols) {
       float g = 0.f, z = 0.f;
 #pragma unroll
