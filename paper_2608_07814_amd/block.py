@@ -268,9 +268,12 @@ def _block_norm(h, y, w_pre, w_post, scale, gate, slot_row, slot_weights, residu
         Kp = mx4_padded(d)
         if x is None:
             x = Mx8(h.new_empty((T, Kp), dtype=torch.uint8), h.new_empty((T, Kp // 32), dtype=torch.uint8), d)
+            xp = _arg("x_values", x_values, shape, None, gpu), _ptr(x.codes), _ptr(x.scales)
         elif x.K != d:
             raise ValueError("x.K does not fit h")
-        xp = _arg("x_values", x_values, shape, None, gpu), _arg("x codes", x.codes, (T, Kp), torch.uint8, gpu), _arg("x scales", x.scales, (T, Kp // 32), torch.uint8, gpu)
+        else:
+            xp = (_arg("x_values", x_values, shape, None, gpu), _arg("x codes", x.codes, (T, Kp), torch.uint8, gpu),
+                  _arg("x scales", x.scales, (T, Kp // 32), torch.uint8, gpu))
     else:
         xp = (_arg("x", x, shape, None, gpu),)
     if dropout is not None:
@@ -611,11 +614,13 @@ def mx8_quantize(x: torch.Tensor, *, act: int = MX4_NONE, out: Optional[Mx8] = N
     Kp = mx4_padded(K)
     cs, ss = (*lead, Kp), (*lead, Kp // 32)
     if out is None:
-        out = Mx8(x.new_empty(cs, dtype=torch.uint8), x.new_empty(ss, dtype=torch.uint8), K)
+        codes, scales = x.new_empty(cs, dtype=torch.uint8), x.new_empty(ss, dtype=torch.uint8)
+        out, cp, sp = Mx8(codes, scales, K), codes.data_ptr() or _EMPTY, scales.data_ptr() or _EMPTY
     elif out.K != K:
         raise ValueError("out.K does not fit x")
-    st = lib().lx_mx8_quantize(x.data_ptr(), _dtype("x", x), lead.numel(), K, act, _arg("codes", out.codes, cs, torch.uint8, gpu),
-                               _arg("scales", out.scales, ss, torch.uint8, gpu), _current_raw_stream(gpu))
+    else:
+        cp, sp = _arg("codes", out.codes, cs, torch.uint8, gpu), _arg("scales", out.scales, ss, torch.uint8, gpu)
+    st = lib().lx_mx8_quantize(x.data_ptr(), _dtype("x", x), lead.numel(), K, act, cp, sp, _current_raw_stream(gpu))
     if st:
         _check(st)
     return out
@@ -682,9 +687,9 @@ def mx8_gemm(a: Mx8, b: Mx4, *, offsets: Optional[torch.Tensor] = None, row_map:
         bias = bias.view(1, -1)
     e = LxEpilogue(act, 0 if bias is None else _dtype("bias", bias), 0 if residual is None else _dtype("residual", residual),
                    _arg("bias", bias, (G, N), None, gpu), _arg("residual", residual, (M, cols), None, gpu))
-    L = lib()
-    keep, ws, n = _workspace(workspace, L.lx_mx8_gemm_workspace_bytes(M, N, K, G, act), ac)
-    st = L.lx_mx8_gemm(_arg("a codes", ac, (rows, Kp), torch.uint8, gpu),
+    # (lx_mx8_gemm_workspace_bytes is 0 for all sizes: the question takes half a microsecond)
+    keep, ws, n = (None, None, 0) if workspace is None else _workspace(workspace, 0, ac)
+    st = lib().lx_mx8_gemm(_arg("a codes", ac, (rows, Kp), torch.uint8, gpu),
                        _arg("a scales", a.scales, (rows, Kp // 32), torch.uint8, gpu), rows,
                        _arg("row_map", row_map, (M,), torch.int32, gpu),
                        _arg("b codes", bc, (*lead, Kp // 2), torch.uint8, gpu),
