@@ -263,11 +263,8 @@ lx_status lx_mx8_dequantize(const void* codes, const void* scales, int64_t rows,
  * K a multiple of 8, at most 2^24, M and N at most 2^31 - 256, M * N < 2^40, G in 1 ..
  * LX_MAX_NODES. A, B and out 16-byte, scales, row_map and offsets 4-byte aligned;
  * workspace 256-byte aligned, lx_mx8_gemm_workspace_bytes bytes (NULL where that is
- * 0). The order in which a sum is formed depends on the sizes, G, act and the
- * result's type, not on the values. Products are exact in fp32 where the result is in fp32 or 8
- * bits; for bf16, of 16 products that are added at a time, what lies more than 13 bits
- * below the exponents of the largest may be left out (1e-5 of a sum of normal
- * values, next to the result's 2^-9). */
+ * 0). Products are exact in fp32, whatever the result's type. The order in which a sum
+ * is formed depends on the sizes, G and act, not on the values or the result's type. */
 typedef enum lx_act { LX_ACT_NONE = 0, LX_ACT_SILU = 1, LX_ACT_GELU = 2, LX_ACT_SWIGLU = 3 } lx_act;
 typedef struct lx_epilogue {
   lx_act act;

@@ -25,8 +25,9 @@ __device__ __forceinline__ v8i frag8(const vu4& p, const vu4& q) {
 
 // The instruction adds up 16 products at a time and drops what lies more than 13 bits
 // below the largest product's exponents: e4m3 reaches over 18 binades, and a few of
-// its bits are lost then (the sums of normal values are off by 1e-5 of their size;
-// with both operands e2m1 nothing is). Activations whose exponent field's top bit is
+// its bits are lost then (the sums of normal values are off by 1e-5 of their size, and
+// what is left of large products that cancel by all of it; with both operands e2m1
+// nothing is). Activations whose exponent field's top bit is
 // set (from 2 on under the block's scale) and the others are within the window among
 // themselves, so two instructions, one for each, drop nothing.
 template <bool HI>
@@ -251,10 +252,12 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // Workgroups stay for several tiles: the next one's place and rows are looked up under
 // the first loads of the present one, and its first loads are under way while the
 // present one's results are written.
-// Bound by the matrix units, on long runs by what they draw: 8192 x 8192 x 8192 takes 432 us
-// to bf16, 2.5 PFLOP/s of the 3.04 that the instruction reaches from registers on random
-// operands, and 680 to fp32, where every product is two instructions (3.2). Tried and no
-// faster: fragments read a step ahead between fences (463 for 420).
+// Bound by the matrix units, on long runs by what they draw: 8192 x 8192 x 8192 takes 725
+// us, 3.0 PFLOP/s of instructions (two to a product) of the 3.04 that one instruction after
+// the other reaches from registers on random operands. Tried and no
+// faster: fragments read a step ahead between fences (463 for 420, with one instruction to a
+// product, which took 432 for 8192 x 8192 x 8192 and 200 for 291 at 3001 x 4096 x 14336: what
+// it drops is more than a bf16 result is rounded by where products cancel).
 template <int BM_, int BN_>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, THR = BM * BN > 128 * 128 ? 512 : 256, NW = THR / 64;
@@ -274,7 +277,7 @@ struct Tile {
   static_assert(BM + BN <= THR && RB % 2 == 0 && NI % 2 == 0, "one row of scales per thread; halves");
 };
 
-template <class T, bool GLU, bool EXACT>
+template <class T, bool GLU>
 __global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_tile(const Mx8GemmArgs a) {
   constexpr int BM = T::BM, BN = T::BN, THR = T::THR, NW = T::NW, WC = T::WC, WM = T::WM, WN = T::WN, MI = T::MI, NI = T::NI;
   constexpr int RA = T::RA, RB = T::RB, SA = T::SA, STAGE = T::STAGE, SGRP = T::SGRP;
@@ -450,12 +453,8 @@ __global__ __launch_bounds__(T::THR, T::PER_CU * T::THR / 256) void k_mx8_gemm_t
           acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag4(f.b[ni]), v, acc[mi][ni], 4, 0, 2 * S, q.b[ni],
                                                                         2 * S, q.a[mi]);
       };
-      if constexpr (EXACT) {
-        row(half_of<false>(x));
-        row(half_of<true>(x));
-      } else {
-        row(x);
-      }
+      row(half_of<false>(x));
+      row(half_of<true>(x));
     }
   };
   using std::integral_constant;
@@ -591,11 +590,7 @@ hipError_t launch_tile(const Mx8GemmArgs& a, hipStream_t s) {
   const int64_t tiles = a.offsets ? std::min<int64_t>((int64_t)a.M / T::BM + a.G, a.M) : ((int64_t)a.M + T::BM - 1) / T::BM;
   const int64_t cols = a.out_scales ? LX_MX8_KP((int64_t)a.cols) : a.cols, items = tiles * ((cols + OC - 1) / OC);
   const unsigned grid = (unsigned)std::min<int64_t>((items + 7) / 8 * 8, 256 * T::PER_CU);
-  // a bf16 result is rounded by 2^-9: next to it what one instruction drops does not count
-  if (a.out_scales || a.out_f32)
-    k_mx8_gemm_tile<T, GLU, true><<<grid, T::THR, 0, s>>>(a);
-  else
-    k_mx8_gemm_tile<T, GLU, false><<<grid, T::THR, 0, s>>>(a);
+  k_mx8_gemm_tile<T, GLU><<<grid, T::THR, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -615,14 +610,13 @@ hipError_t launch(const Mx8GemmArgs& a, hipStream_t s) {
 
 // Which kernel: the one with the least time by a model of rounds. A round is what the
 // compute units take at once, in us per 4096 values of K (`half` where there are so few
-// tiles that they share nothing) and besides, for filling and writing out; for results
-// in bf16, and for those of two instructions:
+// tiles that they share nothing) and besides, for filling and writing out:
 //                  half      full      besides        tiles at once
 //   16 x 32        5.5       5.5       1.3            256          (rows4)
 //   16 x 64        16        27        3              512, 1024    (rows; with SwiGLU 16 x 128, 18, 45)
-//   64 x 128       17, 21    19, 27    3.5, 4.5       256, 512
-//   128 x 128      19, 33    30, 51    6, 7           256, 512
-//   256 x 256      47, 75    47, 75    22, 28         256          (with SwiGLU 12 besides)
+//   64 x 128       21        27        4.5            256, 512
+//   128 x 128      33        51        7              256, 512
+//   256 x 256      75        75        28             256          (with SwiGLU 12 besides)
 // Of groups' rows only the mean is known: their last tiles are taken to be half full. Of
 // those the wider tiles leave out what lies past them (`last`: the rows that they cost), up
 // to where they wait for the weights, at 0.8 of a full tile. Over 250 drawn sizes (17 .. 16384 rows,
@@ -630,10 +624,10 @@ hipError_t launch(const Mx8GemmArgs& a, hipStream_t s) {
 // than the best of the five, 38% at worst. us of rows4, rows, 64, 128, 256:
 //   512 x 1536 x 2048, 128 groups, SwiGLU to 8 bits     74  44  50  56  83
 //   2048 x 1536 x 2048, 128 groups, the same           118  70  50  56  84
-//   32768 x 2048 x 768, 128 groups, fp32              1088   -  196 167 202
-//   3001 x 4096 x 14336, bf16                         1853   -  206 180 190
-//   8192 x 8192 x 8192, bf16                             -   -  825 532 432
-Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool exact, bool swiglu) {
+//   32768 x 2048 x 768, 128 groups, fp32              1080 627  202 171 223
+//   3001 x 4096 x 14336, bf16                            -   -  314 291 310
+//   8192 x 8192 x 8192, bf16                             -   -  913 893 723
+Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool swiglu) {
   Mx8GemmPlan p{};
   const int64_t groups = G > 1 ? std::min(M, G) : 1;
   p.kernel = Mx8GemmPlan::kTile64;
@@ -649,9 +643,9 @@ Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool exact, bool swiglu) 
       p.kernel = k;
     }
   };
-  offer(Mx8GemmPlan::kTile64, 64, 128, 32, 512, 256, exact ? 21 : 17, exact ? 27 : 19, exact ? 4.5 : 3.5);
-  offer(Mx8GemmPlan::kTile128, 128, 128, 32, 512, 256, exact ? 33 : 19, exact ? 51 : 30, exact ? 7 : 6);
-  offer(Mx8GemmPlan::kTile256, 256, 256, 64, 256, 256, exact ? 75 : 47, exact ? 75 : 47, swiglu ? 12 : exact ? 28 : 22);
+  offer(Mx8GemmPlan::kTile64, 64, 128, 32, 512, 256, 21, 27, 4.5);
+  offer(Mx8GemmPlan::kTile128, 128, 128, 32, 512, 256, 33, 51, 7);
+  offer(Mx8GemmPlan::kTile256, 256, 256, 64, 256, 256, 75, 75, swiglu ? 12 : 28);
   offer(Mx8GemmPlan::kRows4, 16, 32, 8, 256, 256, 5.5, 5.5, 1.3);
   if (G > 1) offer(Mx8GemmPlan::kRows, 16, swiglu ? 128 : 64, 8, 1024, 512, swiglu ? 18 : 16, swiglu ? 45 : 27, 3);
   return p;

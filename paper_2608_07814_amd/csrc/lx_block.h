@@ -126,8 +126,7 @@ hipError_t launch_mx4_gemm_sum(const Mx4GemmArgs& a, hipStream_t s);
 struct Mx8GemmPlan {
   enum Kernel : int32_t { kRows, kRows4, kTile64, kTile128, kTile256 } kernel;
 };
-// exact: the result is in fp32 or 8 bits (two instructions per product).
-Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool exact, bool swiglu);
+Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool swiglu);
 struct Mx8GemmArgs {
   const uint8_t *a, *as, *b, *bs;
   int32_t a_rows;
