@@ -209,9 +209,8 @@ lx_status lx_mx4_gemm(const void* a, const void* a_scales, int32_t a_rows, const
  * x [d][f]. Only the chosen experts' weights are read, each once per 16 of its
  * tokens; a NaN scale or an infinite activation reaches the tokens that it is
  * multiplied for only. Weights below 2^-126 under a block's scale may count as 0.
- * Sums are formed in fp32; with a bf16 out the activations between the two
- * products keep 16 bits (next to the 8 of the result), with fp32 all 24. out
- * [T][d]. d and f multiples of 8, at most 2^20, E in 1 .. LX_MAX_NODES, k in 1 ..
+ * Sums are formed in fp32, and the activations between the two products keep its
+ * 24 bits. out [T][d]. d and f multiples of 8, at most 2^20, E in 1 .. LX_MAX_NODES, k in 1 ..
  * LX_MAX_K (LX_ERR_UNSUPPORTED; T over the most as well). All 16-byte aligned but
  * ids, weights and scales (4); workspace 256-byte aligned, as many bytes as the
  * function before says. */

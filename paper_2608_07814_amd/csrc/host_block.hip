@@ -185,8 +185,7 @@ lx_status check_few(int32_t T, int32_t k, int32_t E, int32_t d, int32_t f) {
 struct FewLayout {
   size_t unit, counter, part, hidden, total;
 };
-// Fills in a's split and the workspace's layout (for fp32 results, whose hidden
-// activations take more).
+// Fills in a's split and the workspace's layout.
 FewLayout few_layout(FewArgs& a) {
   a.units = std::min(a.E, a.T * a.k);
   few_plan(a);

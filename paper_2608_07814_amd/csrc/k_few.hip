@@ -28,7 +28,6 @@ namespace {
 
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef uint32_t vu4w __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t vu2 __attribute__((ext_vector_type(2)));
 
 // 8 codes under the scale f, as bf16.
 __device__ __forceinline__ bf8 read8(uint32_t codes, float f) {
@@ -38,11 +37,11 @@ __device__ __forceinline__ bf8 read8(uint32_t codes, float f) {
 }
 
 // An fp32 value as three bf16 terms that add up to it exactly: its upper 8 bits (cut
-// off, so that none overflows), those of the rest (rounded to nearest: without the
-// third term the error is at most 2^-16 of the value), and the remainder. Infinities
-// and NaN are the first term alone.
+// off, so that none overflows), those of the rest (rounded to nearest), and the
+// remainder. Infinities and NaN are the first term alone.
+constexpr int kTerms = 3;
 struct Terms {
-  uint32_t t[3];  // in the upper halves
+  uint32_t t[kTerms];  // in the upper halves
 };
 __device__ __forceinline__ Terms terms(float x) {
   Terms r;
@@ -63,7 +62,7 @@ __device__ __forceinline__ uint32_t two(uint32_t lo, uint32_t hi) { return lo >>
 // x (T d is at most 2^26; not `there`: zeros), and as terms.
 template <bool F32>
 struct Acts {
-  static constexpr int N = F32 ? 3 : 1, R = F32 ? 2 : 1;
+  static constexpr int N = F32 ? kTerms : 1, R = F32 ? 2 : 1;
   vu4 r[R];
   __device__ __forceinline__ void load(const void* x, uint32_t row, bool there, int c, int K) {
 #pragma unroll
@@ -94,7 +93,7 @@ struct Acts {
         for (int j = 0; j < 4; ++j) {
           const Terms u = terms(__uint_as_float(r[j / 2][j % 2 * 2])), v = terms(__uint_as_float(r[j / 2][j % 2 * 2 + 1]));
 #pragma unroll
-          for (int n = 0; n < 3; ++n) t[n][j] = two(u.t[n], v.t[n]);
+          for (int n = 0; n < kTerms; ++n) t[n][j] = two(u.t[n], v.t[n]);
         }
       }
     }
@@ -217,7 +216,7 @@ __device__ __forceinline__ int token_list(uint64_t mask) {
 // a load instruction of the second launch takes, 8 values of each block of every token,
 // is contiguous. `cols`: the tokens of the 16.
 __device__ __forceinline__ uint16_t* hidden_of(const FewArgs& a, int base, int c0) {
-  return a.hidden + (int64_t)(base + c0) * a.planes * LX_MX4_KP(a.f);
+  return a.hidden + (int64_t)(base + c0) * kTerms * LX_MX4_KP(a.f);
 }
 __device__ __forceinline__ int64_t hidden_at(int fp, int term, int step, int j, int q, int cols, int col) {
   return ((int64_t)term * fp / 8 + ((step * 4 + j) * 4 + q)) * cols * 8 + col * 8;
@@ -238,7 +237,7 @@ __device__ __forceinline__ int64_t hidden_at(int fp, int term, int step, int j, 
 // on the same codes (64 tokens on 8 experts 338 for 349, 61 on 128 89 for 85).
 template <bool F32>
 __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
-  constexpr int N = F32 ? 3 : 1;
+  constexpr int N = F32 ? kTerms : 1;
   __shared__ __attribute__((aligned(16))) uint8_t stage[4][2][kStage];
   __shared__ float weight[64];
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -371,8 +370,7 @@ __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
       const Terms h = terms(at < a.f ? silu(g) * z * weight[c0 + col] : 0.f);
       uint16_t* const p = hidden_of(a, c.base, c0) + e8;
 #pragma unroll
-      for (int m = 0; m < 3; ++m)
-        if (m < a.planes) p[hidden_at(fp, m, at / 128, at / 8 % 4, at / 32 % 4, cols, col)] = (uint16_t)(h.t[m] >> 16);
+      for (int m = 0; m < kTerms; ++m) p[hidden_at(fp, m, at / 128, at / 8 % 4, at / 32 % 4, cols, col)] = (uint16_t)(h.t[m] >> 16);
     }
     __syncthreads();
   }
@@ -393,8 +391,8 @@ __device__ __forceinline__ float load_dev(const float* p) {
 // stored and loaded coherently and complete before the counter is raised, which is all
 // the order that it needs (fences, which write back and empty whole caches, took the
 // launch from 93 to 205 us).
-// TERMS of the hidden activations are multiplied: for a bf16 output two (2^-16 of a value
-// at most, next to the 2^-9 that the output is rounded by), for fp32 all three. They are
+// All terms of the hidden activations are multiplied, for a bf16 output too (with two,
+// 2^-16 of a value at most, too little is left where sums cancel). They are
 // columns of one instruction side by side, PACKED tokens at a time, so that a batch's
 // activations fit in registers and are asked for together with its codes: there is one
 // wait to a batch (term by term, a step ahead: 87 for 66 us, 5 tokens on experts of 14336
@@ -402,9 +400,8 @@ __device__ __forceinline__ float load_dev(const float* p) {
 // of these). Weights at 3.1 and 2.0 TB/s. A workgroup to an expert and 16 to 64 columns,
 // its products joined by the last one or by a third launch, took 30% or 0 to 20% longer.
 constexpr int kDownWaves = 16;
-template <int TERMS>
 __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a) {
-  constexpr int U = kBatch, PACKED = 16 / TERMS;
+  constexpr int U = kBatch, PACKED = 16 / kTerms;
   __shared__ __attribute__((aligned(16))) uint8_t stage[kDownWaves][kStage];
   // [kDownWaves][T][16] sums, then three words for each unit with tokens
   extern __shared__ __attribute__((aligned(16))) float sums[];
@@ -442,7 +439,7 @@ __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a
     for (int r = 0; r < 4; ++r) {  // the terms' sums, the least first
       float s = 0.f;
 #pragma unroll
-      for (int m = TERMS - 1; m > 0; --m) s += __uint_as_float(__builtin_amdgcn_ds_bpermute((lane + m * PACKED) * 4, (int)__float_as_uint(acc[r])));
+      for (int m = kTerms - 1; m > 0; --m) s += __uint_as_float(__builtin_amdgcn_ds_bpermute((lane + m * PACKED) * 4, (int)__float_as_uint(acc[r])));
       acc[r] += s;
     }
     const int t = __builtin_amdgcn_ds_bpermute(min(c0 + l16, count - 1) * 4, token);
@@ -473,7 +470,7 @@ __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a
       int l = lane;
       asm volatile("" : "+v"(l));  // (what follows from it is not kept over the batches)
       // (columns without a token, and steps past the last, repeat some that are there)
-      const int m = min((l & 15) / PACKED, TERMS - 1), col = min((l & 15) % PACKED, to - c0 - 1);
+      const int m = min((l & 15) / PACKED, kTerms - 1), col = min((l & 15) % PACKED, to - c0 - 1);
       const uint32_t own = ((uint32_t)(m * (fp / 8) + (l >> 4)) * cols + col) * 16;
       vu4 x[U][4];
 #pragma unroll
@@ -538,7 +535,6 @@ void few_plan(FewArgs& a) {
   const int64_t steps = (int64_t)a.units * ((a.f + 127) / 128), most = (steps + kDownWaves * kBatch - 1) / (kDownWaves * kBatch);
   a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, 256 / cols, 8}));
   a.counters = a.splits > 1 ? cols : 0;
-  a.planes = a.out_f32 ? 3 : 2;
 }
 
 hipError_t launch_few_up(const FewArgs& a, hipStream_t s) {
@@ -550,24 +546,21 @@ hipError_t launch_few_up(const FewArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int TERMS>
-static hipError_t launch_down(const FewArgs& a, hipStream_t s) {
+hipError_t launch_few_down(const FewArgs& a, hipStream_t s) {
   // next to the codes' 64 KB the sums and the units take up to 88 KB
   static DeviceOnce once;
   int device = 0;
   hipError_t e = hipGetDevice(&device);
   if (e == hipSuccess)
     e = once.run(device, hipSuccess, [] {
-      return hipFuncSetAttribute((const void*)k_few_down<TERMS>, hipFuncAttributeMaxDynamicSharedMemorySize,
+      return hipFuncSetAttribute((const void*)k_few_down, hipFuncAttributeMaxDynamicSharedMemorySize,
                                  LX_MOE_FEW_MAX_T * (kDownWaves * 16 * (int)sizeof(float) + LX_MAX_K * 12));
     });
   if (e != hipSuccess) return e;
   const unsigned grid = (unsigned)((a.d + 15) / 16) * a.splits;
   const size_t lds = a.units * 12 + (size_t)kDownWaves * a.T * 16 * sizeof(float);
-  k_few_down<TERMS><<<grid, kDownWaves * 64, lds, s>>>(a);
+  k_few_down<<<grid, kDownWaves * 64, lds, s>>>(a);
   return hipGetLastError();
 }
-
-hipError_t launch_few_down(const FewArgs& a, hipStream_t s) { return a.out_f32 ? launch_down<3>(a, s) : launch_down<2>(a, s); }
 
 }  // namespace lx

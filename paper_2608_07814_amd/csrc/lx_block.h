@@ -157,15 +157,15 @@ struct FewArgs {
   const uint8_t *gu, *gu_s, *down, *down_s;
   void* out;
   int32_t units;         // min(E, T k): the experts, or the slots
-  int32_t splits, counters, planes;  // few_plan
+  int32_t splits, counters;  // few_plan
   // left by the first launch for the second, per unit: its expert (-1: it has no
   // tokens), the first of its rows of hidden, and its tokens as bits
   FewUnit* unit;         // [units]
-  uint16_t* hidden;      // [T k][planes][LX_MX4_KP(f)]: bf16 terms
+  uint16_t* hidden;      // [T k][3][LX_MX4_KP(f)]: bf16 terms
   int32_t* counter;      // [counters], cleared by the first launch
   float* part;           // splits > 1: [d / 16][splits][T][16]
 };
-// From T, d, f, units and out_f32 the split of the work.
+// From d, f and units the split of the work.
 void few_plan(FewArgs& a);
 hipError_t launch_few_up(const FewArgs& a, hipStream_t s);
 hipError_t launch_few_down(const FewArgs& a, hipStream_t s);
