@@ -92,7 +92,8 @@ lx_status lx_block_norm_backward(const lx_norm_layer* layer, int32_t T, const vo
  * and scale:
  *
  *   h_out  = residual_scale h + gate_t scale_c drop(v)_tc
- *   drop(v)_tc = v_tc / (1 - q) if u_tc >= 65536 q, else 0 (whatever v_tc holds)
+ *   drop(v)_tc = v_tc / (1 - q) if u_tc >= 65536 q, else 0 (and scale_c drop(v)_tc
+ *                too, whatever y_tc, w_post_c and scale_c hold)
  *
  * with q = p rounded to a multiple of 2^-16, 0 <= q < 1 (p from 1 - 2^-17 on is
  * refused), and 16 random bits u_tc from Philox4x32 of ten rounds: key = the

@@ -111,21 +111,21 @@ __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) 
     const int64_t t = t0 + g, row = t * a.d;
     const bool live = t < a.T;
     // with dropout: the columns that are kept, formed as in the forward; a dropped
-    // value counts as 0 whatever it holds
+    // value's product with its weight counts as 0 whatever they hold
     auto mask = [&](int i) __attribute__((always_inline)) {
       if constexpr (DROP) return dropout_kept(a.drop, keys, col(i) / 8, (uint32_t)t);
       return 0u;
     };
-    auto drop = [&](float v, uint32_t kept, int e) __attribute__((always_inline)) {
-      if constexpr (DROP) return kept >> e & 1 ? v * a.drop.scale : 0.f;
-      return v;
+    auto drop = [&](float v, float w, uint32_t kept, int e) __attribute__((always_inline)) {
+      if constexpr (DROP) return kept >> e & 1 ? w * (v * a.drop.scale) : 0.f;
+      return w * v;
     };
     float s[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     auto add = [&](const Row& q, const Weights& w, uint32_t kept) __attribute__((always_inline)) {
       const F8 m = unpack8(q.m, a.h_f32), y = unpack8(q.y, a.y_f32), D = unpack8(q.D, a.h_f32), dx = unpack8(q.dx, a.x_f32);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float dm = dx.v[e] * w.pre.v[e], sy = w.s.v[e] * drop(y.v[e], kept, e);
+        const float dm = dx.v[e] * w.pre.v[e], sy = drop(y.v[e], w.s.v[e], kept, e);
         s[0] += m.v[e] * m.v[e];
         s[1] += y.v[e] * y.v[e];
         s[2] += dm * m.v[e];
@@ -172,12 +172,12 @@ __global__ __launch_bounds__(kBwd) void k_block_norm_grad(const NormGradArgs a) 
       for (int e = 0; e < 8; ++e) {
         const float mm = m.v[e] * rh, n = y.v[e] * ry, d = D.v[e] + rh * (dx.v[e] * w.pre.v[e] - mm * mean);
         sp[i].v[e] += dx.v[e] * mm;
-        sq[i].v[e] += gate * d * drop(n, kept, e);
+        sq[i].v[e] += gate * d * drop(n, 1.f, kept, e);
         dh.v[e] = alpha * d;
         // (without w_post zn is 0 and dy does not depend on y, which may be infinite or
         // NaN: its product with 0 must not count. With w_post zn is NaN then. A
         // choice by a.w_post took 71 for 62 us at 1024 x 16384)
-        dy.v[e] = ry * gate * (d * drop(w.s.v[e], kept, e) - __builtin_amdgcn_fmed3f(n, -FLT_MAX, FLT_MAX) * zn);
+        dy.v[e] = ry * gate * (d * drop(w.s.v[e], 1.f, kept, e) - __builtin_amdgcn_fmed3f(n, -FLT_MAX, FLT_MAX) * zn);
       }
       if (col(i) < a.d && live) {
         store8(a.dh, a.h_f32, row + col(i), dh);
@@ -243,8 +243,10 @@ __global__ __launch_bounds__(1024) void k_block_norm_grad_sum(const NormGradArgs
   auto w1 = [&](const void* p) {
     return !p ? 1.f : a.w_f32 ? ((const float*)p)[c] : __uint_as_float((uint32_t)((const uint16_t*)p)[c] << 16);
   };
-  if (a.dw_post) a.dw_post[c] = w1(a.scale) * s;
-  if (a.dscale) a.dscale[c] = w1(a.w_post) * s;
+  // (with dropout a column that every token drops has 0, whatever its weights hold)
+  const bool none = a.drop.rng && s == 0.f;
+  if (a.dw_post) a.dw_post[c] = none ? 0.f : w1(a.scale) * s;
+  if (a.dscale) a.dscale[c] = none ? 0.f : w1(a.w_post) * s;
 }
 
 // Lanes of a row and groups of 8 columns per lane: a row's lanes hold one group

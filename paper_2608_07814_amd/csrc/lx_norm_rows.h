@@ -136,10 +136,10 @@ __device__ __forceinline__ void block_norm_rows(const NormArgs& a, float* lds, P
       for (int i = 0; i < NV; ++i) {
         h[i] = unpack8(rh[i], h_f32);
         if constexpr (DROP) {
-          // (a dropped value counts as 0 even where the row's factor is not finite)
+          // (a dropped value adds 0 even where the row's factor or a weight is not finite)
           const uint32_t kept = dropout_kept(a.drop, keys, col[i] / 8, (uint32_t)t);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) h[i].v[e] = a.alpha * h[i].v[e] + gate * ((kept >> e & 1 ? f * y[i].v[e] : 0.f) * sw[i].v[e]);
+          for (int e = 0; e < 8; ++e) h[i].v[e] = a.alpha * h[i].v[e] + gate * (kept >> e & 1 ? f * y[i].v[e] * sw[i].v[e] : 0.f);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) h[i].v[e] = a.alpha * h[i].v[e] + f * (y[i].v[e] * sw[i].v[e]);
