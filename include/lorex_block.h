@@ -264,7 +264,10 @@ lx_status lx_mx8_dequantize(const void* codes, const void* scales, int64_t rows,
  * LX_MAX_NODES. A, B and out 16-byte, scales, row_map and offsets 4-byte aligned;
  * workspace 256-byte aligned, lx_mx8_gemm_workspace_bytes bytes (NULL where that is
  * 0). Products are exact in fp32, whatever the result's type. The order in which a sum
- * is formed depends on the sizes, G and act, not on the values or the result's type. */
+ * is formed depends on the sizes, G and act, not on the values or the result's type, and
+ * for more than a few rows on whether A's codes or a group's weights reach 2^32 bytes (or
+ * a_rows is 0): from there on the kernels of few rows run, which read a group's weights
+ * once per 16 rows; rows that are gathered from that far are better copied together first. */
 typedef enum lx_act { LX_ACT_NONE = 0, LX_ACT_SILU = 1, LX_ACT_GELU = 2, LX_ACT_SWIGLU = 3 } lx_act;
 typedef struct lx_epilogue {
   lx_act act;

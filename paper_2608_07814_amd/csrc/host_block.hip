@@ -436,10 +436,12 @@ lx_status lx_mx8_gemm(const void* a, const void* a_scales, int32_t a_rows, const
   g.out_f32 = out_dtype == LX_F32;
   g.out = out;
   g.out_scales = (uint8_t*)out_scales;
-  g.plan = mx8_gemm_plan(M, N, g.Kp, G, e.act == LX_ACT_SWIGLU);
-  // the tile kernels address A and a group's weights by 32-bit byte offsets
+  // the tile kernels address A, of which they read at least a row, and a group's weights by
+  // 32-bit byte offsets; the row kernels' have 64 bits
   const int64_t most = (int64_t)1 << 32;
-  if (a_rows == 0 || (int64_t)a_rows * g.Kp >= most || (int64_t)N * (g.Kp / 2) >= most) g.plan.kernel = Mx8GemmPlan::kRows;
+  const bool far = a_rows == 0 || (int64_t)a_rows * g.Kp >= most || (int64_t)N * (g.Kp / 2) >= most;
+  g.plan = mx8_gemm_plan(M, N, g.Kp, G, e.act == LX_ACT_SWIGLU, false);
+  if (far && g.plan.tile()) g.plan = mx8_gemm_plan(M, N, g.Kp, G, e.act == LX_ACT_SWIGLU, true);
   return run("mx8_gemm", launch_mx8_gemm, g, stream);
 }
 

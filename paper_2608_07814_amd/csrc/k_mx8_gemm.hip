@@ -621,16 +621,17 @@ hipError_t launch(const Mx8GemmArgs& a, hipStream_t s) {
 // those the wider tiles leave out what lies past them (`last`: the rows that they cost), up
 // to where they wait for the weights, at 0.8 of a full tile. Over 250 drawn sizes (17 .. 16384 rows,
 // 256 .. 14336 columns, K of 64 .. 14336, 1 .. 128 groups) the choice takes 1.5% longer
-// than the best of the five, 38% at worst. us of rows4, rows, 64, 128, 256:
+// than the best of the five, 38% at worst; between the two row kernels alone (where operands
+// reach 2^32 bytes), over 393, 1.2%, 27% at worst. us of rows4, rows, 64, 128, 256:
 //   512 x 1536 x 2048, 128 groups, SwiGLU to 8 bits     74  44  50  56  83
 //   2048 x 1536 x 2048, 128 groups, the same           118  70  50  56  84
 //   32768 x 2048 x 768, 128 groups, fp32              1080 627  202 171 223
 //   3001 x 4096 x 14336, bf16                            -   -  314 291 310
 //   8192 x 8192 x 8192, bf16                             -   -  913 893 723
-Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool swiglu) {
+Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool swiglu, bool rows_only) {
   Mx8GemmPlan p{};
   const int64_t groups = G > 1 ? std::min(M, G) : 1;
-  p.kernel = Mx8GemmPlan::kTile64;
+  p.kernel = Mx8GemmPlan::kRows;
   double best = 0;
   auto offer = [&](Mx8GemmPlan::Kernel k, int64_t bm, int64_t bn, double last, int at_once, int few, double half, double full, double besides) {
     const double m = M, in_parts = G > 1 ? m + groups * (bm / 2) : m;  // rows with the last tiles full
@@ -643,11 +644,13 @@ Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool swiglu) {
       p.kernel = k;
     }
   };
-  offer(Mx8GemmPlan::kTile64, 64, 128, 32, 512, 256, 21, 27, 4.5);
-  offer(Mx8GemmPlan::kTile128, 128, 128, 32, 512, 256, 33, 51, 7);
-  offer(Mx8GemmPlan::kTile256, 256, 256, 64, 256, 256, 75, 75, swiglu ? 12 : 28);
+  if (!rows_only) {
+    offer(Mx8GemmPlan::kTile64, 64, 128, 32, 512, 256, 21, 27, 4.5);
+    offer(Mx8GemmPlan::kTile128, 128, 128, 32, 512, 256, 33, 51, 7);
+    offer(Mx8GemmPlan::kTile256, 256, 256, 64, 256, 256, 75, 75, swiglu ? 12 : 28);
+  }
   offer(Mx8GemmPlan::kRows4, 16, 32, 8, 256, 256, 5.5, 5.5, 1.3);
-  if (G > 1) offer(Mx8GemmPlan::kRows, 16, swiglu ? 128 : 64, 8, 1024, 512, swiglu ? 18 : 16, swiglu ? 45 : 27, 3);
+  if (G > 1 || rows_only) offer(Mx8GemmPlan::kRows, 16, swiglu ? 128 : 64, 8, 1024, 512, swiglu ? 18 : 16, swiglu ? 45 : 27, 3);
   return p;
 }
 

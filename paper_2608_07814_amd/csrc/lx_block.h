@@ -125,8 +125,10 @@ hipError_t launch_mx4_gemm_sum(const Mx4GemmArgs& a, hipStream_t s);
 // Products of 8-bit activations and 4-bit weights.
 struct Mx8GemmPlan {
   enum Kernel : int32_t { kRows, kRows4, kTile64, kTile128, kTile256 } kernel;
+  bool tile() const { return kernel >= kTile64; }
 };
-Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool swiglu);
+// rows_only: the tile kernels cannot run.
+Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool swiglu, bool rows_only);
 struct Mx8GemmArgs {
   const uint8_t *a, *as, *b, *bs;
   int32_t a_rows;
