@@ -250,8 +250,10 @@ lx_status lx_mx8_dequantize(const void* codes, const void* scales, int64_t rows,
  *   out[m][n] = act(z[m][n]) + residual[m][n]
  *
  * LX_ACT_SWIGLU: B's N rows are N / 2 gate rows, then N / 2 up rows, and out [M][N
- * / 2] = silu(z[m][n]) z[m][N / 2 + n] + residual[m][n]; GELU is z Phi(z). A: codes
- * [a_rows][LX_MX8_KP(K)] and scales; B: as in lx_mx4_gemm; row_map, offsets, G, M,
+ * / 2] = silu(z[m][n]) z[m][N / 2 + n] + residual[m][n]; GELU is z Phi(z). (silu here is by
+ * the exponential and reciprocal instructions, in lx_mx8_quantize by expf and a division: a
+ * value next to the border of two codes may get either.) A: codes [a_rows][LX_MX8_KP(K)] and
+ * scales; B: as in lx_mx4_gemm; row_map, offsets, G, M,
  * rows of no group and map entries out of range (a product of 0 then, bias,
  * activation and residual as for any other row) as there. bias [G][N], residual
  * [M][columns], fp32 or bf16 each, aligned to their type; epilogue NULL: neither,

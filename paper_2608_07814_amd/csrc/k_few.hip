@@ -228,13 +228,14 @@ __device__ __forceinline__ int64_t hidden_at(int fp, int term, int step, int j, 
 // first does the work. Many short workgroups hide each other's waits: several tiles to
 // a workgroup in turn, the next one's weights on their way, took a third longer. The
 // results go to a.hidden as bf16 terms. Experts of 14336 x 4096, 5 tokens on 6 or 7 of
-// them: 97 us, the weights at 4.2 TB/s; of 768 x 2048, 61 tokens on 90 of 128: 48 us, 3.1
+// them: 90 to 96 us, the weights at 4.3 TB/s; of 768 x 2048, 61 tokens on 90 of 128: 47 us, 3.2
 // (the first-level cache is asked for something in every cycle: by 16 loads of activations
 // a batch, most of whose lanes have no token, next to 8 of codes). Both launches with fp32
 // activations take 20 to 35% longer, for the instructions that split them. Tried and no
 // faster: a tile of its own for each wavefront where rows are short; x through LDS (64
 // tokens on 8 experts 182 for 205, most others a little slower); four sets of 16 tokens
-// on the same codes (64 tokens on 8 experts 338 for 349, 61 on 128 89 for 85).
+// on the same codes (both launches, with two terms of the hidden activations: 64 tokens on 8
+// experts 338 for 349, 61 on 128 89 for 85).
 template <bool F32>
 __global__ __launch_bounds__(256, 4) void k_few_up(const FewArgs a) {
   constexpr int N = F32 ? kTerms : 1;
@@ -395,9 +396,10 @@ __device__ __forceinline__ float load_dev(const float* p) {
 // 2^-16 of a value at most, too little is left where sums cancel). They are
 // columns of one instruction side by side, PACKED tokens at a time, so that a batch's
 // activations fit in registers and are asked for together with its codes: there is one
-// wait to a batch (term by term, a step ahead: 87 for 66 us, 5 tokens on experts of 14336
-// x 4096; 42 for 36, 61 tokens on 90 experts of 768 x 2048; 11.2 for 8.3, one token on 8
-// of these). Weights at 3.1 and 2.0 TB/s. A workgroup to an expert and 16 to 64 columns,
+// wait to a batch. 5 tokens on 6 or 7 experts of 14336 x 4096 65 us, the weights at 3.1
+// TB/s; 61 tokens on 90 experts of 768 x 2048 51, 1.5 TB/s (with two terms, eight tokens to an
+// instruction, 36); one token on 8 of these 8. Term by term, a step ahead, all with two:
+// 87 for 66, 42 for 36. A workgroup to an expert and 16 to 64 columns,
 // its products joined by the last one or by a third launch, took 30% or 0 to 20% longer.
 constexpr int kDownWaves = 16;
 __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a) {
@@ -528,8 +530,8 @@ __global__ __launch_bounds__(kDownWaves * 64, 4) void k_few_down(const FewArgs a
 }  // namespace
 
 // Workgroups of a column tile of the second launch: so many that every compute unit has
-// one, but no more than leave a wavefront a batch (4 tokens on 128 experts of 768 x 2048:
-// 17 us on 256 workgroups, 19 on 128; 61 tokens: 42 on 256, 53 on 512).
+// one, but no more than leave a wavefront a batch (both launches, 4 tokens on 128 experts of
+// 768 x 2048: 27.6 us on 256 workgroups, 30.0 on 128, 31.5 on 512; 61 tokens: 97, 134, 106).
 void few_plan(FewArgs& a) {
   const int cols = (a.d + 15) / 16;
   const int64_t steps = (int64_t)a.units * ((a.f + 127) / 128), most = (steps + kDownWaves * kBatch - 1) / (kDownWaves * kBatch);

@@ -9,8 +9,9 @@ namespace {
 
 // Both directions are bound by memory, but for SwiGLU's exponential and quotient. A
 // lane has 8 values of a row, 4 lanes share a block of 32; rows as in the 4-bit
-// rounding. Rounding 3001 x 14336 in bf16 27 us (130 MB, 4.9 TB/s), 8192 x 4096 22, 4096 x
-// 4096 9; reading 8192 x 4096 back 16.4 (102 MB, 6.2 TB/s, in part from cache).
+// rounding. Rounding 3001 x 14336 in bf16 27 us (130 MB, 4.9 TB/s), 8192 x 4096 22 to 24, 4096 x
+// 4096 9; with SwiGLU 3001 x 14336 in bf16 64 (216 MB, 3.4 TB/s), 32768 x 768 53 (2.4), in
+// fp32 46 (5.0); reading 8192 x 4096 back 16.4 (102 MB, 6.2 TB/s, in part from cache).
 template <int U, bool SWIGLU>
 __global__ __launch_bounds__(256) void k_mx8_quantize(const Mx4Args a, int tpr) {
   const int Kp = LX_MX8_KP(a.K);

@@ -616,18 +616,22 @@ hipError_t launch(const Mx8GemmArgs& a, hipStream_t s) {
 //   16 x 64        16        27        3              512, 1024    (rows; with SwiGLU 16 x 128, 18, 45)
 //   64 x 128       21        27        4.5            256, 512
 //   128 x 128      33        51        7              256, 512
-//   256 x 256      75        75        28             256          (with SwiGLU 12 besides)
+//   256 x 256      75        75        28             256          (with SwiGLU, half the results, 12)
 // Of groups' rows only the mean is known: their last tiles are taken to be half full. Of
 // those the wider tiles leave out what lies past them (`last`: the rows that they cost), up
-// to where they wait for the weights, at 0.8 of a full tile. Over 250 drawn sizes (17 .. 16384 rows,
-// 256 .. 14336 columns, K of 64 .. 14336, 1 .. 128 groups) the choice takes 1.5% longer
-// than the best of the five, 38% at worst; between the two row kernels alone (where operands
+// to where they wait for the weights, at 0.8 of a full tile. Over 419 sizes, all but 16 drawn
+// (17 .. 16384 rows, 256 .. 14336 columns, K of 64 .. 14336, 1 .. 128 groups), the choice takes
+// 2.4% longer than the best of the five (of those over 60 us 1.7%, 18% at worst; of shorter
+// ones 68%, at 1141 x 576 x 8640 in 64 groups: 97 for 57); with 28 besides for SwiGLU, as without it, 2.2
+// and 26% over 60 us; between the two row kernels alone (where operands
 // reach 2^32 bytes), over 393, 1.2%, 27% at worst. us of rows4, rows, 64, 128, 256:
 //   512 x 1536 x 2048, 128 groups, SwiGLU to 8 bits     74  44  50  56  83
 //   2048 x 1536 x 2048, 128 groups, the same           118  70  50  56  84
 //   32768 x 2048 x 768, 128 groups, fp32              1080 627  202 171 223
 //   3001 x 4096 x 14336, bf16                            -   -  314 291 310
 //   8192 x 8192 x 8192, bf16                             -   -  913 893 723
+//   32768 x 1536 x 2048, 128 groups, SwiGLU to 8 bits    -   -  245 239 241  (12 takes 256, 28 128)
+//   7735 x 11824 x 1368, the same in one group           -   -  285 278 220  (the same)
 Mx8GemmPlan mx8_gemm_plan(int M, int N, int Kp, int G, bool swiglu, bool rows_only) {
   Mx8GemmPlan p{};
   const int64_t groups = G > 1 ? std::min(M, G) : 1;

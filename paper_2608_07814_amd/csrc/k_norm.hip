@@ -6,10 +6,10 @@
 // row sums go over lanes by DPP, over wavefronts through LDS. Workgroups stay
 // for many rows, so the weight vectors are read once per workgroup. Measured:
 // forward 8192 x 4096 (fp32 output of the block, bf16 streams) 68 us, 4.9 TB/s; all
-// in bf16 46 us (268 MB, 5.9 TB/s, in part from cache), with dropout 48.5; 4096 x 2048
+// in bf16 46 us (268 MB, 5.9 TB/s, in part from cache), with dropout 49; 4096 x 2048
 // with 8 experts' fp32 rows combined 57 us (319 MB, in part from cache);
 // backward 8192 x 4096 (fp32 stream) 126 us, 4.8 TB/s (with dropout 123 of 606 MB; all in
-// bf16 76, with dropout 84: the generator's 20 wide products a group of 8 columns show
+// bf16 77, with dropout 85: the generator's 20 wide products a group of 8 columns show
 // where the row kernel is not waiting for memory); a large copy reaches 5.45.
 #include "lx_block.h"
 #include "lx_norm_rows.h"

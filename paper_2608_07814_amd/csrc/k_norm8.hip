@@ -1,8 +1,9 @@
 // The block norms with the next block's input in 8 bits (formulas in lorex_block.h):
 // the rows of k_norm.hip, whose lanes hold 8 consecutive columns each, so that four
 // of them share a block and its scale goes over them by DPP. Bound by memory like
-// the norms with a bf16 output, of which this writes half: 8192 x 4096 in bf16 45 us (236
-// MB, 5.3 TB/s), 2048 x 8192 27, one row of 2048 with 8 experts' fp32 rows 5.0.
+// the norms with a bf16 output, of which this writes half: 8192 x 4096 in bf16 46 us over
+// four sets of inputs in turn (236 MB, 5.2 TB/s), 48 to 53 where its result is read back in
+// between, 2048 x 8192 27, one row of 2048 with 8 experts' fp32 rows 5.0.
 #include "lx_block.h"
 #include "lx_mx8.h"
 #include "lx_norm_rows.h"
