@@ -243,8 +243,8 @@ __global__ __launch_bounds__(1024) void k_block_norm_grad_sum(const NormGradArgs
   auto w1 = [&](const void* p) {
     return !p ? 1.f : a.w_f32 ? ((const float*)p)[c] : __uint_as_float((uint32_t)((const uint16_t*)p)[c] << 16);
   };
-  // (with dropout a column that every token drops has 0, whatever its weights hold)
-  const bool none = a.drop.rng && s == 0.f;
+  // (no tokens, and with dropout a column that all of them drop, give 0 whatever the weights hold)
+  const bool none = (a.drop.rng || a.T == 0) && s == 0.f;
   if (a.dw_post) a.dw_post[c] = none ? 0.f : w1(a.scale) * s;
   if (a.dscale) a.dscale[c] = none ? 0.f : w1(a.w_post) * s;
 }
